@@ -295,6 +295,77 @@ int fsx_backbone_info(const fsx_backbone* bb, int64_t* weight_bytes, int64_t* wo
 /* Wait for the handle's last call, then free it. */
 void fsx_backbone_destroy(fsx_backbone* bb);
 
+/* ---- Whole prompts: a cache rebuilt from scratch (Sec. 3.3: on an instruction change, a notice, an episode's end, or a
+ * history at the training window) ----
+ * Packed rows: the rows of several sequences (agents) lie in one tensor, sequence i in rows start[i] .. start[i] + len[i] - 1
+ * (HOST arrays).  The ranges need not touch or be in order; rows outside them are not touched. */
+
+/* The tensors of fsx_prompt_attention: element (row r, head h, channel c) of X is X[r * X_row + h * X_head + c].  Strides are
+ * in elements, multiples of 8; buffers are 16-byte aligned. */
+typedef struct {
+  int32_t n_heads;      /* query heads */
+  int32_t n_kv_heads;   /* key / value heads, a divisor of n_heads: query head h reads head h / (n_heads / n_kv_heads) */
+  int32_t head_dim;     /* 64 or 128 (FSX_E_UNSUPPORTED otherwise) */
+  int32_t q_dtype;      /* FSX_BF16, or FSX_F32 (rounded to bf16 as they are read); keys and values are FSX_BF16 */
+  int32_t out_dtype;    /* FSX_BF16 or FSX_F32 */
+  float scale;          /* scores = scale * q.k, > 0; 0 = 1 / sqrt(head_dim) */
+  int64_t q_rows;       /* rows that q, out and lse hold */
+  int64_t k_rows;       /* rows that k and v hold */
+  int64_t q_row, q_head, k_row, k_head, v_row, v_head, out_row, out_head;
+} fsx_prompt_desc;
+
+/* Causal attention of n_seq packed sequences (1..FSX_MAX_BATCH) in one call.
+ * Sequence i has q_len[i] new tokens, the last ones of its k_len[i] keys: new token t sees the keys
+ * j <= k_len[i] - q_len[i] + t.  k_len == q_len is a whole prompt, k_len > q_len new rows over a history (q_len = 1: the next
+ * token); a token before the first key (k_len < q_len) sees nothing, its output is 0 and its lse -infinity.  Masked keys and
+ * values may hold anything, infinities and NaN included.  The keys of different sequences may share rows (a common prefix); the
+ * rows of q may not (FSX_E_INVALID).  With strides over one layer of a BF16 cache whose rings have not wrapped, the keys are
+ * read where they stand, in either layout (k_start then counts rows of head_dim, or of H * head_dim, elements).
+ *   out       DEVICE, q's rows and heads (out_dtype)
+ *   lse       DEVICE [q_rows][n_heads] fp32, natural logarithm of each row's sum of exp(score), or NULL
+ *   k_start, k_len  NULL: q_start, q_len
+ *   workspace DEVICE, 16-byte aligned, at most workspace_bytes of it are used, for the partial results of keys that are
+ *             split over workgroups where the queries are few; with less than fsx_prompt_attention_workspace says the keys
+ *             are split less, with none (NULL, 0) not at all.  Calls that overlap must not share one.
+ * Scores, softmax statistics and sums are fp32; the probabilities are rounded to bf16 for the matrix instructions.
+ * Deterministic: the same arguments give the same bits. */
+int fsx_prompt_attention(const fsx_prompt_desc* desc, const void* q, const void* k, const void* v, void* out, float* lse,
+                         int32_t n_seq, const int64_t* q_start, const int64_t* q_len, const int64_t* k_start,
+                         const int64_t* k_len, void* workspace, int64_t workspace_bytes, void* stream);
+/* The most workspace the call would use (0: none); reads desc and the lengths only. */
+int fsx_prompt_attention_workspace(const fsx_prompt_desc* desc, int32_t n_seq, const int64_t* q_len, const int64_t* k_len,
+                                   int64_t* bytes);
+
+/* Replace the rows of layers layer .. layer + n_layers - 1 of every agent whose row_len is not 0 by packed rows (an agent with
+ * row_len 0 is left as it is, its scales too).
+ *   k_rows, v_rows  DEVICE [n_layers][total_rows][H][Dh] in rows_dtype (FSX_BF16 or FSX_F32), 16-byte aligned; agent b's rows
+ *                   are row_start[b] .. row_start[b] + row_len[b] - 1 (HOST [cache->batch])
+ *   headroom  1..64.  An FP8_E4M3 cache gets new scales, written to k_scale / v_scale: per (agent, layer, head)
+ *                   scale = max((amax / 448) * headroom, 2^-126) in fp32, amax the largest finite magnitude of the rows that
+ *                   are kept (1 where that is 0), and the codes of fsx_cache_append_rows_quantize with these scales.  Rows
+ *                   appended later may be headroom times as large before they are clamped.  Other caches: a copy, or one
+ *                   rounding (F32 rows into a BF16 cache).
+ *   policy    an agent with more rows than the ring: FSX_APPEND_RING keeps the newest `capacity`, FSX_APPEND_ERROR is
+ *                   FSX_E_CAPACITY and nothing is written
+ * The ring state of a replaced agent becomes start 0, len = the rows kept, pos = row_len, on the host before returning; layers
+ * may be replaced one call at a time (each sets the same state), and the cache is whole again after the last.  head_dim must
+ * be a multiple of 16 of at most 512; a shared cache is refused with FSX_E_UNSUPPORTED. */
+int fsx_cache_replace_rows(fsx_cache_desc* cache, int32_t layer, int32_t n_layers, const void* k_rows, const void* v_rows,
+                           int32_t rows_dtype, int64_t total_rows, const int64_t* row_start, const int64_t* row_len,
+                           float headroom, int32_t policy, void* stream);
+
+/* Read cached rows back, decoded: rows first[b] .. first[b] + row_len[b] - 1 of agent b, counted from its oldest valid row
+ * (first NULL: 0), of layers layer .. layer + n_layers - 1 into packed rows.
+ *   k_rows, v_rows  DEVICE [n_layers][total_rows][H][Dh] in rows_dtype (FSX_BF16 or FSX_F32), 16-byte aligned; agent b's rows
+ *                   go to row_start[b] .. row_start[b] + row_len[b] - 1 (HOST [cache->batch]; the ranges must not overlap);
+ *                   either may be NULL and is then not read
+ * FP8_E4M3 rows are code * scale in fp32, rounded once to rows_dtype; other rows are copied or rounded once.  first + row_len
+ * beyond the agent's valid rows is FSX_E_CAPACITY.  Shared caches are read through each agent's own start and len.  head_dim
+ * as fsx_cache_replace_rows. */
+int fsx_cache_read_rows(const fsx_cache_desc* cache, int32_t layer, int32_t n_layers, const int64_t* first, void* k_rows,
+                        void* v_rows, int32_t rows_dtype, int64_t total_rows, const int64_t* row_start,
+                        const int64_t* row_len, void* stream);
+
 /* Synchronise `stream` and report whether the ticks enqueued on this handle completed: FSX_OK, or
  * FSX_E_HIP if a tick kernel gave up on a wait (its waypoints were then written as NaN).  The
  * failure is reported once per failed tick and cleared by reporting it. */

@@ -2,12 +2,14 @@
 // launch sequence.  See include/fsx.h for the contract of every entry point.
 
 #include <algorithm>
+#include <array>
 #include <cstdio>
 #include <mutex>
 #include <cstring>
 #include <string>
 #include <vector>
 
+#include "common.h"
 #include "kernels.h"
 
 using namespace fsx;
@@ -31,6 +33,7 @@ int esize(int dtype) { return dtype == FSX_F32 ? 4 : (dtype == FSX_BF16 ? 2 : 1)
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
+constexpr int64_t MAX_PROMPT = 1 << 24;  // rows of one packed sequence
 constexpr int KSPLIT_MAX = 8;  // split factor bound of the per-phase path's split-K projections
 
 }  // namespace
@@ -878,6 +881,238 @@ extern "C" int fsx_cache_append_rows_quantize(fsx_cache_desc* cache, const void*
                                               int32_t rows_dtype, int32_t n_rows, int32_t policy, void* stream) {
   if (rows_dtype < 0) return fail(FSX_E_INVALID, "rows must be BF16 or F32");
   return append_impl(cache, k_rows, v_rows, rows_dtype, n_rows, policy, stream);
+}
+
+// ------------------------------------------------------------------------------------------------------------
+// Whole prompts: packed rows of several sequences, their attention, and the rows of a cache replaced and read back.
+
+// The ranges [start[i], start[i] + len[i]) lie in 0..rows.
+static int check_ranges(const char* what, int n, const int64_t* start, const int64_t* len, int64_t rows) {
+  for (int i = 0; i < n; ++i) {
+    if (len[i] < 0 || len[i] > MAX_PROMPT)
+      return fail(FSX_E_INVALID, std::string(what) + ": length " + std::to_string(i) + " outside 0..2^24");
+    if (start[i] < 0 || start[i] > rows - len[i])
+      return fail(FSX_E_INVALID, std::string(what) + ": rows of sequence " + std::to_string(i) + " outside 0..rows-1");
+  }
+  return FSX_OK;
+}
+
+// No two of them share a row (they are written to).
+static int check_apart(const char* what, int n, const int64_t* start, const int64_t* len) {
+  std::array<int, FSX_MAX_BATCH> ord;
+  int m = 0;
+  for (int i = 0; i < n; ++i)
+    if (len[i] > 0) ord[m++] = i;
+  std::sort(ord.begin(), ord.begin() + m, [&](int x, int y) { return start[x] < start[y]; });
+  for (int i = 1; i < m; ++i)
+    if (start[ord[i]] < start[ord[i - 1]] + len[ord[i - 1]])
+      return fail(FSX_E_INVALID, std::string(what) + ": sequences " + std::to_string(ord[i - 1]) + " and " +
+                                     std::to_string(ord[i]) + " share rows");
+  return FSX_OK;
+}
+
+static int check_prompt_desc(const fsx_prompt_desc* d) {
+  if (!d) return fail(FSX_E_INVALID, "desc is NULL");
+  if (d->n_heads < 1 || d->n_heads > 1024 || d->n_kv_heads < 1 || d->n_heads % d->n_kv_heads)
+    return fail(FSX_E_INVALID, "n_heads must be in 1..1024 and n_kv_heads one of its divisors");
+  if (d->head_dim != 64 && d->head_dim != 128) return fail(FSX_E_UNSUPPORTED, "head_dim must be 64 or 128");
+  if ((d->q_dtype != FSX_BF16 && d->q_dtype != FSX_F32) || (d->out_dtype != FSX_BF16 && d->out_dtype != FSX_F32))
+    return fail(FSX_E_UNSUPPORTED, "q and out must be BF16 or F32");
+  if (!(d->scale >= 0.f) || d->scale > 1e30f) return fail(FSX_E_INVALID, "scale must be positive, or 0 for 1 / sqrt(head_dim)");
+  if (d->q_rows < 0 || d->k_rows < 0 || d->q_rows > (int64_t)1 << 40 || d->k_rows > (int64_t)1 << 40)
+    return fail(FSX_E_INVALID, "q_rows and k_rows must be in 0..2^40");
+  for (const auto& x : {std::array<int64_t, 3>{d->q_row, d->q_head, d->q_rows}, {d->k_row, d->k_head, d->k_rows},
+                        {d->v_row, d->v_head, d->k_rows}, {d->out_row, d->out_head, d->q_rows}})
+    if (x[0] < 0 || x[1] < 0 || x[0] % 8 || x[1] % 8 || x[1] > (int64_t)1 << 50 || (__int128)x[0] * x[2] > (__int128)1 << 60)
+      return fail(FSX_E_INVALID, "strides must be non-negative multiples of 8 elements, within 2^60 elements in all");
+  return FSX_OK;
+}
+
+// Rows and heads of the output must not overlap, whichever of the two strides is the larger.
+static int check_out_strides(const fsx_prompt_desc& d) {
+  const bool head_major = d.out_head > d.out_row;
+  const int64_t lo = head_major ? d.out_row : d.out_head, hi = head_major ? d.out_head : d.out_row;
+  const int64_t n_lo = head_major ? d.q_rows : d.n_heads, n_hi = head_major ? d.n_heads : d.q_rows;
+  if ((n_lo > 1 && lo < d.head_dim) || (n_hi > 1 && hi < (__int128)(n_lo - 1) * lo + d.head_dim))
+    return fail(FSX_E_INVALID, "rows and heads of out overlap");
+  return FSX_OK;
+}
+
+extern "C" int fsx_prompt_attention_workspace(const fsx_prompt_desc* desc, int32_t n_seq, const int64_t* q_len,
+                                              const int64_t* k_len, int64_t* bytes) {
+  if (!bytes) return fail(FSX_E_INVALID, "bytes is NULL");
+  *bytes = 0;
+  const int rc = check_prompt_desc(desc);
+  if (rc) return rc;
+  if (n_seq < 1 || n_seq > FSX_MAX_BATCH) return fail(FSX_E_INVALID, "n_seq must be in 1..64");
+  if (!q_len) return fail(FSX_E_INVALID, "q_len is NULL");
+  if (!k_len) k_len = q_len;
+  for (int i = 0; i < n_seq; ++i)
+    if (q_len[i] < 0 || q_len[i] > MAX_PROMPT || k_len[i] < 0 || k_len[i] > MAX_PROMPT)
+      return fail(FSX_E_INVALID, "length " + std::to_string(i) + " outside 0..2^24");
+  g_err.clear();
+  return FSX_OK;
+}
+
+extern "C" int fsx_prompt_attention(const fsx_prompt_desc* desc, const void* q, const void* k, const void* v, void* out,
+                                    float* lse, int32_t n_seq, const int64_t* q_start, const int64_t* q_len,
+                                    const int64_t* k_start, const int64_t* k_len, void* workspace, int64_t workspace_bytes,
+                                    void* stream) {
+  int rc = check_prompt_desc(desc);
+  if (rc) return rc;
+  if (n_seq < 1 || n_seq > FSX_MAX_BATCH) return fail(FSX_E_INVALID, "n_seq must be in 1..64");
+  if (!q_start || !q_len) return fail(FSX_E_INVALID, "q_start and q_len must be non-NULL host arrays");
+  if (!k_start != !k_len) return fail(FSX_E_INVALID, "k_start and k_len must both be given or both be NULL");
+  if (!k_start) {
+    k_start = q_start;
+    k_len = q_len;
+  }
+  const fsx_prompt_desc& d = *desc;
+  if ((rc = check_out_strides(d))) return rc;
+  if ((rc = check_ranges("queries", n_seq, q_start, q_len, d.q_rows))) return rc;
+  if ((rc = check_ranges("keys", n_seq, k_start, k_len, d.k_rows))) return rc;
+  if ((rc = check_apart("queries", n_seq, q_start, q_len))) return rc;
+  if (workspace_bytes < 0 || (workspace_bytes > 0 && !workspace) || !aligned16(workspace))
+    return fail(FSX_E_INVALID, "workspace must be 16-byte aligned, of workspace_bytes >= 0 bytes");
+  PromptArgs a{};
+  int64_t rows = 0, keys = 0;
+  for (int i = 0; i < n_seq; ++i) {
+    rows += q_len[i];
+    keys += k_len[i];
+  }
+  if (rows == 0) {
+    g_err.clear();
+    return FSX_OK;
+  }
+  if (!q || !out || (keys > 0 && (!k || !v))) return fail(FSX_E_INVALID, "q, k, v and out must be non-NULL");
+  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out))
+    return fail(FSX_E_INVALID, "q, k, v and out must be 16-byte aligned");
+  if (rows * d.n_heads > (int64_t)INT32_MAX) return fail(FSX_E_UNSUPPORTED, "rows * n_heads beyond 2^31");
+  a.q = q; a.k = (const uint16_t*)k; a.v = (const uint16_t*)v; a.out = out; a.lse = lse;
+  a.q_row = d.q_row; a.q_head = d.q_head; a.k_row = d.k_row; a.k_head = d.k_head;
+  a.v_row = d.v_row; a.v_head = d.v_head; a.o_row = d.out_row; a.o_head = d.out_head;
+  a.H = d.n_heads; a.G = d.n_heads / d.n_kv_heads; a.D = d.head_dim;
+  a.q_f32 = d.q_dtype == FSX_F32; a.o_f32 = d.out_dtype == FSX_F32;
+  a.c = (d.scale > 0.f ? d.scale : 1.0f / sqrtf((float)d.head_dim)) * LOG2E;
+  for (int i = 0; i < n_seq; ++i) {
+    if (q_len[i] == 0) continue;
+    const int j = a.n_seq++;
+    a.q0[j] = q_start[i]; a.k0[j] = k_start[i]; a.nq[j] = (int32_t)q_len[i]; a.nk[j] = (int32_t)k_len[i];
+    a.row_prefix[j + 1] = a.row_prefix[j] + (int32_t)q_len[i];
+  }
+  HIP_TRY(launch_prompt_attention(a, (hipStream_t)stream));
+  g_err.clear();
+  return FSX_OK;
+}
+
+static CacheView cache_view(const fsx_cache_desc& c) {
+  CacheView cv{};
+  cv.k = c.k; cv.v = c.v; cv.k_scale = c.k_scale; cv.v_scale = c.v_scale;
+  cv.cap = c.capacity; cv.n_layers = c.n_layers; cv.dtype = c.dtype; cv.H = c.n_heads; cv.Dh = c.head_dim;
+  const bool shared = (c.layout & FSX_CACHE_SHARED) != 0, token_major = (c.layout & FSX_CACHE_TOKEN_MAJOR) != 0;
+  cv.bs = shared ? 0 : (int64_t)c.n_layers * c.n_heads * c.capacity * c.head_dim;
+  cv.sbs = shared ? 0 : c.n_layers * c.n_heads;
+  cv.hs = token_major ? c.head_dim : c.capacity * c.head_dim;
+  cv.rs = token_major ? (int64_t)c.n_heads * c.head_dim : c.head_dim;
+  return cv;
+}
+
+// What replacing and reading rows check alike.
+static int check_rows(const fsx_cache_desc* c, int32_t layer, int32_t n_layers, int32_t rows_dtype, int64_t total_rows,
+                      const int64_t* row_start, const int64_t* row_len) {
+  const int rc = validate_cache(nullptr, c, c ? c->batch : 0);
+  if (rc) return rc;
+  if (c->n_layers <= 0 || c->n_heads <= 0 || c->head_dim <= 0) return fail(FSX_E_INVALID, "cache geometry must be positive");
+  if (c->head_dim % 16 || c->head_dim > 512) return fail(FSX_E_UNSUPPORTED, "head_dim must be a multiple of 16 of at most 512");
+  if (layer < 0 || n_layers < 1 || layer > c->n_layers - n_layers)
+    return fail(FSX_E_INVALID, "layers outside 0..n_layers-1 of the cache");
+  if (rows_dtype != FSX_BF16 && rows_dtype != FSX_F32) return fail(FSX_E_INVALID, "rows must be BF16 or F32");
+  if (!row_start || !row_len) return fail(FSX_E_INVALID, "row_start and row_len must be non-NULL host arrays");
+  if (total_rows < 0) return fail(FSX_E_INVALID, "total_rows must be >= 0");
+  return check_ranges("packed rows", c->batch, row_start, row_len, total_rows);
+}
+
+static int check_row_buffers(const fsx_cache_desc* c, const void* k_rows, const void* v_rows) {
+  if (!c->k || !c->v) return fail(FSX_E_INVALID, "cache k/v pointers are NULL");
+  if (c->dtype == FSX_FP8_E4M3 && (!c->k_scale || !c->v_scale)) return fail(FSX_E_INVALID, "fp8 cache needs k_scale and v_scale");
+  if (!aligned16(k_rows) || !aligned16(v_rows) || !aligned16(c->k) || !aligned16(c->v))
+    return fail(FSX_E_INVALID, "row and cache buffers must be 16-byte aligned");
+  return FSX_OK;
+}
+
+extern "C" int fsx_cache_replace_rows(fsx_cache_desc* cache, int32_t layer, int32_t n_layers, const void* k_rows,
+                                      const void* v_rows, int32_t rows_dtype, int64_t total_rows, const int64_t* row_start,
+                                      const int64_t* row_len, float headroom, int32_t policy, void* stream) {
+  int rc = check_rows(cache, layer, n_layers, rows_dtype, total_rows, row_start, row_len);
+  if (rc) return rc;
+  if (policy != FSX_APPEND_RING && policy != FSX_APPEND_ERROR) return fail(FSX_E_INVALID, "unknown append policy");
+  if (!(headroom >= 1.f && headroom <= 64.f)) return fail(FSX_E_INVALID, "headroom must be in 1..64");
+  if (cache->layout & FSX_CACHE_SHARED)
+    return fail(FSX_E_UNSUPPORTED, "a shared cache is a set of views of one agent's rings; replace its rows through a "
+                                   "descriptor of that agent alone");
+  const int B = cache->batch;
+  RowsArgs a{};
+  for (int b = 0; b < B; ++b) {
+    if (row_len[b] > cache->capacity && policy == FSX_APPEND_ERROR)
+      return fail(FSX_E_CAPACITY, "agent " + std::to_string(b) + ": more rows than the ring holds (policy FSX_APPEND_ERROR)");
+    if (row_len[b] > 0 && cache->capacity == 0) return fail(FSX_E_CAPACITY, "the ring has no slots");
+    const int64_t n = std::min(row_len[b], cache->capacity);
+    a.n[b] = (int32_t)n;
+    a.src[b] = row_start[b] + row_len[b] - n;
+    a.slot[b] = 0;
+    a.prefix[b + 1] = a.prefix[b] + n;
+  }
+  if (a.prefix[B] == 0) {
+    g_err.clear();
+    return FSX_OK;
+  }
+  if (!k_rows || !v_rows) return fail(FSX_E_INVALID, "row pointers must be non-NULL");
+  if ((rc = check_row_buffers(cache, k_rows, v_rows))) return rc;
+  a.cv = cache_view(*cache);
+  a.cv.layer = layer;
+  a.k = const_cast<void*>(k_rows); a.v = const_cast<void*>(v_rows);
+  a.rows_f32 = rows_dtype == FSX_F32; a.layers = n_layers; a.B = B; a.total = total_rows; a.headroom = headroom;
+  HIP_TRY(launch_replace_rows(a, (hipStream_t)stream));
+  for (int b = 0; b < B; ++b)
+    if (row_len[b] > 0) {
+      cache->start[b] = 0;
+      cache->len[b] = a.n[b];
+      cache->pos[b] = row_len[b];
+    }
+  g_err.clear();
+  return FSX_OK;
+}
+
+extern "C" int fsx_cache_read_rows(const fsx_cache_desc* cache, int32_t layer, int32_t n_layers, const int64_t* first,
+                                   void* k_rows, void* v_rows, int32_t rows_dtype, int64_t total_rows,
+                                   const int64_t* row_start, const int64_t* row_len, void* stream) {
+  int rc = check_rows(cache, layer, n_layers, rows_dtype, total_rows, row_start, row_len);
+  if (rc) return rc;
+  const int B = cache->batch;
+  if ((rc = check_apart("packed rows", B, row_start, row_len))) return rc;
+  RowsArgs a{};
+  for (int b = 0; b < B; ++b) {
+    const int64_t f = first ? first[b] : 0;
+    if (f < 0) return fail(FSX_E_INVALID, "first must be >= 0");
+    if (row_len[b] > 0 && f > cache->len[b] - row_len[b])
+      return fail(FSX_E_CAPACITY, "agent " + std::to_string(b) + ": rows beyond the cache's valid ones");
+    a.n[b] = (int32_t)row_len[b];
+    a.src[b] = row_start[b];
+    a.slot[b] = row_len[b] > 0 ? (cache->start[b] + f) % cache->capacity : 0;
+    a.prefix[b + 1] = a.prefix[b] + row_len[b];
+  }
+  if (a.prefix[B] == 0 || (!k_rows && !v_rows)) {
+    g_err.clear();
+    return FSX_OK;
+  }
+  if ((rc = check_row_buffers(cache, k_rows, v_rows))) return rc;
+  a.cv = cache_view(*cache);
+  a.cv.layer = layer;
+  a.k = k_rows; a.v = v_rows;
+  a.rows_f32 = rows_dtype == FSX_F32; a.layers = n_layers; a.B = B; a.total = total_rows;
+  HIP_TRY(launch_read_rows(a, (hipStream_t)stream));
+  g_err.clear();
+  return FSX_OK;
 }
 
 extern "C" int fsx_expert_status(fsx_expert* ex, void* stream) {

@@ -50,6 +50,32 @@ __device__ __forceinline__ float e4m3_to_f32(uint8_t c) {
   return (float)r[0];
 }
 
+// E4M3 code of x / scale: RNE(clamp(x / scale, -448, 448)), NaN stays NaN.  The encoding follows the format's definition
+// step by step (exact in fp32: the quotient is rounded once by the division, the mantissa rounding is a rint of an
+// exactly scaled value), so the codes are reproducible bit for bit.
+__device__ __forceinline__ uint32_t e4m3_encode(float x, float scale) {
+  float y = x / scale;
+  if (y != y) return 0x7Fu | (__float_as_uint(y) >> 31 << 7);
+  y = fminf(fmaxf(y, -448.0f), 448.0f);
+  const uint32_t sign = __float_as_uint(y) >> 31 << 7;
+  const float a = fabsf(y);
+  uint32_t code;
+  if (a < 0.015625f) {  // below the smallest normal 2^-6: subnormal steps of 2^-9
+    code = (uint32_t)rintf(a * 512.0f);  // 8 -> the smallest normal, code 0x08
+  } else {
+    int e;
+    const float m = frexpf(a, &e);  // a = m 2^e, m in [0.5, 1)
+    uint32_t mant = (uint32_t)rintf((m * 2.0f - 1.0f) * 8.0f);
+    int ex = e - 1;
+    if (mant == 8) {
+      mant = 0;
+      ++ex;
+    }
+    code = ((uint32_t)(ex + 7) << 3) | mant;
+  }
+  return sign | code;
+}
+
 // ---------------------------------------------------------------- MFMA (16x16x32, fp32 accumulate)
 // Operand layout (wave64): lane l holds A[row = l%16][k = 8*(l/16) + j] and
 // B[k = 8*(l/16) + j][col = l%16], j = 0..7; the result lane l holds

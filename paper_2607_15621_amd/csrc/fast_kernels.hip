@@ -1342,33 +1342,8 @@ __global__ __launch_bounds__(256) void k_append(AppendArgs a) {
   a.vc[dst] = a.vs[i];
 }
 
-// Quantising append into an fp8 cache: the rows arrive in bf16 or fp32 and each element is stored as the E4M3 code
-// RNE(clamp(x / scale, -448, 448)) with the (agent, layer, head) scale the cache already has.  The encoding follows
-// the format's definition step by step (exact in fp32: the quotient is rounded once by the division, the mantissa
-// rounding is a rint of an exactly scaled value), so the codes are reproducible bit for bit.
-__device__ __forceinline__ uint32_t e4m3_encode(float x, float scale) {
-  float y = x / scale;
-  if (y != y) return 0x7Fu | (__float_as_uint(y) >> 31 << 7);
-  y = fminf(fmaxf(y, -448.0f), 448.0f);
-  const uint32_t sign = __float_as_uint(y) >> 31 << 7;
-  const float a = fabsf(y);
-  uint32_t code;
-  if (a < 0.015625f) {  // below the smallest normal 2^-6: subnormal steps of 2^-9
-    code = (uint32_t)rintf(a * 512.0f);  // 8 -> the smallest normal, code 0x08
-  } else {
-    int e;
-    const float m = frexpf(a, &e);  // a = m 2^e, m in [0.5, 1)
-    uint32_t mant = (uint32_t)rintf((m * 2.0f - 1.0f) * 8.0f);
-    int ex = e - 1;
-    if (mant == 8) {
-      mant = 0;
-      ++ex;
-    }
-    code = ((uint32_t)(ex + 7) << 3) | mant;
-  }
-  return sign | code;
-}
-
+// Quantising append into an fp8 cache: the rows arrive in bf16 or fp32 and each element is stored as its E4M3 code
+// (e4m3_encode) with the (agent, layer, head) scale the cache already has.
 struct QAppendArgs {
   const void* ks;
   const void* vs;

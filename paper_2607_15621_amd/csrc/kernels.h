@@ -217,6 +217,42 @@ hipError_t launch_append(const fsx_cache_desc& c, const void* k_rows, const void
 hipError_t launch_append_quantize(const fsx_cache_desc& c, const void* k_rows, const void* v_rows, int rows_dtype,
                                   int n_rows, const int64_t* dst_first_slot, hipStream_t s);
 
+// ------------------------------------------------------------------ whole prompts
+// Packed sequences of the prompt attention, longest keys first, by value in kernel arguments.
+struct PromptArgs {
+  const void* q;
+  const uint16_t* k;
+  const uint16_t* v;
+  void* out;
+  float* lse;           // [q_rows][H] or NULL
+  int64_t q_row, q_head, k_row, k_head, v_row, v_head, o_row, o_head;  // elements
+  int32_t H, G, D;      // query heads, query heads per key head, head width
+  int32_t q_f32, o_f32;
+  float c;              // scores in log2 units = c * q.k
+  int32_t n_seq;
+  int64_t q0[FSX_MAX_BATCH], k0[FSX_MAX_BATCH];
+  int32_t nq[FSX_MAX_BATCH], nk[FSX_MAX_BATCH];
+  int32_t row_prefix[FSX_MAX_BATCH + 1];  // query rows of the sequences before
+};
+hipError_t launch_prompt_attention(const PromptArgs& a, hipStream_t s);
+
+// ------------------------------------------------------------------ cache rows replaced and read
+// Rows of one agent: packed rows src .. src + n - 1 of every layer <-> ring slots (slot + i) mod cap.
+struct RowsArgs {
+  CacheView cv;          // layer: the first one; scales of a cache that is replaced are written
+  void* k;               // packed rows [layers][total][H][Dh], or NULL
+  void* v;
+  int32_t rows_f32;      // packed rows are fp32, else bf16
+  int32_t layers, B;
+  int64_t total;
+  float headroom;
+  int64_t src[FSX_MAX_BATCH], slot[FSX_MAX_BATCH];
+  int32_t n[FSX_MAX_BATCH];
+  int64_t prefix[FSX_MAX_BATCH + 1];  // rows of the agents before
+};
+hipError_t launch_replace_rows(const RowsArgs& a, hipStream_t s);
+hipError_t launch_read_rows(const RowsArgs& a, hipStream_t s);
+
 // ------------------------------------------------------------------ simple per-op path (any dtype)
 struct GenericWeights {
   const void* wq; const void* wk; const void* wv; const void* wo;

@@ -30,7 +30,8 @@ SYMBOLS = ("fsx_expert_create", "fsx_expert_forward", "fsx_cache_append_rows", "
            "fsx_probe_hbm_read", "fsx_expert_forward_noalloc", "fsx_cache_append_rows_quantize",
            "fsx_loop_create", "fsx_loop_tick", "fsx_loop_append", "fsx_loop_sync", "fsx_loop_destroy",
            "fsx_loop_last_error", "fsx_backbone_create", "fsx_backbone_append", "fsx_backbone_info",
-           "fsx_backbone_destroy")
+           "fsx_backbone_destroy", "fsx_prompt_attention", "fsx_prompt_attention_workspace", "fsx_cache_replace_rows",
+           "fsx_cache_read_rows")
 
 
 class FsxError(RuntimeError):
@@ -68,6 +69,13 @@ class LoopTickInfo(ctypes.Structure):
     _fields_ = [("tick", ctypes.c_int64), ("published", ctypes.c_int32), ("staleness", ctypes.c_int32),
                 ("start", ctypes.c_int64 * MAX_BATCH), ("len", ctypes.c_int64 * MAX_BATCH),
                 ("pos", ctypes.c_int64 * MAX_BATCH)]
+
+
+class PromptDesc(ctypes.Structure):
+    _fields_ = [("n_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("q_dtype", ctypes.c_int32), ("out_dtype", ctypes.c_int32), ("scale", ctypes.c_float)] + \
+               [(n, ctypes.c_int64) for n in ("q_rows", "k_rows", "q_row", "q_head", "k_row", "k_head", "v_row", "v_head",
+                                              "out_row", "out_head")]
 
 
 class CacheDescC(ctypes.Structure):
@@ -123,6 +131,16 @@ def lib() -> ctypes.CDLL:
         L.fsx_backbone_destroy.argtypes = [vp]
         L.fsx_backbone_destroy.restype = None
         for n in ("fsx_backbone_create", "fsx_backbone_append", "fsx_backbone_info"):
+            getattr(L, n).restype = ctypes.c_int
+        P64 = ctypes.POINTER(i64)
+        L.fsx_prompt_attention.argtypes = [ctypes.POINTER(PromptDesc), vp, vp, vp, vp, vp, i32, P64, P64, P64, P64, vp, i64,
+                                           vp]
+        L.fsx_prompt_attention_workspace.argtypes = [ctypes.POINTER(PromptDesc), i32, P64, P64, P64]
+        L.fsx_cache_replace_rows.argtypes = [ctypes.POINTER(CacheDescC), i32, i32, vp, vp, i32, i64, P64, P64,
+                                             ctypes.c_float, i32, vp]
+        L.fsx_cache_read_rows.argtypes = [ctypes.POINTER(CacheDescC), i32, i32, P64, vp, vp, i32, i64, P64, P64, vp]
+        for n in ("fsx_prompt_attention", "fsx_prompt_attention_workspace", "fsx_cache_replace_rows",
+                  "fsx_cache_read_rows"):
             getattr(L, n).restype = ctypes.c_int
         for n in ("fsx_expert_create", "fsx_expert_forward", "fsx_cache_append_rows", "fsx_expert_info",
                   "fsx_expert_status", "fsx_expert_trace", "fsx_probe_hbm_read"):
@@ -281,6 +299,101 @@ def cache_append_rows_quantize(cache: CacheDesc, k_rows, v_rows, rows_dtype: int
     """fsx_cache_append_rows_quantize: bf16 / fp32 rows encoded into an fp8 cache with its scales."""
     _check(lib().fsx_cache_append_rows_quantize(ctypes.byref(cache.c), _ptr(k_rows), _ptr(v_rows), rows_dtype,
                                                 n_rows, policy, _stream(stream)))
+
+
+class PackedRows:
+    """Rows of several sequences (or agents) in one tensor: sequence i in rows start[i] .. start[i] + len[i] - 1; without
+    starts, one after the other."""
+
+    def __init__(self, lengths, starts=None):
+        self.len = np.array(lengths, dtype=np.int64).reshape(-1)
+        self.start = (np.cumsum(self.len) - self.len if starts is None else
+                      np.array(starts, dtype=np.int64).reshape(-1))
+        if len(self.start) != len(self.len):
+            raise ValueError("as many starts as lengths")
+        P = ctypes.POINTER(ctypes.c_int64)
+        self.n, self.c_start, self.c_len = len(self.len), self.start.ctypes.data_as(P), self.len.ctypes.data_as(P)
+
+
+def _dtype_of(t) -> int:
+    code = {"torch.float32": F32, "torch.bfloat16": BF16}.get(str(t.dtype))
+    if code is None:
+        raise ValueError(f"tensors of dtype {t.dtype} are not taken here: float32 or bfloat16")
+    return code
+
+
+def _prompt_desc(q, k, v, out, scale: float) -> PromptDesc:
+    """Tensors [rows][heads][head_dim], their last dimension dense."""
+    for t in (q, k, v, out):
+        if t.dim() != 3 or (t.stride(2) != 1 and t.numel()):
+            raise ValueError("q, k, v and out must be [rows][heads][head_dim] with a dense last dimension")
+    if k.shape != v.shape or q.shape != out.shape or q.shape[2] != k.shape[2]:
+        raise ValueError("k and v, q and out must have the same shapes, and all one head_dim")
+    if _dtype_of(k) != BF16 or _dtype_of(v) != BF16:
+        raise ValueError("k and v must be bfloat16")
+    return PromptDesc(q.shape[1], k.shape[1], q.shape[2], _dtype_of(q), _dtype_of(out), scale, q.shape[0], k.shape[0],
+                      *q.stride()[:2], *k.stride()[:2], *v.stride()[:2], *out.stride()[:2])
+
+
+def prompt_attention(q, k, v, out, q_rows: PackedRows, k_rows: Optional[PackedRows] = None, scale: float = 0.0, lse=None,
+                     workspace=None, stream=None):
+    """fsx_prompt_attention: causal attention of packed sequences.  q, out [rows][n_heads][head_dim], k, v
+    [rows][n_kv_heads][head_dim] (any row and head strides); lse [rows][n_heads] float32, dense, or None; workspace a
+    device tensor of prompt_attention_workspace bytes, or None (keys are then not split over workgroups)."""
+    if lse is not None and (_dtype_of(lse) != F32 or tuple(lse.shape) != tuple(q.shape[:2]) or not lse.is_contiguous()):
+        raise ValueError("lse must be a dense float32 [rows][n_heads]")
+    if k_rows is not None and k_rows.n != q_rows.n:
+        raise ValueError("as many sequences of keys as of queries")
+    d = _prompt_desc(q, k, v, out, scale)
+    _check(lib().fsx_prompt_attention(ctypes.byref(d), _ptr(q), _ptr(k), _ptr(v), _ptr(out), _ptr(lse), q_rows.n,
+                                      q_rows.c_start, q_rows.c_len, k_rows.c_start if k_rows is not None else None,
+                                      k_rows.c_len if k_rows is not None else None, _ptr(workspace),
+                                      workspace.numel() * workspace.element_size() if workspace is not None else 0,
+                                      _stream(stream)))
+
+
+def prompt_attention_workspace(q, k, q_rows: PackedRows, k_rows: Optional[PackedRows] = None) -> int:
+    """fsx_prompt_attention_workspace: bytes of the workspace that the call can use (0: none)."""
+    if k_rows is not None and k_rows.n != q_rows.n:
+        raise ValueError("as many sequences of keys as of queries")
+    d, need = _prompt_desc(q, k, k, q, 0.0), ctypes.c_int64()
+    _check(lib().fsx_prompt_attention_workspace(ctypes.byref(d), q_rows.n, q_rows.c_len,
+                                                k_rows.c_len if k_rows is not None else None, ctypes.byref(need)))
+    return need.value
+
+
+def _row_tensors(cache: CacheDesc, n_layers: int, k_rows, v_rows, rows: PackedRows):
+    """Dtype and total rows of packed rows [n_layers][total_rows][H][Dh] (either tensor may be None)."""
+    if rows.n != cache.c.batch:
+        raise ValueError("rows of every agent of the cache")
+    given = [t for t in (k_rows, v_rows) if t is not None]
+    for t in given:
+        if t.dim() != 4 or not t.is_contiguous() or t.shape != given[0].shape or t.dtype != given[0].dtype or \
+                tuple(t.shape[2:]) != (cache.c.n_heads, cache.c.head_dim) or t.shape[0] != n_layers:
+            raise ValueError("packed rows must be dense [n_layers][rows][n_heads][head_dim] tensors of one dtype")
+    return (_dtype_of(given[0]), given[0].shape[1]) if given else (BF16, int((rows.start + rows.len).max(initial=0)))
+
+
+def cache_replace_rows(cache: CacheDesc, layer: int, n_layers: int, k_rows, v_rows, rows: PackedRows, headroom: float = 1.0,
+                       policy: int = APPEND_RING, stream=None):
+    """fsx_cache_replace_rows: the rows of every agent with rows.len > 0, in layers layer .. layer + n_layers - 1, become
+    packed rows [n_layers][total][H][Dh]; an fp8 cache's scales are found from them."""
+    dtype, total = _row_tensors(cache, n_layers, k_rows, v_rows, rows)
+    _check(lib().fsx_cache_replace_rows(ctypes.byref(cache.c), layer, n_layers, _ptr(k_rows), _ptr(v_rows), dtype, total,
+                                        rows.c_start, rows.c_len, headroom, policy, _stream(stream)))
+
+
+def cache_read_rows(cache: CacheDesc, layer: int, n_layers: int, k_rows, v_rows, rows: PackedRows, first=None, stream=None):
+    """fsx_cache_read_rows: cached rows first[b] .. first[b] + rows.len[b] - 1 (0: the oldest valid row) into packed rows
+    [n_layers][total][H][Dh], decoded; k_rows or v_rows may be None."""
+    dtype, total = _row_tensors(cache, n_layers, k_rows, v_rows, rows)
+    if first is not None:
+        first = np.array(first, dtype=np.int64).reshape(-1)
+        if len(first) != rows.n:
+            raise ValueError("a first row of every agent of the cache")
+    _check(lib().fsx_cache_read_rows(ctypes.byref(cache.c), layer, n_layers,
+                                     first.ctypes.data_as(ctypes.POINTER(ctypes.c_int64)) if first is not None else None,
+                                     _ptr(k_rows), _ptr(v_rows), dtype, total, rows.c_start, rows.c_len, _stream(stream)))
 
 
 class Loop:

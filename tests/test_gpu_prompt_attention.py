@@ -1,0 +1,278 @@
+"""Causal attention of packed prompts (fsx_prompt_attention) against the formula in 64 bits.
+
+Tolerances, per element of the output: with A = sum_j P_j |v_j| and half a bf16 step u = 2^-8, the probabilities' rounding moves
+an output by at most u A and the output's own rounding by u |O| (0 for an fp32 output).  A score is a sum of D products in fp32,
+scaled once: it is off by at most ds = (D + 4) 2^-24 scale sum_c |q_c k_c|, which changes every weight by a factor within
+exp(+-2 ds), and the statistics add (keys + 16) roundings of 2^-24.  The log sum moves by ds and the same roundings.
+"""
+
+from __future__ import annotations
+
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2607_15621_amd import fsx
+
+pytestmark = pytest.mark.gpu
+
+BF16, F32, F64 = torch.bfloat16, torch.float32, torch.float64
+U = torch.finfo(BF16).eps / 2
+
+
+def reference(q, k, v, scale):
+    """Output, tolerance without the output's rounding, log sums and their tolerance of one sequence, on the CPU in 64 bits:
+    [rows][heads][channels] and [rows][heads].  Masked keys take no part."""
+    n, H, D = q.shape
+    m, G = k.shape[0], H // k.shape[1]
+    q = q.to(BF16).to(F64)
+    out, tol = torch.zeros(n, H, D, dtype=F64), torch.zeros(n, H, D, dtype=F64)
+    lse, ltol = torch.full((n, H), -math.inf, dtype=F64), torch.zeros(n, H, dtype=F64)
+    for h in range(H):
+        kh, vh = k[:, h // G].to(F64), v[:, h // G].to(F64)
+        x, mag = scale * (q[:, h] @ kh.t()), scale * (q[:, h].abs() @ kh.abs().t())
+        for t in range(n):
+            seen = m - n + t + 1
+            if seen <= 0:
+                continue
+            s, big = x[t, :seen], mag[t, :seen].max()
+            z = torch.logsumexp(s, 0)
+            p = torch.exp(s - z)
+            ds = (D + 4) * 2.0 ** -24 * big + (seen + 16) * 2.0 ** -24
+            a = p @ vh[:seen].abs()
+            out[t, h], tol[t, h] = p @ vh[:seen], a * (U + 4 * ds) + 1e-30
+            lse[t, h], ltol[t, h] = z, 2 * ds + 2.0 ** -22 * z.abs() + 1e-7
+    return out, tol, lse, ltol
+
+
+def check(got, want, tol, what):
+    got = got.detach().cpu().to(F64)
+    assert got.shape == want.shape
+    assert torch.equal(got.isnan(), want.isnan()), what
+    ok = want.isnan() | (got == want) | ((got - want).abs() <= tol)
+    worst = ((got - want).abs() / tol)[~ok]
+    assert bool(ok.all()), (what, int((~ok).sum()), float(worst.max()))
+
+
+class Case:
+    def __init__(self, q_len, k_len=None, heads=4, kv_heads=4, dim=128, q_dtype=BF16, out_dtype=BF16, layout="packed", seed=0,
+                 amp=1.0, gap=0, scale=0.0):
+        g = torch.Generator().manual_seed(seed)
+        self.q_len, self.k_len = list(q_len), list(q_len if k_len is None else k_len)
+        self.H, self.Hk, self.D, self.scale = heads, kv_heads, dim, scale
+        # the sequences lie in reverse order, `gap` rows apart
+        self.q_rows, self.k_rows = (fsx.PackedRows(n, self._starts(n, gap)) for n in (self.q_len, self.k_len))
+        nq, nk = (int((r.start + r.len).max(initial=0)) + gap for r in (self.q_rows, self.k_rows))
+        # (what the host holds is exact in the types that the device gets)
+        self.hq = (torch.randn(nq, heads, dim, generator=g) * amp).to(q_dtype)
+        self.hk = (torch.randn(nk, kv_heads, dim, generator=g) * amp).to(BF16)
+        self.hv = torch.randn(nk, kv_heads, dim, generator=g).to(BF16)
+        self.layout, self.out_dtype = layout, out_dtype
+
+    @staticmethod
+    def _starts(lens, gap):
+        starts, at = [], gap
+        for n in reversed(lens):
+            starts.append(at)
+            at += n + gap
+        return starts[::-1]
+
+    def place(self, t, dtype=None):
+        """The tensor on the device in the layout under test, as [rows][heads][channels]."""
+        t = t.cuda()
+        if self.layout == "packed":
+            return t.contiguous()
+        if self.layout == "head_major":
+            return t.transpose(0, 1).contiguous().transpose(0, 1)
+        wide = torch.full((t.shape[0], t.shape[1] + 3, t.shape[2] + 24), float("nan"), dtype=t.dtype, device="cuda")
+        wide[:, 1:1 + t.shape[1], 8:8 + t.shape[2]] = t  # rows of a wider projection, other columns between the heads
+        return wide[:, 1:1 + t.shape[1], 8:8 + t.shape[2]]
+
+    def run(self, workspace=True, stream=None):
+        q, k, v = self.place(self.hq), self.place(self.hk), self.place(self.hv)
+        out = self.place(torch.full(tuple(self.hq.shape), 7.0, dtype=self.out_dtype))
+        lse = torch.full(tuple(self.hq.shape[:2]), 7.0, device="cuda")
+        need = fsx.prompt_attention_workspace(q, k, self.q_rows, self.k_rows)
+        ws = torch.full((need,), 255, dtype=torch.uint8, device="cuda") if workspace and need else None
+        torch.cuda.synchronize()
+        fsx.prompt_attention(q, k, v, out, self.q_rows, self.k_rows, self.scale, lse, ws, stream)
+        torch.cuda.synchronize()
+        return out, lse
+
+    def check(self, out, lse):
+        touched = torch.zeros(self.hq.shape[0], dtype=torch.bool)
+        for i in range(len(self.q_len)):
+            a, n, b, m = self.q_rows.start[i], self.q_len[i], self.k_rows.start[i], self.k_len[i]
+            touched[a:a + n] = True
+            o, tol, z, ztol = reference(self.hq[a:a + n], self.hk[b:b + m], self.hv[b:b + m],
+                                        self.scale or 1 / math.sqrt(self.D))
+            if self.out_dtype is BF16:
+                tol = tol + U * (o.abs() + tol)
+            check(out[a:a + n], o, tol, f"sequence {i}: output")
+            check(lse[a:a + n], z, ztol, f"sequence {i}: log sums")
+        rest = out.cpu()[~touched]
+        assert bool((rest == 7.0).all()) and bool((lse.cpu()[~touched] == 7.0).all()), "rows outside the sequences"
+
+
+LENGTHS = [(1,), (2,), (17,), (31, 33), (64,), (65, 1, 63), (127, 128, 129), (200, 5), (257,), (1, 1, 1, 300, 0, 12)]
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("lens", LENGTHS, ids=str)
+def test_whole_prompts(lens, dim):
+    c = Case(lens, dim=dim, seed=len(lens) + lens[0])
+    c.check(*c.run())
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("q_len,k_len", [((1,), (1,)), ((1, 1, 1), (700, 3, 1025)), ((4, 64), (2100, 65)), ((33, 1), (34, 900)),
+                                         ((5, 3, 80), (2, 0, 40)), ((130, 7), (1300, 7)), ((16,) * 20, tuple(range(20, 420, 20)))],
+                         ids=str)
+def test_new_rows_over_a_history(q_len, k_len, dim):
+    """Fewer queries than keys, and more (rows before the first key see nothing), with and without a workspace."""
+    c = Case(q_len, k_len, heads=4, kv_heads=2, dim=dim, seed=sum(k_len))
+    c.check(*c.run())
+    c.check(*c.run(workspace=False))
+
+
+@pytest.mark.parametrize("heads,kv_heads", [(1, 1), (8, 1), (6, 2), (5, 5), (32, 8), (40, 2)])
+def test_grouped_heads(heads, kv_heads):
+    c = Case((70, 9), (70, 400), heads=heads, kv_heads=kv_heads, seed=heads)
+    c.check(*c.run())
+    c = Case((1, 1), (333, 64), heads=heads, kv_heads=kv_heads, seed=heads)
+    c.check(*c.run())
+
+
+@pytest.mark.parametrize("layout", ["packed", "head_major", "wide"])
+@pytest.mark.parametrize("q_dtype,out_dtype", [(BF16, BF16), (F32, BF16), (BF16, F32), (F32, F32)], ids=str)
+def test_layouts_and_types(layout, q_dtype, out_dtype):
+    c = Case((90, 33, 2), (90, 200, 1000), heads=4, kv_heads=2, q_dtype=q_dtype, out_dtype=out_dtype, layout=layout, gap=3, seed=5)
+    c.check(*c.run())
+
+
+@pytest.mark.parametrize("amp,scale", [(0.0, 0.0), (30.0, 0.0), (1.0, 2.5), (100.0, 1.0), (1e-20, 0.0)])
+def test_flat_and_peaked_softmax(amp, scale):
+    c = Case((150, 1), (150, 600), heads=2, kv_heads=2, amp=amp, scale=scale, seed=9)
+    c.check(*c.run())
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_masked_places_may_hold_anything(bad, dim):
+    """Rows between and behind the sequences, and keys and values after a token's own place."""
+    c = Case((100, 40, 1), (100, 170, 500), heads=4, kv_heads=2, dim=dim, gap=70, seed=21)
+    inside = torch.zeros(c.hk.shape[0], dtype=torch.bool)
+    for i in range(3):
+        inside[c.k_rows.start[i]:c.k_rows.start[i] + c.k_len[i]] = True
+    c.hk[~inside] = bad
+    c.hv[~inside] = bad
+    for i, t in ((0, 97), (0, 33), (1, 169), (1, 150)):
+        c.hv[c.k_rows.start[i] + t, t % 2, 5] = bad  # a value that later rows see, and those before them do not
+    out, lse = c.run()
+    for i in range(3):
+        a, n, b, m = c.q_rows.start[i], c.q_len[i], c.k_rows.start[i], c.k_len[i]
+        v = c.hv[b:b + m].clone()
+        hit = ~torch.isfinite(v.float())
+        v[hit] = 0
+        o, tol, z, ztol = reference(c.hq[a:a + n], c.hk[b:b + m], v, 1 / math.sqrt(dim))
+        for t, h, ch in hit.nonzero().tolist():
+            o[max(0, t - (m - n)):, 2 * h:2 * h + 2, ch] += bad  # the weight is positive
+        check(out[a:a + n], o, tol + U * (o.nan_to_num(0, 0, 0).abs() + tol), f"sequence {i}: output")
+        check(lse[a:a + n], z, ztol, f"sequence {i}: log sums")
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_masked_keys_that_are_not_finite(bad):
+    """A key that is not finite spoils the rows that see it (here: to NaN, whose scores then have no maximum) and no other."""
+    c = Case((120,), heads=2, kv_heads=2, seed=22)
+    c.hk[100:, 1] = bad
+    out, lse = c.run()
+    o, tol, z, ztol = reference(c.hq[:100], c.hk[:100], c.hv[:100], 1 / math.sqrt(128))
+    check(out[:100], o, tol + U * (o.abs() + tol), "rows before")
+    check(lse[:100], z, ztol, "rows before")
+    if math.isnan(bad):
+        assert bool(out[100:, 1].isnan().all())
+
+
+def test_the_same_bits_every_time_and_on_another_stream():
+    c = Case((130, 1, 64), (1300, 2000, 64), heads=8, kv_heads=2, seed=4)
+    out, lse = c.run()
+    for stream in (None, torch.cuda.Stream()):
+        again, lse2 = c.run(stream=stream)
+        assert torch.equal(out.view(torch.int16), again.view(torch.int16)) and torch.equal(lse, lse2)
+
+
+def test_captured_calls_are_replayed():
+    """Two graphs with a workspace each, replayed in turn with other inputs between, against eager calls."""
+    runs = []
+    for seed in (1, 2):
+        c = Case((60, 1, 1), (60, 900, 2000), heads=8, kv_heads=2, seed=seed)
+        q, k, v = c.place(c.hq), c.place(c.hk), c.place(c.hv)
+        out, need = torch.empty_like(q), fsx.prompt_attention_workspace(q, k, c.q_rows, c.k_rows)
+        ws = torch.empty(max(16, need), dtype=torch.uint8, device="cuda")
+        s = torch.cuda.Stream()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(s):
+            fsx.prompt_attention(q, k, v, out, c.q_rows, c.k_rows, workspace=ws)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=s):
+            fsx.prompt_attention(q, k, v, out, c.q_rows, c.k_rows, workspace=ws)
+        runs.append((c, q, k, v, out, ws, graph))
+    for turn in range(3):
+        for c, q, k, v, out, ws, graph in runs:
+            q.copy_(torch.randn(q.shape, generator=torch.Generator().manual_seed(50 + turn)).to(BF16))
+            out.zero_()
+            torch.cuda.synchronize()
+            graph.replay()
+            torch.cuda.synchronize()
+            got, want = out.clone(), torch.empty_like(out)
+            fsx.prompt_attention(q, k, v, want, c.q_rows, c.k_rows, workspace=torch.empty_like(ws))
+            torch.cuda.synchronize()
+            assert torch.equal(got.view(torch.int16), want.view(torch.int16)), turn
+
+
+def test_offsets_beyond_32_bits():
+    """Keys and values of the last of many rings: more than 2^32 elements before them."""
+    c = Case((3, 1), (70, 500), heads=2, kv_heads=1, seed=8)
+    far = (1 << 25) + 11  # rows of 128 channels: 2^32 elements
+    big = torch.empty(far + 600, 1, 128, dtype=BF16, device="cuda")
+    big[far:far + c.hk.shape[0]] = c.hk.cuda()
+    bigv = torch.empty(far + 600, 1, 128, dtype=BF16, device="cuda")
+    bigv[far:far + c.hv.shape[0]] = c.hv.cuda()
+    q, out = c.hq.cuda(), torch.full(tuple(c.hq.shape), 7.0, dtype=BF16, device="cuda")
+    lse = torch.full(tuple(c.hq.shape[:2]), 7.0, device="cuda")
+    rows = fsx.PackedRows(c.k_len, c.k_rows.start + far)
+    fsx.prompt_attention(q, big, bigv, out, c.q_rows, rows, lse=lse)
+    torch.cuda.synchronize()
+    c.check(out, lse)
+
+
+@pytest.mark.parametrize("layout", [fsx.CACHE_HEAD_MAJOR, fsx.CACHE_TOKEN_MAJOR])
+def test_keys_where_they_stand_in_a_cache(layout):
+    """One layer of a bf16 cache whose rings have not wrapped, read in place: rows and heads are strides of the cache."""
+    B, L, H, cap, D, layer = 3, 2, 4, 150, 128, 1
+    c = Case((1, 9, 70), (100, 37, 150), heads=8, kv_heads=H, seed=3)
+    shape = (B, L, cap, H, D) if layout == fsx.CACHE_TOKEN_MAJOR else (B, L, H, cap, D)
+    k, v = (torch.full(shape, float("nan"), dtype=BF16, device="cuda") for _ in "kv")
+    for b in range(B):
+        for t, h in ((k, c.hk), (v, c.hv)):
+            rows = h[c.k_rows.start[b]:c.k_rows.start[b] + c.k_len[b]].cuda()
+            if layout == fsx.CACHE_TOKEN_MAJOR:
+                t[b, layer, :c.k_len[b]] = rows
+            else:
+                t[b, layer, :, :c.k_len[b]] = rows.transpose(0, 1)
+    if layout == fsx.CACHE_TOKEN_MAJOR:
+        view = [t.view(B * L * cap, H, D) for t in (k, v)]
+        starts = [(b * L + layer) * cap for b in range(B)]
+    else:  # rows of one head; the heads lie cap rows apart
+        n = B * L * H * cap - (H - 1) * cap
+        view = [t.view(-1).as_strided((n, H, D), (D, cap * D, 1)) for t in (k, v)]
+        starts = [(b * L + layer) * H * cap for b in range(B)]
+    out = torch.full(tuple(c.hq.shape), 7.0, dtype=BF16, device="cuda")
+    lse = torch.full(tuple(c.hq.shape[:2]), 7.0, device="cuda")
+    fsx.prompt_attention(c.hq.cuda(), *view, out, c.q_rows, fsx.PackedRows(c.k_len, starts), lse=lse)
+    torch.cuda.synchronize()
+    c.check(out, lse)
