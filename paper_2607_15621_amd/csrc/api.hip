@@ -938,6 +938,22 @@ static int check_out_strides(const fsx_prompt_desc& d) {
   return FSX_OK;
 }
 
+// The sequences that have queries, those with the most keys first.
+static void prompt_sequences(PromptArgs& a, int n_seq, const int64_t* q_start, const int64_t* q_len, const int64_t* k_start,
+                             const int64_t* k_len) {
+  std::array<int, FSX_MAX_BATCH> ord;
+  for (int i = 0; i < n_seq; ++i)
+    if (q_len[i] > 0) ord[a.n_seq++] = i;
+  std::stable_sort(ord.begin(), ord.begin() + a.n_seq, [&](int x, int y) { return k_len[x] > k_len[y]; });
+  for (int j = 0; j < a.n_seq; ++j) {
+    const int i = ord[j];
+    a.q0[j] = q_start ? q_start[i] : 0;
+    a.k0[j] = k_start ? k_start[i] : 0;
+    a.nq[j] = (int32_t)q_len[i];
+    a.nk[j] = (int32_t)k_len[i];
+  }
+}
+
 extern "C" int fsx_prompt_attention_workspace(const fsx_prompt_desc* desc, int32_t n_seq, const int64_t* q_len,
                                               const int64_t* k_len, int64_t* bytes) {
   if (!bytes) return fail(FSX_E_INVALID, "bytes is NULL");
@@ -950,6 +966,10 @@ extern "C" int fsx_prompt_attention_workspace(const fsx_prompt_desc* desc, int32
   for (int i = 0; i < n_seq; ++i)
     if (q_len[i] < 0 || q_len[i] > MAX_PROMPT || k_len[i] < 0 || k_len[i] > MAX_PROMPT)
       return fail(FSX_E_INVALID, "length " + std::to_string(i) + " outside 0..2^24");
+  PromptArgs a{};
+  a.H = desc->n_heads; a.G = desc->n_heads / desc->n_kv_heads; a.D = desc->head_dim;
+  prompt_sequences(a, n_seq, nullptr, q_len, nullptr, k_len);
+  if (a.n_seq > 0) plan_prompt(a, INT64_MAX, bytes);
   g_err.clear();
   return FSX_OK;
 }
@@ -987,20 +1007,15 @@ extern "C" int fsx_prompt_attention(const fsx_prompt_desc* desc, const void* q, 
   if (!q || !out || (keys > 0 && (!k || !v))) return fail(FSX_E_INVALID, "q, k, v and out must be non-NULL");
   if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out))
     return fail(FSX_E_INVALID, "q, k, v and out must be 16-byte aligned");
-  if (rows * d.n_heads > (int64_t)INT32_MAX) return fail(FSX_E_UNSUPPORTED, "rows * n_heads beyond 2^31");
+  if (rows * d.n_heads > (int64_t)1 << 30) return fail(FSX_E_UNSUPPORTED, "query rows * n_heads beyond 2^30");
   a.q = q; a.k = (const uint16_t*)k; a.v = (const uint16_t*)v; a.out = out; a.lse = lse;
   a.q_row = d.q_row; a.q_head = d.q_head; a.k_row = d.k_row; a.k_head = d.k_head;
   a.v_row = d.v_row; a.v_head = d.v_head; a.o_row = d.out_row; a.o_head = d.out_head;
   a.H = d.n_heads; a.G = d.n_heads / d.n_kv_heads; a.D = d.head_dim;
   a.q_f32 = d.q_dtype == FSX_F32; a.o_f32 = d.out_dtype == FSX_F32;
   a.c = (d.scale > 0.f ? d.scale : 1.0f / sqrtf((float)d.head_dim)) * LOG2E;
-  for (int i = 0; i < n_seq; ++i) {
-    if (q_len[i] == 0) continue;
-    const int j = a.n_seq++;
-    a.q0[j] = q_start[i]; a.k0[j] = k_start[i]; a.nq[j] = (int32_t)q_len[i]; a.nk[j] = (int32_t)k_len[i];
-    a.row_prefix[j + 1] = a.row_prefix[j] + (int32_t)q_len[i];
-  }
-  HIP_TRY(launch_prompt_attention(a, (hipStream_t)stream));
+  prompt_sequences(a, n_seq, q_start, q_len, k_start, k_len);
+  HIP_TRY(launch_prompt_attention(a, workspace, workspace_bytes, (hipStream_t)stream));
   g_err.clear();
   return FSX_OK;
 }

@@ -232,9 +232,15 @@ struct PromptArgs {
   int32_t n_seq;
   int64_t q0[FSX_MAX_BATCH], k0[FSX_MAX_BATCH];
   int32_t nq[FSX_MAX_BATCH], nk[FSX_MAX_BATCH];
-  int32_t row_prefix[FSX_MAX_BATCH + 1];  // query rows of the sequences before
+  int32_t item_prefix[FSX_MAX_BATCH + 1];  // workgroups of the sequences before
+  // keys in chunks (few rows)
+  float* part;           // states of the workgroups
+  int32_t chunk;         // tiles of a chunk
+  int32_t n_split[FSX_MAX_BATCH], merge_prefix[FSX_MAX_BATCH + 1];
 };
-hipError_t launch_prompt_attention(const PromptArgs& a, hipStream_t s);
+// Whether the keys are walked in chunks, and how; the bytes of workspace that the plan uses, at most workspace_bytes.
+bool plan_prompt(PromptArgs& a, int64_t workspace_bytes, int64_t* need);
+hipError_t launch_prompt_attention(PromptArgs a, void* workspace, int64_t workspace_bytes, hipStream_t s);
 
 // ------------------------------------------------------------------ cache rows replaced and read
 // Rows of one agent: packed rows src .. src + n - 1 of every layer <-> ring slots (slot + i) mod cap.

@@ -4,69 +4,545 @@
 // Query t of a sequence with nq new tokens over nk keys sees the keys j <= nk - nq + t; per head
 //   O_t = sum_j exp(s_tj) v_j / sum_j exp(s_tj),   s_tj = scale q_t . k_j,   lse_t = log sum_j exp(s_tj).
 
+#include <algorithm>
+
 #include "common.h"
 #include "kernels.h"
 
 namespace fsx {
 
-// One wave per (query row, head): 64 keys at a time, one per lane, with the running maximum and sum of the softmax; then a
-// lane owns D / 64 output channels.  Masked keys are never read.
-template <int D>
-__global__ __launch_bounds__(256) void k_prompt_rows(PromptArgs a) {
-  __shared__ float sq[4][D];
-  __shared__ float sp[4][64];
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const int64_t item = (int64_t)blockIdx.x * 4 + w;
-  if (item >= (int64_t)a.row_prefix[a.n_seq] * a.H) return;
-  const int r = (int)(item / a.H), h = (int)(item % a.H);
-  int s = 0;
-  while (r >= a.row_prefix[s + 1]) ++s;
-  const int t = r - a.row_prefix[s], seen = a.nk[s] - a.nq[s] + t + 1;
-  const int64_t row = a.q0[s] + t;
-  for (int c = lane; c < D; c += 64) {
-    const int64_t i = row * a.q_row + h * a.q_head + c;
-    sq[w][c] = a.q_f32 ? bf16_to_f32(f32_to_bf16(((const float*)a.q)[i])) : bf16_to_f32(((const uint16_t*)a.q)[i]);
-  }
-  const uint16_t* k = a.k + a.k0[s] * a.k_row + (h / a.G) * a.k_head;
-  const uint16_t* v = a.v + a.k0[s] * a.v_row + (h / a.G) * a.v_head;
-  float m = -INFINITY, l = 0.f, o[D / 64] = {};
-  for (int j0 = 0; j0 < seen; j0 += 64) {
-    const int n = min(64, seen - j0);
-    float x = -INFINITY;
-    if (lane < n) {
-      const uint16_t* kr = k + (int64_t)(j0 + lane) * a.k_row;
-      float dot = 0.f;
-      for (int c = 0; c < D; ++c) dot += sq[w][c] * bf16_to_f32(kr[c]);
-      x = dot * a.c;
-    }
-    float mx = x;
-    for (int i = 1; i < 64; i <<= 1) mx = fmaxf(mx, __shfl_xor(mx, i));
-    const float mn = fmaxf(m, mx), mz = mn == -INFINITY ? 0.f : mn;
-    const float p = lane < n ? exp2f(x - mz) : 0.f, alpha = exp2f(m - mz);
-    l = l * alpha + wave_sum(p);
-    m = mn;
-    sp[w][lane] = p;
-    for (int e = 0; e < D / 64; ++e) o[e] *= alpha;
-    for (int j = 0; j < n; ++j)
-      for (int e = 0; e < D / 64; ++e) o[e] += sp[w][j] * bf16_to_f32(v[(int64_t)(j0 + j) * a.v_row + lane + 64 * e]);
-  }
-  for (int e = 0; e < D / 64; ++e) {
-    const float y = seen > 0 ? o[e] / l : 0.f;
-    const int64_t i = row * a.o_row + h * a.o_head + lane + 64 * e;
-    if (a.o_f32) ((float*)a.out)[i] = y;
-    else ((uint16_t*)a.out)[i] = f32_to_bf16(y);
-  }
-  if (a.lse && lane == 0) a.lse[row * a.H + h] = seen > 0 ? (m + log2f(l)) / LOG2E : -INFINITY;
+
+// The rows of a (sequence, key head) are its tokens' query heads of that key head, token by token: row r is token r / G, head
+// r % G of the group, so all query heads that share keys read them from one tile.
+//
+// A workgroup takes NW * 32 rows, a wave 32 of them, and walks over the keys in tiles of 64 that direct loads bring into LDS
+// one tile ahead.  Everything is held transposed, a query per lane column:
+//   S^T = K Q^T   32x32x16 MFMA, A = 32 keys x 16 channels from LDS, B = the wave's queries, kept in registers;
+//   a lane then has 16 of 32 keys' scores of one query (lane l and l ^ 32 share query l % 32), so maximum and sum are lane
+//   operations and one exchange of halves;
+//   O^T += V^T P^T   the scores' registers, rounded to bf16, are the B operand as they stand (slots 0-3 of lane half g: keys
+//   4g .. 4g + 3, slots 4-7: 8 + 4g ..); A = V^T in the same order of keys by transposing LDS reads.
+constexpr int PT_KEYS = 64;
+
+typedef __attribute__((__vector_size__(16 * sizeof(float)))) float f32x16;
+typedef __attribute__((__vector_size__(4 * sizeof(short)))) short s16x4;
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+
+__device__ __forceinline__ f32x16 mfma32_bf16(uint4 a, uint4 b, f32x16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
-hipError_t launch_prompt_attention(const PromptArgs& a, hipStream_t s) {
-  const int64_t items = (int64_t)a.row_prefix[a.n_seq] * a.H;
-  if (items == 0) return hipSuccess;
-  const dim3 grid((unsigned)((items + 3) / 4));
+// Four values down a column: lane i of 16 gets column i of the 4 rows x 16 columns of 16 bits whose 8-byte pieces the lanes
+// point at (row i / 4, columns 4 (i % 4) ..).
+__device__ __forceinline__ uint2 lds_column4(const char* p) {
+  return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p)));
+}
+
+// Where 16-byte piece p of a tile's row lies: in row-piece p ^ k_turn (keys) or p ^ v_turn (values), so that the 16 rows (four
+// rows, two pieces each) that a read takes at once lie in different banks.  With the pieces in order the reads of 32 rows
+// took 16 times (values: twice) as long.
+template <int D>
+__device__ __forceinline__ int k_turn(int row) { return D == 128 ? row & 15 : (row >> 1) & 7; }
+template <int D>
+__device__ __forceinline__ int v_turn(int row) { return D == 128 ? 2 * (row & 7) : 2 * (row & 3); }
+
+// Sequence and place in it of item i, items of sequence s being prefix[s] .. prefix[s + 1] - 1.
+__device__ __forceinline__ int find_seq(const int32_t* prefix, int n_seq, int i, int lane) {
+  return __popcll(__ballot(lane < n_seq && prefix[min(lane + 1, FSX_MAX_BATCH)] <= i));
+}
+
+// max / sum with lane l ^ 32
+__device__ __forceinline__ float half_max(float v) {
+  const unsigned u = __builtin_bit_cast(unsigned, v);
+  const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  return vmax(__builtin_bit_cast(float, (unsigned)r[0]), __builtin_bit_cast(float, (unsigned)r[1]));
+}
+__device__ __forceinline__ float half_sum(float v) {
+  const unsigned u = __builtin_bit_cast(unsigned, v);
+  const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  return __builtin_bit_cast(float, (unsigned)r[0]) + __builtin_bit_cast(float, (unsigned)r[1]);
+}
+
+// 32 queries' running state: O^T block b, register i: channel 32 b + 8 (i / 4) + 4 (lane / 32) + i % 4 of query lane % 32;
+// m: maximum in log2 units, l: the lane's share of the sum.
+template <int D>
+struct PromptState {
+  f32x16 o[D / 32];
+  float m, l;
+};
+
+// The wave's queries as the B operand: step s, lane l: channels 16 s + 8 (l / 32) .. + 7 of query l % 32.
+template <int D>
+__device__ __forceinline__ void load_queries(const PromptArgs& a, int64_t at, bool valid, int half, uint4 (&qf)[D / 16]) {
+#pragma unroll
+  for (int s = 0; s < D / 16; ++s) {
+    qf[s] = make_uint4(0, 0, 0, 0);
+    if (!valid) continue;
+    if (a.q_f32) {
+      const float4* p = reinterpret_cast<const float4*>((const float*)a.q + at + 16 * s + 8 * half);
+      const float4 lo = p[0], hi = p[1];
+      qf[s] = make_uint4(pack_bf16x2(lo.x, lo.y), pack_bf16x2(lo.z, lo.w), pack_bf16x2(hi.x, hi.y), pack_bf16x2(hi.z, hi.w));
+    } else {
+      qf[s] = *reinterpret_cast<const uint4*>((const uint16_t*)a.q + at + 16 * s + 8 * half);
+    }
+  }
+}
+
+// Block b of the output row (query lane % 32), scaled by inv.
+__device__ __forceinline__ void store_block(const PromptArgs& a, const f32x16& o, int b, int64_t at, bool valid, float inv, int half) {
+#pragma unroll
+  for (int g = 0; g < 4; g += 2) {  // channels 32 b + 8 g .. + 15
+    if (a.o_f32) {
+      if (valid)
+#pragma unroll
+        for (int e = g; e < g + 2; ++e)
+          *reinterpret_cast<float4*>((float*)a.out + at + 32 * b + 8 * e + 4 * half) =
+              make_float4(o[4 * e] * inv, o[4 * e + 1] * inv, o[4 * e + 2] * inv, o[4 * e + 3] * inv);
+      continue;
+    }
+    uint32_t x[2][2];
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+#pragma unroll
+      for (int w = 0; w < 2; ++w) x[e][w] = pack_bf16x2(o[4 * (g + e) + 2 * w] * inv, o[4 * (g + e) + 2 * w + 1] * inv);
+    // eight channels in a row for each half after the exchange
+    const auto r0 = __builtin_amdgcn_permlane32_swap(x[0][0], x[1][0], false, false);
+    const auto r1 = __builtin_amdgcn_permlane32_swap(x[0][1], x[1][1], false, false);
+    if (valid)
+      *reinterpret_cast<uint4*>((uint16_t*)a.out + at + 32 * b + 8 * (g + half)) = make_uint4(r0[0], r1[0], r0[1], r1[1]);
+  }
+}
+
+// Adds one tile of 32 KB keys, in LDS at kt and vt, to the state.  lim: the last key (counted from the tile's first) that the
+// lane's query sees; masked: whether some query does not see all of them.
+template <int D, int KB>
+__device__ __forceinline__ void add_tile(const char* kt, const char* vt, const uint4 (&qf)[D / 16], float c, int lim, bool masked,
+                                         int lane, PromptState<D>& st) {
+  constexpr int RB = 2 * D;  // bytes of a row
+  const int half = lane >> 5, row = lane & 31;
+  uint4 kf[KB][D / 16];
+#pragma unroll
+  for (int k = 0; k < D / 16; ++k)
+#pragma unroll
+    for (int b = 0; b < KB; ++b)
+      kf[b][k] = *reinterpret_cast<const uint4*>(kt + (32 * b + row) * RB + 16 * ((2 * k + half) ^ k_turn<D>(row)));
+  __builtin_amdgcn_sched_barrier(0);
+  f32x16 s[KB];
+#pragma unroll
+  for (int b = 0; b < KB; ++b) s[b] = f32x16{};
+#pragma unroll
+  for (int k = 0; k < D / 16; ++k)
+#pragma unroll
+    for (int b = 0; b < KB; ++b) s[b] = mfma32_bf16(kf[b][k], qf[k], s[b]);
+  if (masked) {
+#pragma unroll
+    for (int b = 0; b < KB; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[b][i] = 32 * b + 8 * (i / 4) + 4 * half + i % 4 <= lim ? s[b][i] : -INFINITY;
+  }
+  // V^T of 16 keys x 32 channels: group lane / 16 reads the 4 keys of its half, channels 16 ((lane / 16) % 2) ..
+  const int vr = 4 * half + ((lane & 15) >> 2), vc = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+  uint4 vf[2 * KB][D / 32];
+  auto load_v = [&](int k) {
+#pragma unroll
+    for (int b = 0; b < D / 32; ++b) {
+      const int r0 = 16 * k + vr, r1 = r0 + 8;
+      const uint2 lo = lds_column4(vt + r0 * RB + 16 * ((4 * b + vc) ^ v_turn<D>(r0)) + 8 * (lane & 1));
+      const uint2 hi = lds_column4(vt + r1 * RB + 16 * ((4 * b + vc) ^ v_turn<D>(r1)) + 8 * (lane & 1));
+      vf[k][b] = make_uint4(lo.x, lo.y, hi.x, hi.y);
+    }
+  };
+  load_v(0);
+  load_v(1);
+  float mx = vmax(s[0][0], s[KB - 1][1]);
+#pragma unroll
+  for (int b = 0; b < KB; ++b)
+#pragma unroll
+    for (int i = 0; i < 16; i += 2) mx = vmax3(mx, s[b][i], s[b][i + 1]);
+  mx = half_max(mx) * c;
+  // The maximum that the exponents are taken from is raised only where they would pass 2^8: the sums are fp32, and a
+  // probability's rounding to bf16 is relative.
+  if (__any(mx > st.m + 8.f)) {
+    const float mn = fmaxf(st.m, mx), alpha = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(st.m - mn);
+    st.m = mn;
+    st.l *= alpha;
+#pragma unroll
+    for (int b = 0; b < D / 32; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) st.o[b][i] *= alpha;
+  }
+  const float mz = st.m == -INFINITY ? 0.f : st.m;
+  uint4 pf[2 * KB];
+  float ps = 0.f;
+#pragma unroll
+  for (int b = 0; b < KB; ++b) {
+    float p[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      p[i] = __builtin_amdgcn_exp2f(fmaf(s[b][i], c, -mz));
+      ps += p[i];
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      pf[2 * b + h] = make_uint4(pack_bf16x2(p[8 * h], p[8 * h + 1]), pack_bf16x2(p[8 * h + 2], p[8 * h + 3]),
+                                 pack_bf16x2(p[8 * h + 4], p[8 * h + 5]), pack_bf16x2(p[8 * h + 6], p[8 * h + 7]));
+  }
+  st.l += ps;
+#pragma unroll
+  for (int k = 0; k < 2 * KB; ++k) {
+    if (k + 2 < 2 * KB) load_v(k + 2);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int b = 0; b < D / 32; ++b) st.o[b] = mfma32_bf16(vf[k][b], pf[k], st.o[b]);
+  }
+}
+
+// Values that are not finite, in keys that some of the queries do not see: a product with the weight 0 would make NaN of them.
+// They are met only after an output turned out not finite; the tiles are then run again with such values set to zero, and
+// first[kind][channel] is the first key with a NaN, +infinity or -infinity there, to be added to the queries that see it.
+template <int D>
+__device__ __forceinline__ void take_out_nonfinite(char* vt, int rows, int n_keys, int k0, int* first, int tid, int threads) {
+  constexpr int RB = 2 * D;
+  for (int i = tid; i < rows * (RB / 16); i += threads) {
+    const int r = i / (RB / 16), ch = 8 * ((i % (RB / 16)) ^ v_turn<D>(r));
+    uint16_t* p = reinterpret_cast<uint16_t*>(vt + 16 * i);
+    for (int e = 0; e < 8; ++e) {
+      const uint16_t x = p[e];
+      if ((x & 0x7F80) != 0x7F80) continue;
+      p[e] = 0;
+      if (r < n_keys) atomicMin(first + (x & 0x7F ? 0 : 1 + (x >> 15)) * D + ch + e, k0 + r);
+    }
+  }
+}
+template <int D>
+__device__ __forceinline__ void put_back_nonfinite(PromptState<D>& st, const int* first, int lim, int half) {
+#pragma unroll
+  for (int b = 0; b < D / 32; ++b)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int ch = 32 * b + 8 * (i / 4) + 4 * half + i % 4;
+      const float bad[3] = {NAN, INFINITY, -INFINITY};
+#pragma unroll
+      for (int kind = 0; kind < 3; ++kind)
+        if (first[kind * D + ch] <= lim) st.o[b][i] += bad[kind];
+    }
+}
+template <int D>
+__device__ __forceinline__ bool all_finite(const PromptState<D>& st) {
+  float z = 0.f;
+#pragma unroll
+  for (int b = 0; b < D / 32; ++b)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) z = fmaf(st.o[b][i], 0.f, z);
+  return z == 0.f;
+}
+template <int D>
+__device__ __forceinline__ void clear_state(PromptState<D>& st) {
+#pragma unroll
+  for (int b = 0; b < D / 32; ++b) st.o[b] = f32x16{};
+  st.m = -INFINITY;
+  st.l = 0.f;
+}
+
+// A wave's 32 rows r0 .. of (sequence s, key head hk), one per lane column.
+struct PromptRows {
+  int64_t row;  // row of q, out and lse
+  int h, lim;   // query head; last key seen
+  bool valid;
+  int first, last;  // least and largest last key of the wave's rows (none: INT32_MAX, -1)
+  __device__ __forceinline__ PromptRows(const PromptArgs& a, int s, int hk, int r0, int lane) {
+    const int rows = a.nq[s] * a.G, off = a.nk[s] - a.nq[s], r = r0 + (lane & 31), rc = min(r, rows - 1), t = rc / a.G;
+    valid = r < rows;
+    row = a.q0[s] + t;
+    h = hk * a.G + rc - t * a.G;
+    lim = off + t;
+    first = r0 < rows ? off + r0 / a.G : INT32_MAX;
+    last = r0 < rows ? off + (min(r0 + 32, rows) - 1) / a.G : -1;
+  }
+};
+
+template <int D, int NW>
+__global__ __launch_bounds__(NW * 64, 2) void k_prompt_tiles(PromptArgs a) {
+  constexpr int RB = 2 * D, TILE = PT_KEYS * RB, RPI = 1024 / RB, NI = PT_KEYS / RPI / NW;  // rows and loads per wave's load
+  __shared__ __align__(1024) char kb0[TILE], kb1[TILE], vb0[TILE], vb1[TILE];
+  __shared__ int again, first_bad[3 * D];
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
+  const int s = find_seq(a.item_prefix, a.n_seq, blockIdx.x, lane);
+  const int in_seq = blockIdx.x - a.item_prefix[s], Hk = a.H / a.G;
+  const int nk = a.nk[s], rows = a.nq[s] * a.G, tiles = (rows + NW * 32 - 1) / (NW * 32);
+  const int hk = in_seq % Hk, r0 = (tiles - 1 - in_seq / Hk) * NW * 32;  // the rows with the most keys first
+  const PromptRows pr(a, s, hk, r0 + 32 * w, lane);
+  uint4 qf[D / 16];
+  load_queries<D>(a, pr.row * a.q_row + pr.h * a.q_head, pr.valid, half, qf);
+  const int off = nk - a.nq[s], n_tiles = max(0, (off + (min(r0 + NW * 32, rows) - 1) / a.G + PT_KEYS) / PT_KEYS);
+  if (threadIdx.x == 0) again = 0;
+
+  const int lr = lane / (RB / 16), lp = lane % (RB / 16);
+  const uint16_t* kbase = a.k + a.k0[s] * a.k_row + hk * a.k_head;
+  const uint16_t* vbase = a.v + a.k0[s] * a.v_row + hk * a.v_head;
+  auto issue = [&](int j, char* kt, char* vt) {
+#pragma unroll
+    for (int n = 0; n < NI; ++n) {
+      const int i = w + NW * n, tr = i * RPI + lr;
+      const int64_t key = min(j * PT_KEYS + tr, nk - 1);
+      load_lds16(kbase + key * a.k_row + 8 * (lp ^ k_turn<D>(tr)), kt + i * 1024);
+      load_lds16(vbase + key * a.v_row + 8 * (lp ^ v_turn<D>(tr)), vt + i * 1024);
+    }
+  };
+  PromptState<D> st;
+  clear_state(st);
+  auto add = [&](int j, const char* kt, const char* vt) {
+    const int k0 = j * PT_KEYS;
+    if (k0 <= pr.last) add_tile<D, 2>(kt, vt, qf, a.c, pr.lim - k0, k0 + PT_KEYS - 1 > pr.first, lane, st);
+  };
+  if (n_tiles > 0) issue(0, kb0, vb0);
+  for (int j = 0; j < n_tiles; j += 2) {
+    __syncthreads();  // tile j has landed, and every wave is done with the tile before
+    if (j + 1 < n_tiles) issue(j + 1, kb1, vb1);
+    add(j, kb0, vb0);
+    if (j + 1 >= n_tiles) break;
+    __syncthreads();
+    if (j + 2 < n_tiles) issue(j + 2, kb0, vb0);
+    add(j + 1, kb1, vb1);
+  }
+  __syncthreads();
+  if (!__all(all_finite(st))) again = 1;
+  __syncthreads();
+  if (again) {
+    for (int i = threadIdx.x; i < 3 * D; i += NW * 64) first_bad[i] = INT32_MAX;
+    clear_state(st);
+    const int first = off + r0 / a.G;
+    for (int j = 0; j < n_tiles; ++j) {
+      __syncthreads();
+      issue(j, kb0, vb0);
+      __syncthreads();
+      if (j * PT_KEYS + PT_KEYS - 1 > first)
+        take_out_nonfinite<D>(vb0, PT_KEYS, nk - j * PT_KEYS, j * PT_KEYS, first_bad, threadIdx.x, NW * 64);
+      __syncthreads();
+      add(j, kb0, vb0);
+    }
+    put_back_nonfinite(st, first_bad, pr.lim, half);
+  }
+  const float l = half_sum(st.l), inv = pr.lim >= 0 ? 1.f / l : 0.f;
+  const int64_t at = pr.row * a.o_row + pr.h * a.o_head;
+#pragma unroll
+  for (int b = 0; b < D / 32; ++b) store_block(a, st.o[b], b, at, pr.valid, inv, half);
+  if (a.lse && pr.valid && half == 0)
+    a.lse[pr.row * a.H + pr.h] = pr.lim >= 0 ? (st.m + __builtin_amdgcn_logf(l)) * (1.f / LOG2E) : -INFINITY;
+}
+
+// =====================================================================================================
+// Few rows: a workgroup takes 32 rows and `chunk` tiles of 32 keys, which its four waves share out, each with its own two
+// buffers in LDS and no barrier; at the end they merge their states.  Where the keys are in several chunks, the workgroups'
+// states go to the workspace (16-byte piece p of lane l of block b at float4 (4 b + p) 64 + l, then maxima and sums), and
+// k_prompt_merge puts them together in the order of the chunks.
+// =====================================================================================================
+constexpr int PS_WAVES = 4, PS_KEYS = 32;
+
+template <int D>
+__host__ __device__ constexpr int part_floats() { return 32 * D + 64; }
+
+template <int D>
+__global__ __launch_bounds__(PS_WAVES * 64, 1) void k_prompt_split(PromptArgs a) {
+  constexpr int RB = 2 * D, TILE = PS_KEYS * RB, RPI = 1024 / RB, NI = PS_KEYS / RPI;
+  __shared__ __align__(1024) char kb0[PS_WAVES][TILE], kb1[PS_WAVES][TILE], vb0[PS_WAVES][TILE], vb1[PS_WAVES][TILE];
+  __shared__ int first_bad[PS_WAVES][3 * D];
+  __shared__ float sm[PS_WAVES][32], sl[PS_WAVES][32];
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
+  const int s = find_seq(a.item_prefix, a.n_seq, blockIdx.x, lane);
+  const int Hk = a.H / a.G, nk = a.nk[s], rows = a.nq[s] * a.G, n_rt = (rows + 31) / 32;
+  int i = blockIdx.x - a.item_prefix[s];
+  const int hk = i % Hk;
+  i /= Hk;
+  const int r0 = 32 * (n_rt - 1 - i % n_rt), split = i / n_rt;
+  const PromptRows pr(a, s, hk, r0, lane);
+  const int n_tiles = max(0, (pr.last + PS_KEYS) / PS_KEYS), t0 = split * a.chunk, t1 = min(t0 + a.chunk, n_tiles);
+  if (split > 0 && t0 >= t1) return;  // the merge takes as many chunks as these rows have
+  uint4 qf[D / 16];
+  load_queries<D>(a, pr.row * a.q_row + pr.h * a.q_head, pr.valid, half, qf);
+
+  const int lr = lane / (RB / 16), lp = lane % (RB / 16);
+  const uint16_t* kbase = a.k + a.k0[s] * a.k_row + hk * a.k_head;
+  const uint16_t* vbase = a.v + a.k0[s] * a.v_row + hk * a.v_head;
+  auto issue = [&](int j, char* kt, char* vt) {
+#pragma unroll
+    for (int n = 0; n < NI; ++n) {
+      const int tr = n * RPI + lr;
+      const int64_t key = min(j * PS_KEYS + tr, nk - 1);
+      load_lds16(kbase + key * a.k_row + 8 * (lp ^ k_turn<D>(tr)), kt + n * 1024);
+      load_lds16(vbase + key * a.v_row + 8 * (lp ^ v_turn<D>(tr)), vt + n * 1024);
+    }
+  };
+  PromptState<D> st;
+  clear_state(st);
+  auto add = [&](int j, const char* kt, const char* vt) {
+    add_tile<D, 1>(kt, vt, qf, a.c, pr.lim - j * PS_KEYS, j * PS_KEYS + PS_KEYS - 1 > pr.first, lane, st);
+  };
+  // One tile ahead; past the last tile the loads repeat it (from the L2), so that a wait for a fixed number of loads is one for
+  // the tile at hand.
+  if (int j = t0 + w; j < t1) {
+    issue(j, kb0[w], vb0[w]);
+    for (;;) {
+      issue(j + PS_WAVES < t1 ? j + PS_WAVES : j, kb1[w], vb1[w]);
+      vm_wait_below_c<2 * NI>();
+      add(j, kb0[w], vb0[w]);
+      if ((j += PS_WAVES) >= t1) break;
+      issue(j + PS_WAVES < t1 ? j + PS_WAVES : j, kb0[w], vb0[w]);
+      vm_wait_below_c<2 * NI>();
+      add(j, kb1[w], vb1[w]);
+      if ((j += PS_WAVES) >= t1) break;
+    }
+    vm_wait_all();
+  }
+  if (!__all(all_finite(st))) {
+    for (int e = lane; e < 3 * D; e += 64) first_bad[w][e] = INT32_MAX;
+    clear_state(st);
+    for (int j = t0 + w; j < t1; j += PS_WAVES) {
+      issue(j, kb0[w], vb0[w]);
+      vm_wait_all();
+      if (j * PS_KEYS + PS_KEYS - 1 > pr.first)
+        take_out_nonfinite<D>(vb0[w], PS_KEYS, nk - j * PS_KEYS, j * PS_KEYS, first_bad[w], lane, 64);
+      add(j, kb0[w], vb0[w]);
+    }
+    put_back_nonfinite(st, first_bad[w], pr.lim, half);
+  }
+  // the waves' states, merged: wave b takes block b of the output
+  const float lw = half_sum(st.l);
+  __syncthreads();
+  float* ex = reinterpret_cast<float*>(w < 2 ? (w == 0 ? kb0[0] : kb1[0]) : (w == 2 ? vb0[0] : vb1[0]));
+#pragma unroll
+  for (int b = 0; b < D / 32; ++b)
+#pragma unroll
+    for (int p = 0; p < 4; ++p)
+      reinterpret_cast<float4*>(ex)[(4 * b + p) * 64 + lane] =
+          make_float4(st.o[b][4 * p], st.o[b][4 * p + 1], st.o[b][4 * p + 2], st.o[b][4 * p + 3]);
+  if (half == 0) {
+    sm[w][lane] = st.m;
+    sl[w][lane] = lw;
+  }
+  __syncthreads();
+  if (w >= D / 32) return;
+  const int q = lane & 31;
+  float m = -INFINITY, l = 0.f, f[PS_WAVES];
+#pragma unroll
+  for (int x = 0; x < PS_WAVES; ++x) m = fmaxf(m, sm[x][q]);
+  f32x16 o{};
+#pragma unroll
+  for (int x = 0; x < PS_WAVES; ++x) {
+    f[x] = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(sm[x][q] - m);
+    l += sl[x][q] * f[x];
+    const float4* src = reinterpret_cast<const float4*>(x < 2 ? (x == 0 ? kb0[0] : kb1[0]) : (x == 2 ? vb0[0] : vb1[0]));
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+      const float4 v = src[(4 * w + p) * 64 + lane];
+      o[4 * p] += v.x * f[x];
+      o[4 * p + 1] += v.y * f[x];
+      o[4 * p + 2] += v.z * f[x];
+      o[4 * p + 3] += v.w * f[x];
+    }
+  }
+  if (a.n_split[s] > 1) {
+    float* part = a.part + (int64_t)blockIdx.x * part_floats<D>();
+#pragma unroll
+    for (int p = 0; p < 4; ++p)
+      reinterpret_cast<float4*>(part)[(4 * w + p) * 64 + lane] = make_float4(o[4 * p], o[4 * p + 1], o[4 * p + 2], o[4 * p + 3]);
+    if (w == 0) part[32 * D + lane] = half ? l : m;
+    return;
+  }
+  const float inv = pr.lim >= 0 ? 1.f / l : 0.f;
+  store_block(a, o, w, pr.row * a.o_row + pr.h * a.o_head, pr.valid, inv, half);
+  if (a.lse && pr.valid && half == 0 && w == 0)
+    a.lse[pr.row * a.H + pr.h] = pr.lim >= 0 ? (m + __builtin_amdgcn_logf(l)) * (1.f / LOG2E) : -INFINITY;
+}
+
+// The chunks' states of 32 rows put together, a block of 32 channels per wave.
+template <int D>
+__global__ __launch_bounds__(2 * D) void k_prompt_merge(PromptArgs a) {
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, q = lane & 31;
+  const int s = find_seq(a.merge_prefix, a.n_seq, blockIdx.x, lane);
+  const int Hk = a.H / a.G, n_rt = (a.nq[s] * a.G + 31) / 32, i = blockIdx.x - a.merge_prefix[s], hk = i % Hk;
+  const PromptRows pr(a, s, hk, 32 * (n_rt - 1 - i / Hk), lane);
+  const int n_tiles = max(0, (pr.last + PS_KEYS) / PS_KEYS), n = max(1, (n_tiles + a.chunk - 1) / a.chunk);
+  const float* part = a.part + (int64_t)(a.item_prefix[s] + i) * part_floats<D>();
+  const int64_t step = (int64_t)n_rt * Hk * part_floats<D>();
+  float m = -INFINITY, l = 0.f;
+  for (int c = 0; c < n; ++c) m = fmaxf(m, part[c * step + 32 * D + q]);
+  f32x16 o{};
+  for (int c = 0; c < n; ++c) {
+    const float* x = part + c * step;
+    const float f = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(x[32 * D + q] - m);
+    l += x[32 * D + 32 + q] * f;
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+      const float4 v = reinterpret_cast<const float4*>(x)[(4 * w + p) * 64 + lane];
+      o[4 * p] += v.x * f;
+      o[4 * p + 1] += v.y * f;
+      o[4 * p + 2] += v.z * f;
+      o[4 * p + 3] += v.w * f;
+    }
+  }
+  const float inv = pr.lim >= 0 ? 1.f / l : 0.f;
+  store_block(a, o, w, pr.row * a.o_row + pr.h * a.o_head, pr.valid, inv, half);
+  if (a.lse && pr.valid && half == 0 && w == 0)
+    a.lse[pr.row * a.H + pr.h] = pr.lim >= 0 ? (m + __builtin_amdgcn_logf(l)) * (1.f / LOG2E) : -INFINITY;
+}
+
+// Which kernel, and in how many chunks.
+bool plan_prompt(PromptArgs& a, int64_t workspace_bytes, int64_t* need) {
+  const int Hk = a.H / a.G;
+  const int64_t part = 4 * (32 * a.D + 64);
+  *need = 0;
+  int64_t rows = 0, wide = 0, units = 0;
+  int t_max = 0;
+  for (int i = 0; i < a.n_seq; ++i) {
+    const int64_t r = (int64_t)a.nq[i] * a.G, t = (a.nk[i] + PS_KEYS - 1) / PS_KEYS;
+    rows += r * Hk;
+    wide += (r + 255) / 256 * Hk;
+    units += (r + 31) / 32 * Hk * t;
+    t_max = std::max(t_max, (int)t);
+  }
+  if (wide >= 192 || (wide > 0 && rows / wide > 160)) return false;
+  // about two workgroups per CU, of at least 16 tiles
+  int chunk = std::max<int64_t>(16, (units + 511) / 512);
+  for (;; chunk *= 2) {
+    int64_t items = 0;
+    bool split = false;
+    for (int i = 0; i < a.n_seq; ++i) {
+      const int n_rt = (int)(((int64_t)a.nq[i] * a.G + 31) / 32), t = (a.nk[i] + PS_KEYS - 1) / PS_KEYS;
+      a.n_split[i] = std::max(1, (t + chunk - 1) / chunk);
+      split = split || a.n_split[i] > 1;
+      a.item_prefix[i + 1] = a.item_prefix[i] + n_rt * Hk * a.n_split[i];
+      a.merge_prefix[i + 1] = a.merge_prefix[i] + (a.n_split[i] > 1 ? n_rt * Hk : 0);
+    }
+    a.chunk = chunk;
+    *need = split ? a.item_prefix[a.n_seq] * part : 0;
+    if (*need <= workspace_bytes) return true;
+    if (chunk > t_max) return true;
+  }
+}
+
+hipError_t launch_prompt_attention(PromptArgs a, void* workspace, int64_t workspace_bytes, hipStream_t s) {
+  if (a.n_seq == 0) return hipSuccess;
+  int64_t need = 0;
+  if (plan_prompt(a, workspace_bytes, &need)) {
+    a.part = (float*)workspace;
+    const dim3 grid(a.item_prefix[a.n_seq]), merge(a.merge_prefix[a.n_seq]);
+    if (a.D == 64) {
+      hipLaunchKernelGGL(k_prompt_split<64>, grid, dim3(PS_WAVES * 64), 0, s, a);
+      if (merge.x) hipLaunchKernelGGL(k_prompt_merge<64>, merge, dim3(128), 0, s, a);
+    } else {
+      hipLaunchKernelGGL(k_prompt_split<128>, grid, dim3(PS_WAVES * 64), 0, s, a);
+      if (merge.x) hipLaunchKernelGGL(k_prompt_merge<128>, merge, dim3(256), 0, s, a);
+    }
+    return hipGetLastError();
+  }
+  for (int i = 0; i < a.n_seq; ++i)
+    a.item_prefix[i + 1] = a.item_prefix[i] + (int)(((int64_t)a.nq[i] * a.G + 255) / 256) * (a.H / a.G);
+  const dim3 grid(a.item_prefix[a.n_seq]);
   if (a.D == 64)
-    hipLaunchKernelGGL(k_prompt_rows<64>, grid, dim3(256), 0, s, a);
+    hipLaunchKernelGGL((k_prompt_tiles<64, 8>), grid, dim3(512), 0, s, a);
   else
-    hipLaunchKernelGGL(k_prompt_rows<128>, grid, dim3(256), 0, s, a);
+    hipLaunchKernelGGL((k_prompt_tiles<128, 8>), grid, dim3(512), 0, s, a);
   return hipGetLastError();
 }
 
