@@ -925,6 +925,8 @@ static int check_prompt_desc(const fsx_prompt_desc* d) {
                         {d->v_row, d->v_head, d->k_rows}, {d->out_row, d->out_head, d->q_rows}})
     if (x[0] < 0 || x[1] < 0 || x[0] % 8 || x[1] % 8 || x[1] > (int64_t)1 << 50 || (__int128)x[0] * x[2] > (__int128)1 << 60)
       return fail(FSX_E_INVALID, "strides must be non-negative multiples of 8 elements, within 2^60 elements in all");
+  if (d->k_row > (int64_t)1 << 27 || d->v_row > (int64_t)1 << 27)
+    return fail(FSX_E_UNSUPPORTED, "rows of k and v more than 2^27 elements apart");
   return FSX_OK;
 }
 

@@ -113,47 +113,40 @@ __device__ __forceinline__ void store_block(const PromptArgs& a, const f32x16& o
   }
 }
 
-// Adds one tile of 32 KB keys, in LDS at kt and vt, to the state.  lim: the last key (counted from the tile's first) that the
-// lane's query sees; masked: whether some query does not see all of them.
+// S^T of a tile of 32 KB keys, in LDS at kt.
 template <int D, int KB>
-__device__ __forceinline__ void add_tile(const char* kt, const char* vt, const uint4 (&qf)[D / 16], float c, int lim, bool masked,
-                                         int lane, PromptState<D>& st) {
-  constexpr int RB = 2 * D;  // bytes of a row
+__device__ __forceinline__ void tile_scores(const char* kt, const uint4 (&qf)[D / 16], int lane, f32x16 (&s)[KB]) {
+  constexpr int KS = D / 16, AHEAD = 4;  // the reads run ahead of the products
   const int half = lane >> 5, row = lane & 31;
-  uint4 kf[KB][D / 16];
-#pragma unroll
-  for (int k = 0; k < D / 16; ++k)
-#pragma unroll
-    for (int b = 0; b < KB; ++b)
-      kf[b][k] = *reinterpret_cast<const uint4*>(kt + (32 * b + row) * RB + 16 * ((2 * k + half) ^ k_turn<D>(row)));
-  __builtin_amdgcn_sched_barrier(0);
-  f32x16 s[KB];
+  uint4 kf[KB * KS];
+  auto load_k = [&](int i) {
+    const int b = i / KS, k = i % KS;
+    kf[i] = *reinterpret_cast<const uint4*>(kt + (32 * b + row) * 2 * D + 16 * ((2 * k + half) ^ k_turn<D>(row)));
+  };
 #pragma unroll
   for (int b = 0; b < KB; ++b) s[b] = f32x16{};
 #pragma unroll
-  for (int k = 0; k < D / 16; ++k)
+  for (int i = 0; i < AHEAD; ++i) load_k(i);
 #pragma unroll
-    for (int b = 0; b < KB; ++b) s[b] = mfma32_bf16(kf[b][k], qf[k], s[b]);
+  for (int i = 0; i < KB * KS; i += 2) {
+    if (i + AHEAD < KB * KS) load_k(i + AHEAD);
+    if (i + AHEAD + 1 < KB * KS) load_k(i + AHEAD + 1);
+    __builtin_amdgcn_sched_barrier(0);
+    s[i / KS] = mfma32_bf16(kf[i], qf[i % KS], s[i / KS]);
+    s[(i + 1) / KS] = mfma32_bf16(kf[i + 1], qf[(i + 1) % KS], s[(i + 1) / KS]);
+  }
+}
+
+// The tile's probabilities (B operand of the second product) from its scores, and the state's maximum and sum.  lim: the last
+// key (counted from the tile's first) that the lane's query sees; masked: whether some query does not see all of them.
+template <int D, int KB>
+__device__ __forceinline__ void tile_softmax(f32x16 (&s)[KB], float c, int lim, bool masked, int half, PromptState<D>& st, uint4 (&pf)[2 * KB]) {
   if (masked) {
 #pragma unroll
     for (int b = 0; b < KB; ++b)
 #pragma unroll
       for (int i = 0; i < 16; ++i) s[b][i] = 32 * b + 8 * (i / 4) + 4 * half + i % 4 <= lim ? s[b][i] : -INFINITY;
   }
-  // V^T of 16 keys x 32 channels: group lane / 16 reads the 4 keys of its half, channels 16 ((lane / 16) % 2) ..
-  const int vr = 4 * half + ((lane & 15) >> 2), vc = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-  uint4 vf[2 * KB][D / 32];
-  auto load_v = [&](int k) {
-#pragma unroll
-    for (int b = 0; b < D / 32; ++b) {
-      const int r0 = 16 * k + vr, r1 = r0 + 8;
-      const uint2 lo = lds_column4(vt + r0 * RB + 16 * ((4 * b + vc) ^ v_turn<D>(r0)) + 8 * (lane & 1));
-      const uint2 hi = lds_column4(vt + r1 * RB + 16 * ((4 * b + vc) ^ v_turn<D>(r1)) + 8 * (lane & 1));
-      vf[k][b] = make_uint4(lo.x, lo.y, hi.x, hi.y);
-    }
-  };
-  load_v(0);
-  load_v(1);
   float mx = vmax(s[0][0], s[KB - 1][1]);
 #pragma unroll
   for (int b = 0; b < KB; ++b)
@@ -172,7 +165,6 @@ __device__ __forceinline__ void add_tile(const char* kt, const char* vt, const u
       for (int i = 0; i < 16; ++i) st.o[b][i] *= alpha;
   }
   const float mz = st.m == -INFINITY ? 0.f : st.m;
-  uint4 pf[2 * KB];
   float ps = 0.f;
 #pragma unroll
   for (int b = 0; b < KB; ++b) {
@@ -188,13 +180,41 @@ __device__ __forceinline__ void add_tile(const char* kt, const char* vt, const u
                                  pack_bf16x2(p[8 * h + 4], p[8 * h + 5]), pack_bf16x2(p[8 * h + 6], p[8 * h + 7]));
   }
   st.l += ps;
+}
+
+// O^T += V^T P^T of a tile, its values in LDS at vt.
+template <int D, int KB>
+__device__ __forceinline__ void tile_values(const char* vt, const uint4 (&pf)[2 * KB], int lane, PromptState<D>& st) {
+  // V^T of 16 keys x 32 channels: group lane / 16 reads the 4 keys of its half, channels 16 ((lane / 16) % 2) ..
+  const int vr = 4 * (lane >> 5) + ((lane & 15) >> 2), vc = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+  uint4 vf[2 * KB][D / 32];
+  auto load_v = [&](int k) {
+#pragma unroll
+    for (int b = 0; b < D / 32; ++b) {
+      const int r0 = 16 * k + vr, r1 = r0 + 8;
+      const uint2 lo = lds_column4(vt + r0 * 2 * D + 16 * ((4 * b + vc) ^ v_turn<D>(r0)) + 8 * (lane & 1));
+      const uint2 hi = lds_column4(vt + r1 * 2 * D + 16 * ((4 * b + vc) ^ v_turn<D>(r1)) + 8 * (lane & 1));
+      vf[k][b] = make_uint4(lo.x, lo.y, hi.x, hi.y);
+    }
+  };
+  load_v(0);
 #pragma unroll
   for (int k = 0; k < 2 * KB; ++k) {
-    if (k + 2 < 2 * KB) load_v(k + 2);
+    if (k + 1 < 2 * KB) load_v(k + 1);
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int b = 0; b < D / 32; ++b) st.o[b] = mfma32_bf16(vf[k][b], pf[k], st.o[b]);
   }
+}
+
+template <int D, int KB>
+__device__ __forceinline__ void add_tile(const char* kt, const char* vt, const uint4 (&qf)[D / 16], float c, int lim, bool masked,
+                                         int lane, PromptState<D>& st) {
+  f32x16 s[KB];
+  uint4 pf[2 * KB];
+  tile_scores<D, KB>(kt, qf, lane, s);
+  tile_softmax<D, KB>(s, c, lim, masked, lane >> 5, st, pf);
+  tile_values<D, KB>(vt, pf, lane, st);
 }
 
 // Values that are not finite, in keys that some of the queries do not see: a product with the weight 0 would make NaN of them.
@@ -261,18 +281,53 @@ struct PromptRows {
   }
 };
 
-template <int D, int NW>
-__global__ __launch_bounds__(NW * 64, 2) void k_prompt_tiles(PromptArgs a) {
-  constexpr int RB = 2 * D, TILE = PT_KEYS * RB, RPI = 1024 / RB, NI = PT_KEYS / RPI / NW;  // rows and loads per wave's load
-  __shared__ __align__(1024) char kb0[TILE], kb1[TILE], vb0[TILE], vb1[TILE];
+// The value is computed here: neither the products nor the vector work that make it may move to the other side of a barrier,
+// which to the compiler concerns memory alone.
+__device__ __forceinline__ void here(f32x16& x) { asm volatile("" : "+v"(x)); }
+__device__ __forceinline__ void here(uint4& x) {
+  u32x4_t y = __builtin_bit_cast(u32x4_t, x);
+  asm volatile("" : "+v"(y));
+  x = __builtin_bit_cast(uint4, y);
+}
+
+// Every wave of the workgroup has got here; memory operations stay on their side.
+__device__ __forceinline__ void meet() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("" ::: "memory");
+}
+
+// Direct load of 16 bytes per lane from base + at (bytes) to LDS at lds + 16 lane.  In assembly, so that the compiler does not
+// take every LDS read that might meet it for one that has to wait: the waits are the kernel's own (vm_wait_all, then meet).
+__device__ __forceinline__ void dma16(const void* base, uint32_t at, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(at), "s"(base) : "memory");
+}
+__device__ __forceinline__ uint32_t lds_address(const void* p) {
+  return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)p;
+}
+
+// The eight waves, two per SIMD, work in turns: while waves 0-3 run matrix instructions (the scores of tile j + 1, then the
+// values of tile j), waves 4-7 run the softmax of tile j on the vector units, and the other way round, a barrier between the
+// turns.  Turn 2 j + 1 is matrix instructions of tile j for waves 0-3, turn 2 j + 2 for waves 4-7.  In turn 2 j + 1 all waves
+// send for V(j + 1) and K(j + 3), over V(j - 1) and K(j), last read in turn 2 j; both have landed at the end of turn 2 j + 2.
+// V(j + 1) is first read in turn 2 j + 3, and K(j + 3) at the end of turn 2 j + 4: a wave reads the first keys of its products
+// before the barrier.
+template <int D>
+__global__ __launch_bounds__(512, 2) void k_prompt_tiles(PromptArgs a) {
+  constexpr int NW = 8, RB = 2 * D, TILE = PT_KEYS * RB, RPI = 1024 / RB, NI = PT_KEYS / RPI / NW;  // rows and loads per wave's load
+  constexpr int KS = D / 16, NV = D / 32, KAHEAD = 8;
+  __shared__ __align__(1024) char kt[3 * TILE], vt[2 * TILE];
   __shared__ int again, first_bad[3 * D];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
+  const bool second = w >= NW / 2;
   const int s = find_seq(a.item_prefix, a.n_seq, blockIdx.x, lane);
   const int in_seq = blockIdx.x - a.item_prefix[s], Hk = a.H / a.G;
   const int nk = a.nk[s], rows = a.nq[s] * a.G, tiles = (rows + NW * 32 - 1) / (NW * 32);
   const int hk = in_seq % Hk, r0 = (tiles - 1 - in_seq / Hk) * NW * 32;  // the rows with the most keys first
   const PromptRows pr(a, s, hk, r0 + 32 * w, lane);
-  uint4 qf[D / 16];
+  uint4 qf[KS];
   load_queries<D>(a, pr.row * a.q_row + pr.h * a.q_head, pr.valid, half, qf);
   const int off = nk - a.nq[s], n_tiles = max(0, (off + (min(r0 + NW * 32, rows) - 1) / a.G + PT_KEYS) / PT_KEYS);
   if (threadIdx.x == 0) again = 0;
@@ -280,49 +335,140 @@ __global__ __launch_bounds__(NW * 64, 2) void k_prompt_tiles(PromptArgs a) {
   const int lr = lane / (RB / 16), lp = lane % (RB / 16);
   const uint16_t* kbase = a.k + a.k0[s] * a.k_row + hk * a.k_head;
   const uint16_t* vbase = a.v + a.k0[s] * a.v_row + hk * a.v_head;
-  auto issue = [&](int j, char* kt, char* vt) {
+  const uint32_t kl = lds_address(kt), vl = lds_address(vt);
+  // the lane's piece of a load, the same in all of a wave's loads
+  const uint32_t kp = 16 * (lp ^ k_turn<D>(w * RPI + lr)), vp = 16 * (lp ^ v_turn<D>(w * RPI + lr));
+  const uint32_t kat = (uint32_t)lr * (uint32_t)a.k_row * 2 + kp, vat = (uint32_t)lr * (uint32_t)a.v_row * 2 + vp;
+  auto issue = [&](int j, uint32_t t, const uint16_t* base, int64_t stride, uint32_t at, uint32_t piece) {
+    if (j >= n_tiles) return;
 #pragma unroll
     for (int n = 0; n < NI; ++n) {
-      const int i = w + NW * n, tr = i * RPI + lr;
-      const int64_t key = min(j * PT_KEYS + tr, nk - 1);
-      load_lds16(kbase + key * a.k_row + 8 * (lp ^ k_turn<D>(tr)), kt + i * 1024);
-      load_lds16(vbase + key * a.v_row + 8 * (lp ^ v_turn<D>(tr)), vt + i * 1024);
+      const int i = w + NW * n, r = j * PT_KEYS + i * RPI;
+      if (r + RPI <= nk) {
+        dma16(base + r * stride, at, t + i * 1024);
+      } else {  // past the last key: that key again
+        const int r1 = min(r, nk - 1);
+        dma16(base + r1 * stride, (uint32_t)min(lr, nk - 1 - r1) * (uint32_t)stride * 2 + piece, t + i * 1024);
+      }
     }
   };
+  auto issue_k = [&](int j, int buf) { issue(j, kl + buf * TILE, kbase, a.k_row, kat, kp); };
+  auto issue_v = [&](int j, int buf) { issue(j, vl + buf * TILE, vbase, a.v_row, vat, vp); };
+
+  // the lane's pieces of K (A operand of the scores, see tile_scores) and V (of the values, see tile_values) in a tile
+  const int krow = lane & 31;
+  const uint32_t kread = krow * RB + 16 * (half ^ k_turn<D>(krow));
+  const int vr = 4 * half + ((lane & 15) >> 2), vc = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+  uint32_t vread[NV];
+#pragma unroll
+  for (int b = 0; b < NV; ++b) vread[b] = vr * RB + 16 * ((4 * b + vc) ^ v_turn<D>(vr)) + 8 * (lane & 1);
+
   PromptState<D> st;
   clear_state(st);
-  auto add = [&](int j, const char* kt, const char* vt) {
-    const int k0 = j * PT_KEYS;
-    if (k0 <= pr.last) add_tile<D, 2>(kt, vt, qf, a.c, pr.lim - k0, k0 + PT_KEYS - 1 > pr.first, lane, st);
+  f32x16 sc[2];
+  uint4 kf[2 * KS], pf[4], vf[4][NV];
+  auto load_k = [&](int i, uint32_t t) {  // the tile's two blocks of keys in turn
+    kf[i] = *reinterpret_cast<const uint4*>(kt + ((t + kread) ^ (32 * (i >> 1))) + (i & 1) * 32 * RB);
   };
-  if (n_tiles > 0) issue(0, kb0, vb0);
-  for (int j = 0; j < n_tiles; j += 2) {
-    __syncthreads();  // tile j has landed, and every wave is done with the tile before
-    if (j + 1 < n_tiles) issue(j + 1, kb1, vb1);
-    add(j, kb0, vb0);
-    if (j + 1 >= n_tiles) break;
-    __syncthreads();
-    if (j + 2 < n_tiles) issue(j + 2, kb0, vb0);
-    add(j + 1, kb1, vb1);
-  }
+  auto load_v = [&](int k, uint32_t t) {
+#pragma unroll
+    for (int b = 0; b < NV; ++b) {
+      const uint2 lo = lds_column4(vt + t + vread[b] + 16 * k * RB), hi = lds_column4(vt + t + vread[b] + (16 * k + 8) * RB);
+      vf[k][b] = make_uint4(lo.x, lo.y, hi.x, hi.y);
+    }
+  };
+  auto scores = [&](uint32_t t, bool values, uint32_t tv) {  // the first KAHEAD keys' pieces are in kf
+#pragma unroll
+    for (int i = 0; i < 2 * KS; i += 2) {
+      if (i + KAHEAD < 2 * KS) {
+        load_k(i + KAHEAD, t);
+        load_k(i + KAHEAD + 1, t);
+      }
+      if (values && i == 2 * KS - KAHEAD / 2 - 2) load_v(0, tv);
+      if (values && i == 2 * KS - 2) load_v(1, tv);
+      __builtin_amdgcn_sched_barrier(0);
+      sc[0] = i == 0 ? mfma32_bf16(kf[i], qf[i / 2], f32x16{}) : mfma32_bf16(kf[i], qf[i / 2], sc[0]);
+      sc[1] = i == 0 ? mfma32_bf16(kf[i + 1], qf[i / 2], f32x16{}) : mfma32_bf16(kf[i + 1], qf[i / 2], sc[1]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+
+  issue_k(0, 0);
+  issue_v(0, 0);
+  issue_k(1, 1);
+  issue_k(2, 2);
+  vm_wait_all();
   __syncthreads();
+  if (n_tiles > 0) {
+#pragma unroll
+    for (int i = 0; i < KAHEAD; ++i) load_k(i, 0);
+    scores(0, false, 0);
+    here(sc[0]);
+    here(sc[1]);
+  }
+  meet();
+  if (second) meet();
+  int kb = 1;  // buffer of K(j + 1)
+  for (int j = 0; j < n_tiles; ++j) {
+    const int k0 = j * PT_KEYS;
+    const uint32_t tk = kb * TILE, tv = (j & 1) * TILE;
+    const int kfree = kb == 0 ? 2 : kb - 1;  // that of K(j), which K(j + 3) takes
+    if (second) {
+      issue_v(j + 1, (j + 1) & 1);
+      issue_k(j + 3, kfree);
+    }
+    tile_softmax<D, 2>(sc, a.c, pr.lim - k0, k0 + PT_KEYS - 1 > pr.first, half, st, pf);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) here(pf[k]);
+    asm volatile("" : "+v"(st.l));
+#pragma unroll
+    for (int i = 0; i < KAHEAD; ++i) load_k(i, tk);
+    if (!second) vm_wait_all();
+    meet();
+    if (!second) {
+      issue_v(j + 1, (j + 1) & 1);
+      issue_k(j + 3, kfree);
+    }
+    __builtin_amdgcn_s_setprio(1);
+    scores(tk, true, tv);
+    here(sc[0]);
+    here(sc[1]);
+#pragma unroll
+    for (int b = 0; b < NV; ++b) here(st.o[b]);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if (k + 2 < 4) load_v(k + 2, tv);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int b = 0; b < NV; ++b) st.o[b] = mfma32_bf16(vf[k][b], pf[k], st.o[b]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+#pragma unroll
+    for (int b = 0; b < NV; ++b) here(st.o[b]);
+    __builtin_amdgcn_s_setprio(0);
+    if (second) vm_wait_all();
+    meet();
+    kb = kb == 2 ? 0 : kb + 1;
+  }
+  if (!second) meet();
   if (!__all(all_finite(st))) again = 1;
   __syncthreads();
   if (again) {
     for (int i = threadIdx.x; i < 3 * D; i += NW * 64) first_bad[i] = INT32_MAX;
     clear_state(st);
-    const int first = off + r0 / a.G;
     for (int j = 0; j < n_tiles; ++j) {
+      const int k0 = j * PT_KEYS;
       __syncthreads();
-      issue(j, kb0, vb0);
+      issue_k(j, 0);
+      issue_v(j, 0);
+      vm_wait_all();
       __syncthreads();
-      if (j * PT_KEYS + PT_KEYS - 1 > first)
-        take_out_nonfinite<D>(vb0, PT_KEYS, nk - j * PT_KEYS, j * PT_KEYS, first_bad, threadIdx.x, NW * 64);
+      if (k0 + PT_KEYS - 1 > off + r0 / a.G) take_out_nonfinite<D>(vt, PT_KEYS, nk - k0, k0, first_bad, threadIdx.x, NW * 64);
       __syncthreads();
-      add(j, kb0, vb0);
+      add_tile<D, 2>(kt, vt, qf, a.c, pr.lim - k0, true, lane, st);
     }
-    put_back_nonfinite(st, first_bad, pr.lim, half);
   }
+  if (again) put_back_nonfinite(st, first_bad, pr.lim, half);
   const float l = half_sum(st.l), inv = pr.lim >= 0 ? 1.f / l : 0.f;
   const int64_t at = pr.row * a.o_row + pr.h * a.o_head;
 #pragma unroll
@@ -540,9 +686,9 @@ hipError_t launch_prompt_attention(PromptArgs a, void* workspace, int64_t worksp
     a.item_prefix[i + 1] = a.item_prefix[i] + (int)(((int64_t)a.nq[i] * a.G + 255) / 256) * (a.H / a.G);
   const dim3 grid(a.item_prefix[a.n_seq]);
   if (a.D == 64)
-    hipLaunchKernelGGL((k_prompt_tiles<64, 8>), grid, dim3(512), 0, s, a);
+    hipLaunchKernelGGL(k_prompt_tiles<64>, grid, dim3(512), 0, s, a);
   else
-    hipLaunchKernelGGL((k_prompt_tiles<128, 8>), grid, dim3(512), 0, s, a);
+    hipLaunchKernelGGL(k_prompt_tiles<128>, grid, dim3(512), 0, s, a);
   return hipGetLastError();
 }
 
