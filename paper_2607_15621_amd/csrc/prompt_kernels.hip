@@ -73,18 +73,20 @@ struct PromptState {
 
 // The wave's queries as the B operand: step s, lane l: channels 16 s + 8 (l / 32) .. + 7 of query l % 32.
 template <int D>
-__device__ __forceinline__ void load_queries(const PromptArgs& a, int64_t at, bool valid, int half, uint4 (&qf)[D / 16]) {
+__device__ __forceinline__ void load_queries(const PromptArgs& a, int64_t at, int half, uint4 (&qf)[D / 16]) {
+  if (a.q_f32) {
+    const float* q = (const float*)a.q + at + 8 * half;
+    float4 x[D / 8];
 #pragma unroll
-  for (int s = 0; s < D / 16; ++s) {
-    qf[s] = make_uint4(0, 0, 0, 0);
-    if (!valid) continue;
-    if (a.q_f32) {
-      const float4* p = reinterpret_cast<const float4*>((const float*)a.q + at + 16 * s + 8 * half);
-      const float4 lo = p[0], hi = p[1];
-      qf[s] = make_uint4(pack_bf16x2(lo.x, lo.y), pack_bf16x2(lo.z, lo.w), pack_bf16x2(hi.x, hi.y), pack_bf16x2(hi.z, hi.w));
-    } else {
-      qf[s] = *reinterpret_cast<const uint4*>((const uint16_t*)a.q + at + 16 * s + 8 * half);
-    }
+    for (int i = 0; i < D / 8; ++i) x[i] = *reinterpret_cast<const float4*>(q + 16 * (i / 2) + 4 * (i % 2));
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s)
+      qf[s] = make_uint4(pack_bf16x2(x[2 * s].x, x[2 * s].y), pack_bf16x2(x[2 * s].z, x[2 * s].w),
+                         pack_bf16x2(x[2 * s + 1].x, x[2 * s + 1].y), pack_bf16x2(x[2 * s + 1].z, x[2 * s + 1].w));
+  } else {
+    const uint16_t* q = (const uint16_t*)a.q + at + 8 * half;
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s) qf[s] = *reinterpret_cast<const uint4*>(q + 16 * s);
   }
 }
 
@@ -138,48 +140,52 @@ __device__ __forceinline__ void tile_scores(const char* kt, const uint4 (&qf)[D 
 }
 
 // The tile's probabilities (B operand of the second product) from its scores, and the state's maximum and sum.  lim: the last
-// key (counted from the tile's first) that the lane's query sees; masked: whether some query does not see all of them.
-template <int D, int KB>
-__device__ __forceinline__ void tile_softmax(f32x16 (&s)[KB], float c, int lim, bool masked, int half, PromptState<D>& st, uint4 (&pf)[2 * KB]) {
+// key (counted from the tile's first) that the lane's query sees; masked: whether some query does not see all of them.  between(i)
+// runs after the exponentials of the i-th 16-key step.
+// The maximum that the exponents are taken from is raised only where they would pass 2^8 (the sums are fp32, and a probability's
+// rounding to bf16 is relative), so the exponentials need not wait for the tile's own maximum; a tile that raises it does them again.
+template <int D, int KB, class Between>
+__device__ __forceinline__ void tile_softmax(f32x16 (&s)[KB], float c, int lim, bool masked, int half, PromptState<D>& st, uint4 (&pf)[2 * KB],
+                                             Between between) {
   if (masked) {
 #pragma unroll
     for (int b = 0; b < KB; ++b)
 #pragma unroll
       for (int i = 0; i < 16; ++i) s[b][i] = 32 * b + 8 * (i / 4) + 4 * half + i % 4 <= lim ? s[b][i] : -INFINITY;
   }
-  float mx = vmax(s[0][0], s[KB - 1][1]);
+  float ps[4];
+  auto probabilities = [&](float mz, int k) {
+    float p[8];
 #pragma unroll
-  for (int b = 0; b < KB; ++b)
+    for (int i = 0; i < 8; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(s[k / 2][8 * (k % 2) + i], c, -mz));
 #pragma unroll
-    for (int i = 0; i < 16; i += 2) mx = vmax3(mx, s[b][i], s[b][i + 1]);
-  mx = half_max(mx) * c;
-  // The maximum that the exponents are taken from is raised only where they would pass 2^8: the sums are fp32, and a
-  // probability's rounding to bf16 is relative.
-  if (__any(mx > st.m + 8.f)) {
-    const float mn = fmaxf(st.m, mx), alpha = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(st.m - mn);
+    for (int i = 0; i < 4; ++i) ps[i] = k == 0 ? p[i] + p[i + 4] : ps[i] + (p[i] + p[i + 4]);
+    pf[k] = make_uint4(pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3]), pack_bf16x2(p[4], p[5]), pack_bf16x2(p[6], p[7]));
+  };
+  float mx[4];
+#pragma unroll
+  for (int k = 0; k < 2 * KB; ++k) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float x = s[k / 2][8 * (k % 2) + 2 * i], y = s[k / 2][8 * (k % 2) + 2 * i + 1];
+      mx[i] = k == 0 ? vmax(x, y) : vmax3(mx[i], x, y);
+    }
+    probabilities(st.m == -INFINITY ? 0.f : st.m, k);
+    between(k);
+  }
+  const float top = half_max(vmax3(vmax(mx[0], mx[1]), mx[2], mx[3])) * c;
+  if (__any(top > st.m + 8.f)) {
+    const float mn = fmaxf(st.m, top), alpha = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(st.m - mn);
     st.m = mn;
     st.l *= alpha;
 #pragma unroll
     for (int b = 0; b < D / 32; ++b)
 #pragma unroll
       for (int i = 0; i < 16; ++i) st.o[b][i] *= alpha;
+#pragma unroll
+    for (int k = 0; k < 2 * KB; ++k) probabilities(mn == -INFINITY ? 0.f : mn, k);
   }
-  const float mz = st.m == -INFINITY ? 0.f : st.m;
-  float ps = 0.f;
-#pragma unroll
-  for (int b = 0; b < KB; ++b) {
-    float p[16];
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      p[i] = __builtin_amdgcn_exp2f(fmaf(s[b][i], c, -mz));
-      ps += p[i];
-    }
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-      pf[2 * b + h] = make_uint4(pack_bf16x2(p[8 * h], p[8 * h + 1]), pack_bf16x2(p[8 * h + 2], p[8 * h + 3]),
-                                 pack_bf16x2(p[8 * h + 4], p[8 * h + 5]), pack_bf16x2(p[8 * h + 6], p[8 * h + 7]));
-  }
-  st.l += ps;
+  st.l += (ps[0] + ps[1]) + (ps[2] + ps[3]);
 }
 
 // O^T += V^T P^T of a tile, its values in LDS at vt.
@@ -213,7 +219,7 @@ __device__ __forceinline__ void add_tile(const char* kt, const char* vt, const u
   f32x16 s[KB];
   uint4 pf[2 * KB];
   tile_scores<D, KB>(kt, qf, lane, s);
-  tile_softmax<D, KB>(s, c, lim, masked, lane >> 5, st, pf);
+  tile_softmax<D, KB>(s, c, lim, masked, lane >> 5, st, pf, [](int) {});
   tile_values<D, KB>(vt, pf, lane, st);
 }
 
@@ -264,7 +270,7 @@ __device__ __forceinline__ void clear_state(PromptState<D>& st) {
   st.l = 0.f;
 }
 
-// A wave's 32 rows r0 .. of (sequence s, key head hk), one per lane column.
+// A wave's 32 rows r0 .. of (sequence s, key head hk), one per lane column; past the last row, that row again, not valid.
 struct PromptRows {
   int64_t row;  // row of q, out and lse
   int h, lim;   // query head; last key seen
@@ -308,17 +314,18 @@ __device__ __forceinline__ uint32_t lds_address(const void* p) {
   return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)p;
 }
 
-// The eight waves, two per SIMD, work in turns: while waves 0-3 run matrix instructions (the scores of tile j + 1, then the
-// values of tile j), waves 4-7 run the softmax of tile j on the vector units, and the other way round, a barrier between the
-// turns.  Turn 2 j + 1 is matrix instructions of tile j for waves 0-3, turn 2 j + 2 for waves 4-7.  In turn 2 j + 1 all waves
-// send for V(j + 1) and K(j + 3), over V(j - 1) and K(j), last read in turn 2 j; both have landed at the end of turn 2 j + 2.
-// V(j + 1) is first read in turn 2 j + 3, and K(j + 3) at the end of turn 2 j + 4: a wave reads the first keys of its products
-// before the barrier.
+// The eight waves, two per SIMD, work in turns, a barrier between the turns: while waves 0-3 run matrix instructions (the scores
+// of tile j + 1, then the values of tile j), waves 4-7 run the softmax of tile j on the vector units, and the other way round.
+// Waves 0-3 run softmax j in turn 2 j and the products in turn 2 j + 1, waves 4-7 one turn later.  V(j) is read in turns 2 j + 1
+// and 2 j + 2, K(j) in turns 2 j - 1 and 2 j (its first pieces one turn before that, ahead of the barrier).
+// Loads go out during a wave's softmax: V(j + 1) and K(j + 3) for waves 0-3 (turn 2 j), V(j + 2) and K(j + 4) for waves 4-7 (turn
+// 2 j + 1), over V(j - 2), K(j - 1), V(j - 1) and K(j) of three and four buffers; a wave waits for its own before it sends for the
+// next two turns later, and the barrier of that turn makes them known to all: V(j + 1) after turn 2 j + 2, K(j + 3) likewise.
 template <int D>
 __global__ __launch_bounds__(512, 2) void k_prompt_tiles(PromptArgs a) {
   constexpr int NW = 8, RB = 2 * D, TILE = PT_KEYS * RB, RPI = 1024 / RB, NI = PT_KEYS / RPI / NW;  // rows and loads per wave's load
   constexpr int KS = D / 16, NV = D / 32, KAHEAD = 8;
-  __shared__ __align__(1024) char kt[3 * TILE], vt[2 * TILE];
+  __shared__ __align__(1024) char kt[4 * TILE], vt[3 * TILE];
   __shared__ int again, first_bad[3 * D];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
   const bool second = w >= NW / 2;
@@ -327,8 +334,6 @@ __global__ __launch_bounds__(512, 2) void k_prompt_tiles(PromptArgs a) {
   const int nk = a.nk[s], rows = a.nq[s] * a.G, tiles = (rows + NW * 32 - 1) / (NW * 32);
   const int hk = in_seq % Hk, r0 = (tiles - 1 - in_seq / Hk) * NW * 32;  // the rows with the most keys first
   const PromptRows pr(a, s, hk, r0 + 32 * w, lane);
-  uint4 qf[KS];
-  load_queries<D>(a, pr.row * a.q_row + pr.h * a.q_head, pr.valid, half, qf);
   const int off = nk - a.nq[s], n_tiles = max(0, (off + (min(r0 + NW * 32, rows) - 1) / a.G + PT_KEYS) / PT_KEYS);
   if (threadIdx.x == 0) again = 0;
 
@@ -339,21 +344,31 @@ __global__ __launch_bounds__(512, 2) void k_prompt_tiles(PromptArgs a) {
   // the lane's piece of a load, the same in all of a wave's loads
   const uint32_t kp = 16 * (lp ^ k_turn<D>(w * RPI + lr)), vp = 16 * (lp ^ v_turn<D>(w * RPI + lr));
   const uint32_t kat = (uint32_t)lr * (uint32_t)a.k_row * 2 + kp, vat = (uint32_t)lr * (uint32_t)a.v_row * 2 + vp;
-  auto issue = [&](int j, uint32_t t, const uint16_t* base, int64_t stride, uint32_t at, uint32_t piece) {
-    if (j >= n_tiles) return;
-#pragma unroll
-    for (int n = 0; n < NI; ++n) {
-      const int i = w + NW * n, r = j * PT_KEYS + i * RPI;
-      if (r + RPI <= nk) {
-        dma16(base + r * stride, at, t + i * 1024);
-      } else {  // past the last key: that key again
-        const int r1 = min(r, nk - 1);
-        dma16(base + r1 * stride, (uint32_t)min(lr, nk - 1 - r1) * (uint32_t)stride * 2 + piece, t + i * 1024);
-      }
+  auto load = [&](int j, int n, uint32_t t, const uint16_t* base, int64_t stride, uint32_t at, uint32_t piece) {
+    const int i = w + NW * n, r = j * PT_KEYS + i * RPI;
+    if (r + RPI <= nk) {
+      dma16(base + r * stride, at, t + i * 1024);
+    } else {  // past the last key: that key again
+      const int r1 = min(r, nk - 1);
+      dma16(base + r1 * stride, (uint32_t)min(lr, nk - 1 - r1) * (uint32_t)stride * 2 + piece, t + i * 1024);
     }
   };
-  auto issue_k = [&](int j, int buf) { issue(j, kl + buf * TILE, kbase, a.k_row, kat, kp); };
-  auto issue_v = [&](int j, int buf) { issue(j, vl + buf * TILE, vbase, a.v_row, vat, vp); };
+  auto load_keys = [&](int j, int n) { load(j, n, kl + (j & 3) * TILE, kbase, a.k_row, kat, kp); };
+  auto load_vals = [&](int j, int n, int buf) { load(j, n, vl + buf * TILE, vbase, a.v_row, vat, vp); };
+  auto load_tile = [&](int jk, int jv, int buf) {  // all of a wave's loads of K(jk) and V(jv)
+#pragma unroll
+    for (int n = 0; n < NI; ++n) {
+      if (jk < n_tiles) load_keys(jk, n);
+      if (jv < n_tiles) load_vals(jv, n, buf);
+    }
+  };
+
+  load_tile(0, 0, 0);
+  load_tile(1, second ? 1 : n_tiles, 1);
+  load_tile(2, n_tiles, 0);
+  if (second) load_tile(3, n_tiles, 0);
+  uint4 qf[KS];
+  load_queries<D>(a, pr.row * a.q_row + pr.h * a.q_head, half, qf);
 
   // the lane's pieces of K (A operand of the scores, see tile_scores) and V (of the values, see tile_values) in a tile
   const int krow = lane & 31;
@@ -363,9 +378,9 @@ __global__ __launch_bounds__(512, 2) void k_prompt_tiles(PromptArgs a) {
 #pragma unroll
   for (int b = 0; b < NV; ++b) vread[b] = vr * RB + 16 * ((4 * b + vc) ^ v_turn<D>(vr)) + 8 * (lane & 1);
 
+  f32x16 sc[2];
   PromptState<D> st;
   clear_state(st);
-  f32x16 sc[2];
   uint4 kf[2 * KS], pf[4], vf[4][NV];
   auto load_k = [&](int i, uint32_t t) {  // the tile's two blocks of keys in turn
     kf[i] = *reinterpret_cast<const uint4*>(kt + ((t + kread) ^ (32 * (i >> 1))) + (i & 1) * 32 * RB);
@@ -393,10 +408,6 @@ __global__ __launch_bounds__(512, 2) void k_prompt_tiles(PromptArgs a) {
     }
   };
 
-  issue_k(0, 0);
-  issue_v(0, 0);
-  issue_k(1, 1);
-  issue_k(2, 2);
   vm_wait_all();
   __syncthreads();
   if (n_tiles > 0) {
@@ -408,27 +419,26 @@ __global__ __launch_bounds__(512, 2) void k_prompt_tiles(PromptArgs a) {
   }
   meet();
   if (second) meet();
-  int kb = 1;  // buffer of K(j + 1)
+  const int jv = second ? 2 : 1, jk = second ? 4 : 3;  // tiles ahead
+  int vb = 0, vn = second ? 2 : 1;                     // buffers of V(j) and V(j + jv)
   for (int j = 0; j < n_tiles; ++j) {
     const int k0 = j * PT_KEYS;
-    const uint32_t tk = kb * TILE, tv = (j & 1) * TILE;
-    const int kfree = kb == 0 ? 2 : kb - 1;  // that of K(j), which K(j + 3) takes
-    if (second) {
-      issue_v(j + 1, (j + 1) & 1);
-      issue_k(j + 3, kfree);
-    }
-    tile_softmax<D, 2>(sc, a.c, pr.lim - k0, k0 + PT_KEYS - 1 > pr.first, half, st, pf);
+    const uint32_t tk = ((j + 1) & 3) * TILE, tv = vb * TILE;
+    vm_wait_all();
+    tile_softmax<D, 2>(sc, a.c, pr.lim - k0, k0 + PT_KEYS - 1 > pr.first, half, st, pf, [&](int k) {
+      if (k >= 2 * NI) return;
+      if (k & 1) {
+        if (j + jk < n_tiles) load_keys(j + jk, k >> 1);
+      } else {
+        if (j + jv < n_tiles) load_vals(j + jv, k >> 1, vn);
+      }
+    });
 #pragma unroll
     for (int k = 0; k < 4; ++k) here(pf[k]);
     asm volatile("" : "+v"(st.l));
 #pragma unroll
     for (int i = 0; i < KAHEAD; ++i) load_k(i, tk);
-    if (!second) vm_wait_all();
     meet();
-    if (!second) {
-      issue_v(j + 1, (j + 1) & 1);
-      issue_k(j + 3, kfree);
-    }
     __builtin_amdgcn_s_setprio(1);
     scores(tk, true, tv);
     here(sc[0]);
@@ -446,9 +456,9 @@ __global__ __launch_bounds__(512, 2) void k_prompt_tiles(PromptArgs a) {
 #pragma unroll
     for (int b = 0; b < NV; ++b) here(st.o[b]);
     __builtin_amdgcn_s_setprio(0);
-    if (second) vm_wait_all();
     meet();
-    kb = kb == 2 ? 0 : kb + 1;
+    vb = vb == 2 ? 0 : vb + 1;
+    vn = vn == 2 ? 0 : vn + 1;
   }
   if (!second) meet();
   if (!__all(all_finite(st))) again = 1;
@@ -459,8 +469,11 @@ __global__ __launch_bounds__(512, 2) void k_prompt_tiles(PromptArgs a) {
     for (int j = 0; j < n_tiles; ++j) {
       const int k0 = j * PT_KEYS;
       __syncthreads();
-      issue_k(j, 0);
-      issue_v(j, 0);
+#pragma unroll
+      for (int n = 0; n < NI; ++n) {
+        load(j, n, kl, kbase, a.k_row, kat, kp);
+        load_vals(j, n, 0);
+      }
       vm_wait_all();
       __syncthreads();
       if (k0 + PT_KEYS - 1 > off + r0 / a.G) take_out_nonfinite<D>(vt, PT_KEYS, nk - k0, k0, first_bad, threadIdx.x, NW * 64);
@@ -505,7 +518,7 @@ __global__ __launch_bounds__(PS_WAVES * 64, 1) void k_prompt_split(PromptArgs a)
   const int n_tiles = max(0, (pr.last + PS_KEYS) / PS_KEYS), t0 = split * a.chunk, t1 = min(t0 + a.chunk, n_tiles);
   if (split > 0 && t0 >= t1) return;  // the merge takes as many chunks as these rows have
   uint4 qf[D / 16];
-  load_queries<D>(a, pr.row * a.q_row + pr.h * a.q_head, pr.valid, half, qf);
+  load_queries<D>(a, pr.row * a.q_row + pr.h * a.q_head, half, qf);
 
   const int lr = lane / (RB / 16), lp = lane % (RB / 16);
   const uint16_t* kbase = a.k + a.k0[s] * a.k_row + hk * a.k_head;
