@@ -255,6 +255,8 @@ struct RowsArgs {
   int64_t src[FSX_MAX_BATCH], slot[FSX_MAX_BATCH];
   int32_t n[FSX_MAX_BATCH];
   int64_t prefix[FSX_MAX_BATCH + 1];  // rows of the agents before
+  int32_t block;                      // rows of a workgroup, and workgroups of the agents before
+  int32_t block_prefix[FSX_MAX_BATCH + 1];
 };
 hipError_t launch_replace_rows(const RowsArgs& a, hipStream_t s);
 hipError_t launch_read_rows(const RowsArgs& a, hipStream_t s);
