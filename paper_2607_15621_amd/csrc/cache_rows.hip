@@ -30,17 +30,33 @@ __device__ __forceinline__ void store_raw(void* base, int64_t at, const Raw16<DT
   for (int i = 0; i < Raw16<DT>::N; ++i) reinterpret_cast<uint4*>((char*)base + at * ES)[i] = r.p[i];
 }
 
-// Codes of x / scale, four to a word, as e4m3_encode gives them.  The instruction rounds to nearest even; of a NaN it drops the
-// sign, which is put back.
-__device__ __forceinline__ uint32_t encode4(float a, float b, float c, float d, float scale) {
-  const float y[4] = {a / scale, b / scale, c / scale, d / scale};
+// A scale and its reciprocal.  With r the correctly rounded 1 / s, q = x r and e = x - q s (exact in an fma), q + e r is the
+// correctly rounded x / s (Markstein, 1990), where nothing underflows: s >= 2^-60 makes sure of that for every quotient that is
+// not far below half the smallest code.  Six instructions where the division takes eleven: the 16 agents' rows were bound by
+// those.
+struct Scale {
+  float s, r;
+  bool tiny;
+  __device__ __forceinline__ explicit Scale(float scale) : s(scale), r(1.0f / scale), tiny(scale < 0x1p-60f) {}
+  __device__ __forceinline__ float quotient(float x) const {
+    if (tiny) return x / s;
+    const float q = __builtin_amdgcn_fmed3f(x * r, -512.0f, 512.0f);  // no element is larger, but for infinities
+    return __builtin_copysignf(fmaf(fmaf(-q, s, x), r, q), x);  // (a zero's sign is lost in the sum)
+  }
+};
+
+// Codes of four elements by the scale, as e4m3_encode gives them.  The instruction rounds to nearest even; of a NaN it drops
+// the sign, which is put back.
+__device__ __forceinline__ uint32_t encode4(float a, float b, float c, float d, const Scale& scale) {
+  const float y[4] = {scale.quotient(a), scale.quotient(b), scale.quotient(c), scale.quotient(d)};
   auto clamp = [](float v) { return __builtin_amdgcn_fmed3f(v, -448.0f, 448.0f); };
   uint32_t w = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(clamp(y[0]), clamp(y[1]), 0, false);
   w = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(clamp(y[2]), clamp(y[3]), (int)w, true);
   if (__builtin_isunordered(y[0], y[1]) || __builtin_isunordered(y[2], y[3])) {
+    const float x[4] = {a, b, c, d};
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      if (y[i] != y[i]) w = (w & ~(0xFFu << 8 * i)) | (0x7Fu | __float_as_uint(y[i]) >> 31 << 7) << 8 * i;
+      if (y[i] != y[i]) w = (w & ~(0xFFu << 8 * i)) | (0x7Fu | __float_as_uint(x[i]) >> 31 << 7) << 8 * i;
   }
   return w;
 }
@@ -68,7 +84,7 @@ __device__ __forceinline__ void to_floats(const Raw16<DT>& r, float (&x)[16]) {
   }
 }
 template <int DT>
-__device__ __forceinline__ Raw16<DT> from_floats(const float (&x)[16], float scale) {
+__device__ __forceinline__ Raw16<DT> from_floats(const float (&x)[16], const Scale& scale) {
   Raw16<DT> r;
 #pragma unroll
   for (int i = 0; i < Raw16<DT>::N; ++i) {
@@ -94,7 +110,7 @@ __device__ __forceinline__ Raw16<TO> convert(const Raw16<FROM>& r, float scale) 
     if constexpr (FROM == FSX_FP8_E4M3)
 #pragma unroll
       for (int i = 0; i < 16; ++i) x[i] *= scale;
-    return from_floats<TO>(x, scale);
+    return from_floats<TO>(x, Scale(scale));
   }
 }
 
@@ -173,62 +189,92 @@ __global__ __launch_bounds__(256) void k_convert_rows(RowsArgs a) {
 }
 
 // ---------------------------------------------------------------------------------------------------------------
-// An fp8 cache's rows that fit the registers of a workgroup: one workgroup per (head, keys or values, layer, agent) holds its
-// rows while it finds their largest magnitude, so they are read once.  Thread t keeps the 16-byte pieces t, t + T, ..
+// An fp8 cache's rows that fit the registers of a workgroup: for one (agent, layer, keys or values, head) after the other it
+// holds the rows while it finds their largest magnitude, so they are read once, and as each piece is encoded the next rows'
+// piece is sent for in its place.  Thread t keeps pieces t, t + T, .. of 16 bytes.
 template <int DT, int T, int U>
 __global__ __launch_bounds__(T) void k_replace_held(RowsArgs a) {
   constexpr int ES = DT == FSX_F32 ? 4 : 2, E = 16 / ES;  // elements of a piece
-  __shared__ float red[T / 64];
+  __shared__ float red[2][T / 64];
   const CacheView& cv = a.cv;
-  const int h = blockIdx.x >> 1, kv = blockIdx.x & 1, l = blockIdx.y, b = blockIdx.z, n = a.n[b];
-  if (n == 0) return;
   const int cpr = cv.Dh / E, step = T / cpr;  // pieces of a row; rows apart
   const int c = threadIdx.x % cpr, r0 = threadIdx.x / cpr;
-  const char* src = (const char*)(kv ? a.v : a.k) + ((((int64_t)l * a.total + a.src[b]) * cv.H + h) * cv.Dh + E * c) * ES;
-  const int64_t stride = (int64_t)cv.H * cv.Dh * ES;
+  const uint32_t stride = (uint32_t)(cv.H * cv.Dh * ES);
+  const int total = 2 * cv.H * a.layers * a.B;
+  struct Item {
+    int h, kv, l, b, n;
+  };
+  auto item = [&](int i) {
+    Item x;
+    x.h = i % cv.H;
+    i /= cv.H;
+    x.kv = i & 1;
+    i >>= 1;
+    x.l = i % a.layers;
+    x.b = i / a.layers;
+    x.n = a.n[x.b];
+    return x;
+  };
+  auto next_of = [&](int i) {  // the next one that has rows
+    for (i += gridDim.x; i < total && a.n[i / (2 * cv.H * a.layers)] == 0;) i += gridDim.x;
+    return i;
+  };
   uint4 x[U];
+  auto load = [&](const Item& it, int u) {  // past the last row: that row again
+    const char* src = (const char*)(it.kv ? a.v : a.k) + (((int64_t)it.l * a.total + a.src[it.b]) * cv.H + it.h) * cv.Dh * ES;
+    x[u] = *reinterpret_cast<const uint4*>(src + ((uint32_t)min(r0 + step * u, it.n - 1) * stride + 16 * c));
+  };
+  int i = next_of((int)blockIdx.x - (int)gridDim.x);
+  if (i >= total) return;
+  Item it = item(i);
 #pragma unroll
-  for (int u = 0; u < U; ++u) {
-    const int r = r0 + step * u;
-    x[u] = make_uint4(0, 0, 0, 0);
-    if (r0 < step && r < n) x[u] = *reinterpret_cast<const uint4*>(src + r * stride);
-  }
-  float top = 0.f;
+  for (int u = 0; u < U; ++u) load(it, u);
+  for (int turn = 0;; turn ^= 1) {
+    float top = 0.f;
 #pragma unroll
-  for (int u = 0; u < U; ++u) top = piece_top<DT>(top, x[u]);
-  top = rows_max(top);  // over lanes 16 apart, then over the 16
+    for (int u = 0; u < U; ++u) top = piece_top<DT>(top, x[u]);
+    top = rows_max(top);  // over lanes 16 apart, then over the 16
 #pragma unroll
-  for (int s = 0; s < 4; ++s) {
-    const int t = __builtin_bit_cast(int, top);
-    const int o = s == 0 ? __builtin_amdgcn_update_dpp(0, t, 0x128, 0xF, 0xF, false)
-                         : (s == 1 ? __builtin_amdgcn_update_dpp(0, t, 0x124, 0xF, 0xF, false)
-                                   : (s == 2 ? __builtin_amdgcn_update_dpp(0, t, 0x122, 0xF, 0xF, false)
-                                             : __builtin_amdgcn_update_dpp(0, t, 0x121, 0xF, 0xF, false)));
-    top = fmaxf(top, __builtin_bit_cast(float, o));
-  }
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = top;
-  __syncthreads();
-#pragma unroll
-  for (int i = 0; i < T / 64; ++i) top = fmaxf(top, red[i]);
-  const float sc = scale_of(top, a.headroom);
-  if (threadIdx.x == 0) const_cast<float*>(kv ? cv.v_scale : cv.k_scale)[cache_scale_index(cv, b, cv.layer + l, h)] = sc;
-  uint8_t* dst = (uint8_t*)const_cast<void*>(kv ? cv.v : cv.k) + cache_head_base(cv, b, cv.layer + l, h) + E * c;
-#pragma unroll
-  for (int u = 0; u < U; ++u) {
-    const int r = r0 + step * u;
-    if (r0 >= step || r >= n) continue;
-    const uint32_t w[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
-    if constexpr (DT == FSX_F32) {
-      *reinterpret_cast<uint32_t*>(dst + r * cv.rs) =
-          encode4(__uint_as_float(w[0]), __uint_as_float(w[1]), __uint_as_float(w[2]), __uint_as_float(w[3]), sc);
-    } else {
-      uint32_t o[2];
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-        o[i] = encode4(__uint_as_float(w[2 * i] << 16), __uint_as_float(w[2 * i] & 0xFFFF0000u), __uint_as_float(w[2 * i + 1] << 16),
-                       __uint_as_float(w[2 * i + 1] & 0xFFFF0000u), sc);
-      *reinterpret_cast<uint2*>(dst + r * cv.rs) = make_uint2(o[0], o[1]);
+    for (int s = 0; s < 4; ++s) {
+      const int t = __builtin_bit_cast(int, top);
+      const int o = s == 0 ? __builtin_amdgcn_update_dpp(0, t, 0x128, 0xF, 0xF, false)
+                           : (s == 1 ? __builtin_amdgcn_update_dpp(0, t, 0x124, 0xF, 0xF, false)
+                                     : (s == 2 ? __builtin_amdgcn_update_dpp(0, t, 0x122, 0xF, 0xF, false)
+                                               : __builtin_amdgcn_update_dpp(0, t, 0x121, 0xF, 0xF, false)));
+      top = fmaxf(top, __builtin_bit_cast(float, o));
     }
+    if ((threadIdx.x & 63) == 0) red[turn][threadIdx.x >> 6] = top;
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < T / 64; ++j) top = fmaxf(top, red[turn][j]);
+    const Scale sc(scale_of(top, a.headroom));
+    if (threadIdx.x == 0) const_cast<float*>(it.kv ? cv.v_scale : cv.k_scale)[cache_scale_index(cv, it.b, cv.layer + it.l, it.h)] = sc.s;
+    uint8_t* dst = (uint8_t*)const_cast<void*>(it.kv ? cv.v : cv.k) + cache_head_base(cv, it.b, cv.layer + it.l, it.h);
+    const int j = next_of(i);
+    const bool more = j < total;
+    const Item nx = item(more ? j : i);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int r = r0 + step * u;
+      const uint32_t w[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
+      uint32_t o[2];
+      if constexpr (DT == FSX_F32) {
+        o[0] = encode4(__uint_as_float(w[0]), __uint_as_float(w[1]), __uint_as_float(w[2]), __uint_as_float(w[3]), sc);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+          o[e] = encode4(__uint_as_float(w[2 * e] << 16), __uint_as_float(w[2 * e] & 0xFFFF0000u), __uint_as_float(w[2 * e + 1] << 16),
+                         __uint_as_float(w[2 * e + 1] & 0xFFFF0000u), sc);
+      }
+      if (more) load(nx, u);
+      if (r0 < step && r < it.n) {
+        if constexpr (DT == FSX_F32) *reinterpret_cast<uint32_t*>(dst + (int64_t)r * cv.rs + E * c) = o[0];
+        else *reinterpret_cast<uint2*>(dst + (int64_t)r * cv.rs + E * c) = make_uint2(o[0], o[1]);
+      }
+    }
+    if (!more) break;
+    i = j;
+    it = nx;
   }
 }
 
@@ -297,22 +343,16 @@ template <int DT>
 static hipError_t launch_replace(const RowsArgs& a, hipStream_t s) {
   if (a.cv.dtype == FSX_FP8_E4M3) {
     const int n = *std::max_element(a.n, a.n + a.B);
-    const int64_t pieces = (int64_t)n * a.cv.Dh * (DT == FSX_F32 ? 4 : 2) / 16;
     const int cpr = a.cv.Dh * (DT == FSX_F32 ? 4 : 2) / 16;
-    auto fits = [&](int T, int U) { return cpr <= T && (int64_t)n <= (int64_t)(T / cpr) * U; };
-    const dim3 grid(2 * a.cv.H, a.layers, a.B);
-    if (fits(256, 4)) {
-      hipLaunchKernelGGL((k_replace_held<DT, 256, 4>), grid, dim3(256), 0, s, a);
+    auto held = [&](auto fn, int T, int U, int per_cu) {
+      if (cpr > T || (int64_t)n > (int64_t)(T / cpr) * U || (int64_t)n * a.cv.H * a.cv.Dh * 4 > INT32_MAX) return false;
+      const int64_t items = (int64_t)2 * a.cv.H * a.layers * a.B;
+      hipLaunchKernelGGL(fn, dim3((unsigned)std::min<int64_t>(items, 256 * per_cu)), dim3(T), 0, s, a);
+      return true;
+    };
+    if (held(k_replace_held<DT, 256, 4>, 256, 4, 6) || held(k_replace_held<DT, 512, 8>, 512, 8, 2) ||
+        held(k_replace_held<DT, 1024, 16>, 1024, 16, 1))
       return hipGetLastError();
-    }
-    if (fits(512, 8)) {
-      hipLaunchKernelGGL((k_replace_held<DT, 512, 8>), grid, dim3(512), 0, s, a);
-      return hipGetLastError();
-    }
-    if (fits(1024, 16)) {
-      hipLaunchKernelGGL((k_replace_held<DT, 1024, 16>), grid, dim3(1024), 0, s, a);
-      return hipGetLastError();
-    }
     hipLaunchKernelGGL(k_clear_scales, dim3((2 * a.cv.H + 255) / 256, a.layers, a.B), dim3(256), 0, s, a);
     RowsArgs t = a;
     const int groups = (a.cv.H * cpr + 255) / 256;

@@ -165,6 +165,28 @@ def test_every_finite_bf16_value_is_encoded_as_the_format_says():
     replace_and_check(r, (256,), [v, -v])
 
 
+@pytest.mark.parametrize("top", [448.0, 1.0, 3.7e-5, 911.3, 2.3e-16, 5.1e-18, 1.7e-37, 3.1e38])
+def test_quotients_next_to_a_border_of_two_codes(top):
+    """Elements at the middle of two codes' values and a step of fp32 to either side, for scales that are not powers of two (and,
+    by `top`, tiny and huge ones)."""
+    codes = torch.arange(0, 0x7F, dtype=torch.uint8).view(FP8).double()
+    middle = (codes[:-1] + codes[1:]) / 2
+    r = Rings([0], 64, L=1, H=16)
+    v = torch.zeros(1, 64, 16, 128)
+    g = torch.Generator().manual_seed(3)
+    for h in range(16):
+        head = top * (0.5 + 0.5 * float(torch.rand((), generator=g)))
+        v[0, 0, h, 0] = head
+        scale = scale_of(v[0, :1], 1.0)[h].double()
+        x = (middle * scale).float()
+        up, down = (torch.nextafter(x, torch.full_like(x, s)) for s in (float("inf"), 0.0))
+        rows = torch.cat([x, up, down, -x, -up, -down])
+        flat = torch.zeros(63 * 128)
+        flat[:len(rows)] = rows.clamp(-head, head)
+        v[0, 1:, h] = flat.view(63, 128)
+    replace_and_check(r, (64,), [v, -v])
+
+
 @pytest.mark.parametrize("shape", [(1, 1, 1), (1, 2, 3), (3, 1, 40), (16, 1, 5)])
 def test_another_stream_and_again(shape):
     B, L, H = shape
