@@ -3,6 +3,7 @@
 // pass of their own before the codes.
 
 #include <algorithm>
+#include <type_traits>
 
 #include "common.h"
 #include "kernels.h"
@@ -30,33 +31,38 @@ __device__ __forceinline__ void store_raw(void* base, int64_t at, const Raw16<DT
   for (int i = 0; i < Raw16<DT>::N; ++i) reinterpret_cast<uint4*>((char*)base + at * ES)[i] = r.p[i];
 }
 
-// A scale and its reciprocal.  With r the correctly rounded 1 / s, q = x r and e = x - q s (exact in an fma), q + e r is the
+// A scale and its reciprocal.  With r the correctly rounded 1 / s, q = x r and e = q s - x (exact in an fma), q - e r is the
 // correctly rounded x / s (Markstein, 1990), where nothing underflows: s >= 2^-60 makes sure of that for every quotient that is
-// not far below half the smallest code.  Six instructions where the division takes eleven: the 16 agents' rows were bound by
-// those.
+// not far below half the smallest code.  (Of a zero, this order of signs keeps its own.)  Three instructions where the division
+// takes eleven: the 16 agents' rows were bound by those.
 struct Scale {
   float s, r;
   bool tiny;
   __device__ __forceinline__ explicit Scale(float scale) : s(scale), r(1.0f / scale), tiny(scale < 0x1p-60f) {}
-  __device__ __forceinline__ float quotient(float x) const {
-    if (tiny) return x / s;
-    const float q = __builtin_amdgcn_fmed3f(x * r, -512.0f, 512.0f);  // no element is larger, but for infinities
-    return __builtin_copysignf(fmaf(fmaf(-q, s, x), r, q), x);  // (a zero's sign is lost in the sum)
-  }
 };
 
-// Codes of four elements by the scale, as e4m3_encode gives them.  The instruction rounds to nearest even; of a NaN it drops
-// the sign, which is put back.
+// Codes of four elements by the scale, as e4m3_encode gives them; the instruction rounds to nearest even.
+// ORDINARY: the scale is not tiny and the elements are finite, so that none is more than a rounding above 448 scales, which
+// needs no clamp.  Otherwise step by step; of a NaN the instruction drops the sign, which is put back.
+template <bool ORDINARY>
 __device__ __forceinline__ uint32_t encode4(float a, float b, float c, float d, const Scale& scale) {
-  const float y[4] = {scale.quotient(a), scale.quotient(b), scale.quotient(c), scale.quotient(d)};
-  auto clamp = [](float v) { return __builtin_amdgcn_fmed3f(v, -448.0f, 448.0f); };
-  uint32_t w = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(clamp(y[0]), clamp(y[1]), 0, false);
-  w = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(clamp(y[2]), clamp(y[3]), (int)w, true);
-  if (__builtin_isunordered(y[0], y[1]) || __builtin_isunordered(y[2], y[3])) {
-    const float x[4] = {a, b, c, d};
+  const float x[4] = {a, b, c, d};
+  float y[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (ORDINARY) {
+      const float q = x[i] * scale.r, e = fmaf(q, scale.s, -x[i]);
+      y[i] = fmaf(-e, scale.r, q);
+    } else {
+      y[i] = __builtin_amdgcn_fmed3f(x[i] / scale.s, -448.0f, 448.0f);
+    }
+  }
+  uint32_t w = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
+  w = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], (int)w, true);
+  if (!ORDINARY) {
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      if (y[i] != y[i]) w = (w & ~(0xFFu << 8 * i)) | (0x7Fu | __float_as_uint(x[i]) >> 31 << 7) << 8 * i;
+      if (x[i] != x[i]) w = (w & ~(0xFFu << 8 * i)) | (0x7Fu | __float_as_uint(x[i]) >> 31 << 7) << 8 * i;
   }
   return w;
 }
@@ -83,7 +89,7 @@ __device__ __forceinline__ void to_floats(const Raw16<DT>& r, float (&x)[16]) {
     }
   }
 }
-template <int DT>
+template <int DT, bool ORDINARY = false>
 __device__ __forceinline__ Raw16<DT> from_floats(const float (&x)[16], const Scale& scale) {
   Raw16<DT> r;
 #pragma unroll
@@ -93,12 +99,47 @@ __device__ __forceinline__ Raw16<DT> from_floats(const float (&x)[16], const Sca
     for (int j = 0; j < 4; ++j) {
       if constexpr (DT == FSX_F32) w[j] = __float_as_uint(x[4 * i + j]);
       else if constexpr (DT == FSX_BF16) w[j] = pack_bf16x2(x[8 * i + 2 * j], x[8 * i + 2 * j + 1]);
-      else w[j] = encode4(x[4 * j], x[4 * j + 1], x[4 * j + 2], x[4 * j + 3], scale);
+      else w[j] = encode4<ORDINARY>(x[4 * j], x[4 * j + 1], x[4 * j + 2], x[4 * j + 3], scale);
     }
     r.p[i] = make_uint4(w[0], w[1], w[2], w[3]);
   }
   return r;
 }
+
+// Scale of the largest finite magnitude `top`.
+__device__ __forceinline__ float scale_of(float top, float headroom) {
+  return top > 0.f ? fmaxf(top / 448.f * headroom, 0x1p-126f) : 1.f;
+}
+
+// Largest magnitude of pieces: fp32, or two bf16 halves side by side, as bits, which positive values compare by.  Pieces are
+// folded whatever they hold; where the result is not finite, they are folded again without what is not.
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+template <int DT>
+__device__ __forceinline__ uint32_t fold_top(uint32_t top, uint4 p, bool finite_only) {
+  const uint32_t w[4] = {p.x, p.y, p.z, p.w};
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    if constexpr (DT == FSX_F32) {
+      uint32_t v = w[j] & 0x7FFFFFFFu;
+      if (finite_only && v >= 0x7F800000u) v = 0;
+      top = max(top, v);
+    } else {
+      u16x2 v = __builtin_bit_cast(u16x2, w[j] & 0x7FFF7FFFu);
+      if (finite_only) {
+        if (v.x >= 0x7F80) v.x = 0;
+        if (v.y >= 0x7F80) v.y = 0;
+      }
+      top = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, top), v));
+    }
+  }
+  return top;
+}
+template <int DT>
+__device__ __forceinline__ float top_value(uint32_t top) {
+  return DT == FSX_F32 ? __uint_as_float(top) : __uint_as_float(max(top << 16, top & 0xFFFF0000u));
+}
+
 // The same elements in another type (a bit copy where the types are the same): cached values times scale, or into a cache by it.
 template <int FROM, int TO>
 __device__ __forceinline__ Raw16<TO> convert(const Raw16<FROM>& r, float scale) {
@@ -107,34 +148,18 @@ __device__ __forceinline__ Raw16<TO> convert(const Raw16<FROM>& r, float scale) 
   } else {
     float x[16];
     to_floats<FROM>(r, x);
-    if constexpr (FROM == FSX_FP8_E4M3)
+    const Scale sc(scale);
+    if constexpr (FROM == FSX_FP8_E4M3) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) x[i] *= scale;
-    return from_floats<TO>(x, Scale(scale));
-  }
-}
-
-// Scale of the largest finite magnitude `top`.
-__device__ __forceinline__ float scale_of(float top, float headroom) {
-  return top > 0.f ? fmaxf(top / 448.f * headroom, 0x1p-126f) : 1.f;
-}
-
-// The larger of `top` and the finite magnitudes of a 16-byte piece.
-template <int DT>
-__device__ __forceinline__ float piece_top(float top, const uint4& p) {
-  const uint32_t w[4] = {p.x, p.y, p.z, p.w};
+    } else if constexpr (TO == FSX_FP8_E4M3) {
+      uint32_t top = 0;
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    if constexpr (DT == FSX_F32) {
-      const float x = __uint_as_float(w[j] & 0x7FFFFFFFu);
-      top = fmaxf(top, x < INFINITY ? x : 0.f);
-    } else {
-      const float x = __uint_as_float((w[j] << 16) & 0x7FFF0000u), y = __uint_as_float(w[j] & 0x7FFF0000u);
-      top = fmaxf(top, x < INFINITY ? x : 0.f);
-      top = fmaxf(top, y < INFINITY ? y : 0.f);
+      for (int i = 0; i < Raw16<FROM>::N; ++i) top = fold_top<FROM>(top, r.p[i], false);
+      if (__all(!sc.tiny && top_value<FROM>(top) < INFINITY)) return from_floats<TO, true>(x, sc);
     }
+    return from_floats<TO>(x, sc);
   }
-  return top;
 }
 
 // ---------------------------------------------------------------------------------------------------------------
@@ -189,6 +214,13 @@ __global__ __launch_bounds__(256) void k_convert_rows(RowsArgs a) {
 }
 
 // ---------------------------------------------------------------------------------------------------------------
+// A buffer at an address that is the same in every lane, which the compiler does not always see.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t uniform_buffer(const void* p, int bytes) {
+  const uint64_t u = (uint64_t)p;
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)u), hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(u >> 32));
+  return __builtin_amdgcn_make_buffer_rsrc((void*)((uint64_t)hi << 32 | lo), 0, __builtin_amdgcn_readfirstlane(bytes), 0x00027000);
+}
+
 // An fp8 cache's rows that fit the registers of a workgroup: for one (agent, layer, keys or values, head) after the other it
 // holds the rows while it finds their largest magnitude, so they are read once, and as each piece is encoded the next rows'
 // piece is sent for in its place.  Thread t keeps pieces t, t + T, .. of 16 bytes.
@@ -198,83 +230,107 @@ __global__ __launch_bounds__(T) void k_replace_held(RowsArgs a) {
   __shared__ float red[2][T / 64];
   const CacheView& cv = a.cv;
   const int cpr = cv.Dh / E, step = T / cpr;  // pieces of a row; rows apart
-  const int c = threadIdx.x % cpr, r0 = threadIdx.x / cpr;
-  const uint32_t stride = (uint32_t)(cv.H * cv.Dh * ES);
   const int total = 2 * cv.H * a.layers * a.B;
+  // Offsets of the thread's first piece from the first row, in the packed rows and in the cache; loads past the last row give
+  // zeros and stores there are dropped (the buffers end with it).
+  const uint32_t c = threadIdx.x % cpr, r0 = threadIdx.x / cpr, none = 0x80000000u;
+  const uint32_t from = r0 < (uint32_t)step ? r0 * (uint32_t)(cv.H * cv.Dh * ES) + 16 * c : none;
+  const uint32_t to = r0 < (uint32_t)step ? r0 * (uint32_t)cv.rs + E * c : none;
+  const uint32_t from_step = (uint32_t)step * (uint32_t)(cv.H * cv.Dh * ES), to_step = (uint32_t)step * (uint32_t)cv.rs;
   struct Item {
     int h, kv, l, b, n;
   };
   auto item = [&](int i) {
-    Item x;
-    x.h = i % cv.H;
-    i /= cv.H;
-    x.kv = i & 1;
-    i >>= 1;
-    x.l = i % a.layers;
-    x.b = i / a.layers;
-    x.n = a.n[x.b];
-    return x;
+    // (the same in every lane, which a division on the vector units hides)
+    const int r = __builtin_amdgcn_readfirstlane(i / cv.H), b = __builtin_amdgcn_readfirstlane((r >> 1) / a.layers);
+    return Item{i - r * cv.H, r & 1, (r >> 1) - b * a.layers, b, a.n[b]};
   };
   auto next_of = [&](int i) {  // the next one that has rows
-    for (i += gridDim.x; i < total && a.n[i / (2 * cv.H * a.layers)] == 0;) i += gridDim.x;
+    for (i += gridDim.x; i < total && a.n[__builtin_amdgcn_readfirstlane(i / (2 * cv.H * a.layers))] == 0;) i += gridDim.x;
     return i;
   };
-  uint4 x[U];
-  auto load = [&](const Item& it, int u) {  // past the last row: that row again
-    const char* src = (const char*)(it.kv ? a.v : a.k) + (((int64_t)it.l * a.total + a.src[it.b]) * cv.H + it.h) * cv.Dh * ES;
-    x[u] = *reinterpret_cast<const uint4*>(src + ((uint32_t)min(r0 + step * u, it.n - 1) * stride + 16 * c));
+  auto source = [&](const Item& it, bool any) {
+    char* p = (char*)(it.kv ? a.v : a.k) + (((int64_t)it.l * a.total + a.src[it.b]) * cv.H + it.h) * cv.Dh * ES;
+    return uniform_buffer(p, any ? ((it.n - 1) * cv.H + 1) * cv.Dh * ES : 0);
   };
+  auto encode = [&](auto ordinary, u32x4_t p, const Scale& sc, __amdgpu_buffer_rsrc_t dst, uint32_t at) {
+    constexpr bool ORD = decltype(ordinary)::value;
+    if constexpr (DT == FSX_F32) {
+      const uint32_t o = encode4<ORD>(__uint_as_float(p.x), __uint_as_float(p.y), __uint_as_float(p.z), __uint_as_float(p.w), sc);
+      __builtin_amdgcn_raw_buffer_store_b32(o, dst, at, 0, 0);
+    } else {
+      const u32x2 o = {encode4<ORD>(__uint_as_float(p.x << 16), __uint_as_float(p.x & 0xFFFF0000u), __uint_as_float(p.y << 16),
+                                    __uint_as_float(p.y & 0xFFFF0000u), sc),
+                       encode4<ORD>(__uint_as_float(p.z << 16), __uint_as_float(p.z & 0xFFFF0000u), __uint_as_float(p.w << 16),
+                                    __uint_as_float(p.w & 0xFFFF0000u), sc)};
+      __builtin_amdgcn_raw_buffer_store_b64(o, dst, at, 0, 0);
+    }
+  };
+  u32x4_t x[U];
   int i = next_of((int)blockIdx.x - (int)gridDim.x);
   if (i >= total) return;
-  Item it = item(i);
-#pragma unroll
-  for (int u = 0; u < U; ++u) load(it, u);
+  bool held = false;
   for (int turn = 0;; turn ^= 1) {
-    float top = 0.f;
+    const Item it = item(i);
+    const auto own = source(it, true);
+    if (!held) {
+      uint32_t f = from;
 #pragma unroll
-    for (int u = 0; u < U; ++u) top = piece_top<DT>(top, x[u]);
+      for (int u = 0; u < U; ++u, f += from_step) x[u] = __builtin_amdgcn_raw_buffer_load_b128(own, f, 0, 0);
+    }
+    uint32_t t = 0;
+#pragma unroll
+    for (int u = 0; u < U; ++u) t = fold_top<DT>(t, make_uint4(x[u].x, x[u].y, x[u].z, x[u].w), false);
+    float top = top_value<DT>(t);
+    // Rows with elements that are not finite (and, below, tiny scales) take their pieces from memory again, in a short loop.
+    const bool finite = top < INFINITY;
+    if (!finite) {
+      t = 0;
+#pragma unroll 1
+      for (uint32_t u = 0, f = from; u < U; ++u, f += from_step) {
+        const u32x4_t p = __builtin_amdgcn_raw_buffer_load_b128(own, f, 0, 0);
+        t = fold_top<DT>(t, make_uint4(p.x, p.y, p.z, p.w), true);
+      }
+      top = top_value<DT>(t);
+    }
     top = rows_max(top);  // over lanes 16 apart, then over the 16
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
-      const int t = __builtin_bit_cast(int, top);
-      const int o = s == 0 ? __builtin_amdgcn_update_dpp(0, t, 0x128, 0xF, 0xF, false)
-                           : (s == 1 ? __builtin_amdgcn_update_dpp(0, t, 0x124, 0xF, 0xF, false)
-                                     : (s == 2 ? __builtin_amdgcn_update_dpp(0, t, 0x122, 0xF, 0xF, false)
-                                               : __builtin_amdgcn_update_dpp(0, t, 0x121, 0xF, 0xF, false)));
+      const int v = __builtin_bit_cast(int, top);
+      const int o = s == 0 ? __builtin_amdgcn_update_dpp(0, v, 0x128, 0xF, 0xF, false)
+                           : (s == 1 ? __builtin_amdgcn_update_dpp(0, v, 0x124, 0xF, 0xF, false)
+                                     : (s == 2 ? __builtin_amdgcn_update_dpp(0, v, 0x122, 0xF, 0xF, false)
+                                               : __builtin_amdgcn_update_dpp(0, v, 0x121, 0xF, 0xF, false)));
       top = fmaxf(top, __builtin_bit_cast(float, o));
     }
     if ((threadIdx.x & 63) == 0) red[turn][threadIdx.x >> 6] = top;
+    const bool all_finite = __all(finite);
     __syncthreads();
 #pragma unroll
     for (int j = 0; j < T / 64; ++j) top = fmaxf(top, red[turn][j]);
     const Scale sc(scale_of(top, a.headroom));
     if (threadIdx.x == 0) const_cast<float*>(it.kv ? cv.v_scale : cv.k_scale)[cache_scale_index(cv, it.b, cv.layer + it.l, it.h)] = sc.s;
-    uint8_t* dst = (uint8_t*)const_cast<void*>(it.kv ? cv.v : cv.k) + cache_head_base(cv, it.b, cv.layer + it.l, it.h);
-    const int j = next_of(i);
-    const bool more = j < total;
-    const Item nx = item(more ? j : i);
+    const auto dst = uniform_buffer((const char*)(it.kv ? cv.v : cv.k) + cache_head_base(cv, it.b, cv.layer + it.l, it.h),
+                                    (int)((it.n - 1) * cv.rs + cv.Dh));
+    i = next_of(i);
+    held = all_finite && !__any(sc.tiny);
+    uint32_t f = from, at = to;
+    if (held) {
+      const auto src = source(item(min(i, total - 1)), i < total);  // (none: the loads give zeros)
+      // running offsets, hidden from the compiler, which would keep all 2 U of them in registers
+      asm volatile("" : "+v"(f), "+v"(at));
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int r = r0 + step * u;
-      const uint32_t w[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
-      uint32_t o[2];
-      if constexpr (DT == FSX_F32) {
-        o[0] = encode4(__uint_as_float(w[0]), __uint_as_float(w[1]), __uint_as_float(w[2]), __uint_as_float(w[3]), sc);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 2; ++e)
-          o[e] = encode4(__uint_as_float(w[2 * e] << 16), __uint_as_float(w[2 * e] & 0xFFFF0000u), __uint_as_float(w[2 * e + 1] << 16),
-                         __uint_as_float(w[2 * e + 1] & 0xFFFF0000u), sc);
+      for (int u = 0; u < U; ++u, f += from_step, at += to_step) {
+        encode(std::true_type{}, x[u], sc, dst, at);
+        x[u] = __builtin_amdgcn_raw_buffer_load_b128(src, f, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
       }
-      if (more) load(nx, u);
-      if (r0 < step && r < it.n) {
-        if constexpr (DT == FSX_F32) *reinterpret_cast<uint32_t*>(dst + (int64_t)r * cv.rs + E * c) = o[0];
-        else *reinterpret_cast<uint2*>(dst + (int64_t)r * cv.rs + E * c) = make_uint2(o[0], o[1]);
-      }
+    } else {
+#pragma unroll 1
+      for (int u = 0; u < U; ++u, f += from_step, at += to_step)
+        encode(std::false_type{}, __builtin_amdgcn_raw_buffer_load_b128(own, f, 0, 0), sc, dst, at);
     }
-    if (!more) break;
-    i = j;
-    it = nx;
+    if (i >= total) break;
   }
 }
 
@@ -301,16 +357,21 @@ __global__ __launch_bounds__(256) void k_row_tops(RowsArgs a) {
   __syncthreads();
   if (p < pieces) {
     const char* src = (const char*)(kv ? a.v : a.k) + ((int64_t)l * a.total + a.src[b] + r0) * pieces * 16 + (int64_t)p * 16;
-    float top = 0.f;
-    int r = 0;
-    for (; r + 8 <= nr; r += 8) {
-      uint4 x[8];
+    auto largest = [&](bool finite_only) {
+      uint32_t t = 0;
+      int r = 0;
+      for (; r + 8 <= nr; r += 8) {
+        uint4 x[8];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) x[u] = *reinterpret_cast<const uint4*>(src + (int64_t)(r + u) * pieces * 16);
+        for (int u = 0; u < 8; ++u) x[u] = *reinterpret_cast<const uint4*>(src + (int64_t)(r + u) * pieces * 16);
 #pragma unroll
-      for (int u = 0; u < 8; ++u) top = piece_top<DT>(top, x[u]);
-    }
-    for (; r < nr; ++r) top = piece_top<DT>(top, *reinterpret_cast<const uint4*>(src + (int64_t)r * pieces * 16));
+        for (int u = 0; u < 8; ++u) t = fold_top<DT>(t, x[u], finite_only);
+      }
+      for (; r < nr; ++r) t = fold_top<DT>(t, *reinterpret_cast<const uint4*>(src + (int64_t)r * pieces * 16), finite_only);
+      return top_value<DT>(t);
+    };
+    float top = largest(false);
+    if (!(top < INFINITY)) top = largest(true);
     atomicMax(&tops[p / cpr - h0], __float_as_uint(top));
   }
   __syncthreads();
@@ -345,7 +406,8 @@ static hipError_t launch_replace(const RowsArgs& a, hipStream_t s) {
     const int n = *std::max_element(a.n, a.n + a.B);
     const int cpr = a.cv.Dh * (DT == FSX_F32 ? 4 : 2) / 16;
     auto held = [&](auto fn, int T, int U, int per_cu) {
-      if (cpr > T || (int64_t)n > (int64_t)(T / cpr) * U || (int64_t)n * a.cv.H * a.cv.Dh * 4 > INT32_MAX) return false;
+      if (cpr > T || (int64_t)n > (int64_t)(T / cpr) * U || (int64_t)(T / cpr) * U * std::max<int64_t>((int64_t)a.cv.H * a.cv.Dh * 4, a.cv.rs) > INT32_MAX)
+        return false;
       const int64_t items = (int64_t)2 * a.cv.H * a.layers * a.B;
       hipLaunchKernelGGL(fn, dim3((unsigned)std::min<int64_t>(items, 256 * per_cu)), dim3(T), 0, s, a);
       return true;
