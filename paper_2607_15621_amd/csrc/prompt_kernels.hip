@@ -491,12 +491,13 @@ __global__ __launch_bounds__(512, 2) void k_prompt_tiles(PromptArgs a) {
 }
 
 // =====================================================================================================
-// Few rows: a workgroup takes 32 rows and `chunk` tiles of 32 keys, which its four waves share out, each with its own two
-// buffers in LDS and no barrier; at the end they merge their states.  Where the keys are in several chunks, the workgroups'
-// states go to the workspace (16-byte piece p of lane l of block b at float4 (4 b + p) 64 + l, then maxima and sums), and
+// Few rows: a workgroup takes 32 rows and `chunk` tiles of 32 keys, which its two waves share out, each with its own two
+// buffers in LDS and no barrier; at the end they merge their states.  (Two workgroups of two waves fit a CU and start and end
+// apart: 64 new rows of four vehicles 54 us with four waves, 48 with two, 51 with one.)  Where the keys are in several chunks, the workgroups'
+// states (of rows that exist) go to the workspace (16-byte piece p of lane l of block b at float4 (4 b + p) 64 + l, then maxima and sums), and
 // k_prompt_merge puts them together in the order of the chunks.
 // =====================================================================================================
-constexpr int PS_WAVES = 4, PS_KEYS = 32;
+constexpr int PS_WAVES = 2, PS_KEYS = 32;
 
 template <int D>
 __host__ __device__ constexpr int part_floats() { return 32 * D + 64; }
@@ -568,56 +569,69 @@ __global__ __launch_bounds__(PS_WAVES * 64, 1) void k_prompt_split(PromptArgs a)
   // the waves' states, merged: wave b takes block b of the output
   const float lw = half_sum(st.l);
   __syncthreads();
-  float* ex = reinterpret_cast<float*>(w < 2 ? (w == 0 ? kb0[0] : kb1[0]) : (w == 2 ? vb0[0] : vb1[0]));
+  auto exchange = [&](int x) { return reinterpret_cast<float4*>(x == 0 ? kb0[0] : (x == 1 ? kb1[0] : (x == 2 ? vb0[0] : vb1[0]))); };
 #pragma unroll
   for (int b = 0; b < D / 32; ++b)
 #pragma unroll
     for (int p = 0; p < 4; ++p)
-      reinterpret_cast<float4*>(ex)[(4 * b + p) * 64 + lane] =
+      exchange(w)[(4 * b + p) * 64 + lane] =
           make_float4(st.o[b][4 * p], st.o[b][4 * p + 1], st.o[b][4 * p + 2], st.o[b][4 * p + 3]);
   if (half == 0) {
     sm[w][lane] = st.m;
     sl[w][lane] = lw;
   }
   __syncthreads();
-  if (w >= D / 32) return;
   const int q = lane & 31;
   float m = -INFINITY, l = 0.f, f[PS_WAVES];
 #pragma unroll
   for (int x = 0; x < PS_WAVES; ++x) m = fmaxf(m, sm[x][q]);
-  f32x16 o{};
 #pragma unroll
   for (int x = 0; x < PS_WAVES; ++x) {
     f[x] = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(sm[x][q] - m);
     l += sl[x][q] * f[x];
-    const float4* src = reinterpret_cast<const float4*>(x < 2 ? (x == 0 ? kb0[0] : kb1[0]) : (x == 2 ? vb0[0] : vb1[0]));
+  }
+  const bool whole = a.n_split[s] == 1;
+  const float inv = pr.lim >= 0 ? 1.f / l : 0.f;
+  float* part = a.part + (int64_t)blockIdx.x * part_floats<D>();
 #pragma unroll
-    for (int p = 0; p < 4; ++p) {
-      const float4 v = src[(4 * w + p) * 64 + lane];
-      o[4 * p] += v.x * f[x];
-      o[4 * p + 1] += v.y * f[x];
-      o[4 * p + 2] += v.z * f[x];
-      o[4 * p + 3] += v.w * f[x];
+  for (int b = w; b < D / 32; b += PS_WAVES) {
+    f32x16 o{};
+#pragma unroll
+    for (int x = 0; x < PS_WAVES; ++x)
+#pragma unroll
+      for (int p = 0; p < 4; ++p) {
+        const float4 v = exchange(x)[(4 * b + p) * 64 + lane];
+        o[4 * p] += v.x * f[x];
+        o[4 * p + 1] += v.y * f[x];
+        o[4 * p + 2] += v.z * f[x];
+        o[4 * p + 3] += v.w * f[x];
+      }
+    if (whole) {
+      store_block(a, o, b, pr.row * a.o_row + pr.h * a.o_head, pr.valid, inv, half);
+    } else if (pr.valid) {
+#pragma unroll
+      for (int p = 0; p < 4; ++p)
+        reinterpret_cast<float4*>(part)[(4 * b + p) * 64 + lane] = make_float4(o[4 * p], o[4 * p + 1], o[4 * p + 2], o[4 * p + 3]);
     }
   }
-  if (a.n_split[s] > 1) {
-    float* part = a.part + (int64_t)blockIdx.x * part_floats<D>();
-#pragma unroll
-    for (int p = 0; p < 4; ++p)
-      reinterpret_cast<float4*>(part)[(4 * w + p) * 64 + lane] = make_float4(o[4 * p], o[4 * p + 1], o[4 * p + 2], o[4 * p + 3]);
-    if (w == 0) part[32 * D + lane] = half ? l : m;
-    return;
-  }
-  const float inv = pr.lim >= 0 ? 1.f / l : 0.f;
-  store_block(a, o, w, pr.row * a.o_row + pr.h * a.o_head, pr.valid, inv, half);
-  if (a.lse && pr.valid && half == 0 && w == 0)
+  if (w != 0) return;
+  if (!whole && pr.valid) part[32 * D + lane] = half ? l : m;
+  if (whole && a.lse && pr.valid && half == 0)
     a.lse[pr.row * a.H + pr.h] = pr.lim >= 0 ? (m + __builtin_amdgcn_logf(l)) * (1.f / LOG2E) : -INFINITY;
 }
 
-// The chunks' states of 32 rows put together, a block of 32 channels per wave.
+// The chunks' states of 32 rows put together.  PM_GROUPS groups of waves, a block of 32 channels per wave, take every
+// PM_GROUPS-th chunk (the states come from other XCDs' memory, so what counts is how many loads are under way), then the first
+// group puts the groups' states together through LDS.
+constexpr int PM_GROUPS = 4;
+
 template <int D>
-__global__ __launch_bounds__(2 * D) void k_prompt_merge(PromptArgs a) {
+__global__ __launch_bounds__(2 * D * PM_GROUPS) void k_prompt_merge(PromptArgs a) {
+  constexpr int NB = D / 32;
+  __shared__ float4 xo[PM_GROUPS - 1][NB][4][64];
+  __shared__ float xm[PM_GROUPS - 1][32], xl[PM_GROUPS - 1][32];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, q = lane & 31;
+  const int blk = w % NB, group = w / NB;
   const int s = find_seq(a.merge_prefix, a.n_seq, blockIdx.x, lane);
   const int Hk = a.H / a.G, n_rt = (a.nq[s] * a.G + 31) / 32, i = blockIdx.x - a.merge_prefix[s], hk = i % Hk;
   const PromptRows pr(a, s, hk, 32 * (n_rt - 1 - i / Hk), lane);
@@ -625,59 +639,132 @@ __global__ __launch_bounds__(2 * D) void k_prompt_merge(PromptArgs a) {
   const float* part = a.part + (int64_t)(a.item_prefix[s] + i) * part_floats<D>();
   const int64_t step = (int64_t)n_rt * Hk * part_floats<D>();
   float m = -INFINITY, l = 0.f;
-  for (int c = 0; c < n; ++c) m = fmaxf(m, part[c * step + 32 * D + q]);
   f32x16 o{};
-  for (int c = 0; c < n; ++c) {
-    const float* x = part + c * step;
-    const float f = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(x[32 * D + q] - m);
-    l += x[32 * D + 32 + q] * f;
+  auto add = [&](float mc, float lc, const float4 (&v)[4], float mz) {
+    const float f = __builtin_amdgcn_exp2f(mc - mz);
+    l += lc * f;
 #pragma unroll
     for (int p = 0; p < 4; ++p) {
-      const float4 v = reinterpret_cast<const float4*>(x)[(4 * w + p) * 64 + lane];
-      o[4 * p] += v.x * f;
-      o[4 * p + 1] += v.y * f;
-      o[4 * p + 2] += v.z * f;
-      o[4 * p + 3] += v.w * f;
+      o[4 * p] += v[p].x * f;
+      o[4 * p + 1] += v[p].y * f;
+      o[4 * p + 2] += v[p].z * f;
+      o[4 * p + 3] += v[p].w * f;
+    }
+  };
+  auto raise = [&](float to) {  // the maximum; what the exponents are taken from
+    const float mz = to == -INFINITY ? 0.f : to, back = __builtin_amdgcn_exp2f(m - mz);
+    m = to;
+    l *= back;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[e] *= back;
+    return mz;
+  };
+  constexpr int AT_ONCE = 4;  // chunks of a wave whose loads are under way
+  if (pr.valid)  // (states of rows that do not exist were not written)
+    for (int c0 = group; c0 < n; c0 += AT_ONCE * PM_GROUPS) {
+      float mc[AT_ONCE], lc[AT_ONCE];
+      float4 v[AT_ONCE][4];
+#pragma unroll
+      for (int c = 0; c < AT_ONCE; ++c) {
+        const float* x = part + min(c0 + c * PM_GROUPS, n - 1) * step;
+        mc[c] = x[32 * D + q];
+        lc[c] = x[32 * D + 32 + q];
+#pragma unroll
+        for (int p = 0; p < 4; ++p) v[c][p] = reinterpret_cast<const float4*>(x)[(4 * blk + p) * 64 + lane];
+      }
+      float mn = m;
+#pragma unroll
+      for (int c = 0; c < AT_ONCE; ++c) mn = c0 + c * PM_GROUPS < n ? fmaxf(mn, mc[c]) : mn;
+      const float mz = raise(mn);
+#pragma unroll
+      for (int c = 0; c < AT_ONCE; ++c)
+        if (c0 + c * PM_GROUPS < n) add(mc[c], lc[c], v[c], mz);
+    }
+  if (group > 0) {
+#pragma unroll
+    for (int p = 0; p < 4; ++p) xo[group - 1][blk][p][lane] = make_float4(o[4 * p], o[4 * p + 1], o[4 * p + 2], o[4 * p + 3]);
+    if (blk == 0 && half == 0) {
+      xm[group - 1][q] = m;
+      xl[group - 1][q] = l;
     }
   }
+  __syncthreads();
+  if (group > 0) return;
+#pragma unroll
+  for (int g = 0; g < PM_GROUPS - 1; ++g) {
+    const float mc = xm[g][q], mz = raise(fmaxf(m, mc));
+    const float4 v[4] = {xo[g][blk][0][lane], xo[g][blk][1][lane], xo[g][blk][2][lane], xo[g][blk][3][lane]};
+    add(mc, xl[g][q], v, mz);
+  }
   const float inv = pr.lim >= 0 ? 1.f / l : 0.f;
-  store_block(a, o, w, pr.row * a.o_row + pr.h * a.o_head, pr.valid, inv, half);
-  if (a.lse && pr.valid && half == 0 && w == 0)
+  store_block(a, o, blk, pr.row * a.o_row + pr.h * a.o_head, pr.valid, inv, half);
+  if (a.lse && pr.valid && half == 0 && blk == 0)
     a.lse[pr.row * a.H + pr.h] = pr.lim >= 0 ? (m + __builtin_amdgcn_logf(l)) * (1.f / LOG2E) : -INFINITY;
 }
 
-// Which kernel, and in how many chunks.
+// Which kernel, and in how many chunks, by what either would take on the chip's 256 CUs (us, measured):
+//   the row tiles: a workgroup per CU, 10 to start and end and 2 per tile of 64 keys where all CUs are at work (1.5 for a few);
+//   the chunks: two workgroups per CU, 5 to start and end and, for each pair of tiles of 32 keys, 1, and 4 more to put chunks
+//   together; the last workgroups leave part of the chip idle for a share of their time;
+//   either at least its keys' way from memory, 4.5 TB/s, which the chunks' work overlaps in part.
+// Measured, chunks and row tiles, 32 heads over 8: one prompt of 1,024 tokens 27 and 33, of 2,048 76 and 59, two of 1,500 89 and
+// 52, 128 new rows of four sequences over 2,000 keys 35 and 55, 256 of two over 4,000 63 and 97; 32 heads over 32: one prompt
+// of 512 15 and 22, sixteen of 1,024 396 and 224; single tokens 41 and 184 over 8,000 keys, 81 and 183 for sixteen over 301 to
+// 7,936.
 bool plan_prompt(PromptArgs& a, int64_t workspace_bytes, int64_t* need) {
+  constexpr int CUS = 256, SLOTS = 2 * CUS, PARTS_MOST = 64;
   const int Hk = a.H / a.G;
   const int64_t part = 4 * (32 * a.D + 64);
+  const double width = a.D == 128 ? 1.0 : 0.6;  // of a tile's work
   *need = 0;
-  int64_t rows = 0, wide = 0, units = 0;
-  int t_max = 0;
+  double tiles = 0, longest = 0, steps = 0, keys = 0;
+  int64_t row_tiles = 0;
+  int t_max = 1;
   for (int i = 0; i < a.n_seq; ++i) {
-    const int64_t r = (int64_t)a.nq[i] * a.G, t = (a.nk[i] + PS_KEYS - 1) / PS_KEYS;
-    rows += r * Hk;
-    wide += (r + 255) / 256 * Hk;
-    units += (r + 31) / 32 * Hk * t;
-    t_max = std::max(t_max, (int)t);
+    const int64_t r = (int64_t)a.nq[i] * a.G, wide = (r + 255) / 256, n_rt = (r + 31) / 32;
+    const double seen = a.nk[i] - 0.5 * std::min(a.nq[i], a.nk[i]);  // keys of a row, on average
+    tiles += (double)Hk * wide * (10 + 2 * width * (seen / PT_KEYS + 1));
+    longest = std::max(longest, 10 + 1.5 * width * (a.nk[i] / PT_KEYS + 1));
+    steps += (double)Hk * n_rt * (seen / PS_KEYS + 1);
+    keys += (double)Hk * a.nk[i];
+    row_tiles += Hk * n_rt;
+    t_max = std::max(t_max, (a.nk[i] + PS_KEYS - 1) / PS_KEYS);
   }
-  if (wide >= 192 || (wide > 0 && rows / wide > 160)) return false;
-  // about two workgroups per CU, of at least 16 tiles
-  int chunk = std::max<int64_t>(16, (units + 511) / 512);
-  for (;; chunk *= 2) {
+  const double memory = keys * a.D * 4 / 4.5e6;
+  tiles = std::max(tiles / CUS, longest);
+  tiles = std::max(tiles, memory) + 0.35 * std::min(tiles, memory);
+  const double per_wave = steps / (SLOTS * PS_WAVES), shared_step = std::max(width, memory / per_wave);
+  double best = 0;
+  for (int k = 1; k <= PARTS_MOST; ++k) {
+    const int chunk = std::max(2 * PS_WAVES, (t_max + k - 1) / k);
     int64_t items = 0;
     bool split = false;
     for (int i = 0; i < a.n_seq; ++i) {
-      const int n_rt = (int)(((int64_t)a.nq[i] * a.G + 31) / 32), t = (a.nk[i] + PS_KEYS - 1) / PS_KEYS;
-      a.n_split[i] = std::max(1, (t + chunk - 1) / chunk);
-      split = split || a.n_split[i] > 1;
-      a.item_prefix[i + 1] = a.item_prefix[i] + n_rt * Hk * a.n_split[i];
-      a.merge_prefix[i + 1] = a.merge_prefix[i] + (a.n_split[i] > 1 ? n_rt * Hk : 0);
+      const int n_rt = (int)(((int64_t)a.nq[i] * a.G + 31) / 32), n = std::max(1, ((a.nk[i] + PS_KEYS - 1) / PS_KEYS + chunk - 1) / chunk);
+      items += (int64_t)n_rt * Hk * n;
+      split = split || n > 1;
     }
+    if (split && items * part > workspace_bytes) break;
+    const double rounds = std::max(1.0, (double)items / SLOTS), pair = (double)chunk / PS_WAVES;
+    const double work = 5 * rounds + width * (rounds > 1 ? std::max(per_wave, pair) : pair);
+    const double tail = rounds > 1 ? 0.15 * pair : 0.4 * std::max(0.0, pair - steps / items / PS_WAVES);
+    const double cost = std::max(memory, work) + 0.35 * std::min(memory, work) + tail * shared_step + (split ? 4 : 0);
+    if (k > 1 && cost >= best) continue;
+    best = cost;
     a.chunk = chunk;
-    *need = split ? a.item_prefix[a.n_seq] * part : 0;
-    if (*need <= workspace_bytes) return true;
-    if (chunk > t_max) return true;
+    *need = split ? items * part : 0;
   }
+  if (tiles <= best || row_tiles * PARTS_MOST > INT32_MAX) {
+    *need = 0;
+    return false;
+  }
+  for (int i = 0; i < a.n_seq; ++i) {
+    const int n_rt = (int)(((int64_t)a.nq[i] * a.G + 31) / 32);
+    a.n_split[i] = std::max(1, ((a.nk[i] + PS_KEYS - 1) / PS_KEYS + a.chunk - 1) / a.chunk);
+    a.item_prefix[i + 1] = a.item_prefix[i] + n_rt * Hk * a.n_split[i];
+    a.merge_prefix[i + 1] = a.merge_prefix[i] + (a.n_split[i] > 1 ? n_rt * Hk : 0);
+  }
+  return true;
 }
 
 hipError_t launch_prompt_attention(PromptArgs a, void* workspace, int64_t workspace_bytes, hipStream_t s) {
@@ -688,10 +775,10 @@ hipError_t launch_prompt_attention(PromptArgs a, void* workspace, int64_t worksp
     const dim3 grid(a.item_prefix[a.n_seq]), merge(a.merge_prefix[a.n_seq]);
     if (a.D == 64) {
       hipLaunchKernelGGL(k_prompt_split<64>, grid, dim3(PS_WAVES * 64), 0, s, a);
-      if (merge.x) hipLaunchKernelGGL(k_prompt_merge<64>, merge, dim3(128), 0, s, a);
+      if (merge.x) hipLaunchKernelGGL(k_prompt_merge<64>, merge, dim3(128 * PM_GROUPS), 0, s, a);
     } else {
       hipLaunchKernelGGL(k_prompt_split<128>, grid, dim3(PS_WAVES * 64), 0, s, a);
-      if (merge.x) hipLaunchKernelGGL(k_prompt_merge<128>, merge, dim3(256), 0, s, a);
+      if (merge.x) hipLaunchKernelGGL(k_prompt_merge<128>, merge, dim3(256 * PM_GROUPS), 0, s, a);
     }
     return hipGetLastError();
   }

@@ -315,11 +315,17 @@ class PackedRows:
         self.n, self.c_start, self.c_len = len(self.len), self.start.ctypes.data_as(P), self.len.ctypes.data_as(P)
 
 
+_dtypes = {}
+
+
 def _dtype_of(t) -> int:
-    code = {"torch.float32": F32, "torch.bfloat16": BF16}.get(str(t.dtype))
-    if code is None:
+    if not _dtypes:
+        import torch
+
+        _dtypes.update({torch.float32: F32, torch.bfloat16: BF16})
+    if t.dtype not in _dtypes:
         raise ValueError(f"tensors of dtype {t.dtype} are not taken here: float32 or bfloat16")
-    return code
+    return _dtypes[t.dtype]
 
 
 def _prompt_desc(q, k, v, out, scale: float) -> PromptDesc:
