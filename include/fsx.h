@@ -290,6 +290,18 @@ int fsx_backbone_create(const fsx_backbone_cfg* cfg, const fsx_layer_weights* la
  * The ring state (start, len, pos) is updated on the host before returning, as fsx_cache_append_rows does. */
 int fsx_backbone_append(fsx_backbone* bb, fsx_cache_desc* cache, const void* tokens, int32_t batch, int32_t n_rows,
                         float* hidden, int32_t policy, void* stream);
+/* Rebuild the cache from scratch (Sec. 3.3: on an instruction change, a notice, an episode's end): whole prompts of agents of
+ * different lengths through the layers, in one call, their rotated keys and values replacing the agents' rows
+ * (fsx_prompt_attention and fsx_cache_replace_rows per layer).
+ *   tokens    DEVICE [sum of n_tokens][d] bf16 embeddings, agent after agent, at positions 0 .. n_tokens[b]-1
+ *   n_tokens  HOST [cache->batch]; an agent with 0 is left as it is.  Their sum is at most max_batch * max_new_rows
+ *             (FSX_E_CAPACITY): the rows that the workspace holds
+ *   hidden    DEVICE [n_layers][sum of n_tokens][d] fp32 output of every layer, or NULL
+ *   headroom, policy  as fsx_cache_replace_rows (an FP8 cache gets new scales, found from the rows).  The attention is over
+ *             the rows as computed, before they are encoded
+ * The ring state of the rebuilt agents is updated on the host before returning, as fsx_cache_replace_rows does. */
+int fsx_backbone_rebuild(fsx_backbone* bb, fsx_cache_desc* cache, const void* tokens, const int64_t* n_tokens, float* hidden,
+                         float headroom, int32_t policy, void* stream);
 /* Bytes of the packed weight matrices (streamed once per call) and of the workspace. */
 int fsx_backbone_info(const fsx_backbone* bb, int64_t* weight_bytes, int64_t* workspace_bytes);
 /* Wait for the handle's last call, then free it. */

@@ -1057,6 +1057,31 @@ static int check_row_buffers(const fsx_cache_desc* c, const void* k_rows, const 
   return FSX_OK;
 }
 
+// The rows of every agent that are kept, into slots from 0 on.
+static int plan_replace(const fsx_cache_desc& c, const int64_t* row_start, const int64_t* row_len, int32_t policy, RowsArgs& a) {
+  a.B = c.batch;
+  for (int b = 0; b < a.B; ++b) {
+    if (row_len[b] > c.capacity && policy == FSX_APPEND_ERROR)
+      return fail(FSX_E_CAPACITY, "agent " + std::to_string(b) + ": more rows than the ring holds (policy FSX_APPEND_ERROR)");
+    if (row_len[b] > 0 && c.capacity == 0) return fail(FSX_E_CAPACITY, "the ring has no slots");
+    const int64_t n = std::min(row_len[b], c.capacity);
+    a.n[b] = (int32_t)n;
+    a.src[b] = row_start[b] + row_len[b] - n;
+    a.slot[b] = 0;
+    a.prefix[b + 1] = a.prefix[b] + n;
+  }
+  return FSX_OK;
+}
+
+static void rings_replaced(fsx_cache_desc* cache, const int64_t* row_len, const RowsArgs& a) {
+  for (int b = 0; b < a.B; ++b)
+    if (row_len[b] > 0) {
+      cache->start[b] = 0;
+      cache->len[b] = a.n[b];
+      cache->pos[b] = row_len[b];
+    }
+}
+
 extern "C" int fsx_cache_replace_rows(fsx_cache_desc* cache, int32_t layer, int32_t n_layers, const void* k_rows,
                                       const void* v_rows, int32_t rows_dtype, int64_t total_rows, const int64_t* row_start,
                                       const int64_t* row_len, float headroom, int32_t policy, void* stream) {
@@ -1067,19 +1092,9 @@ extern "C" int fsx_cache_replace_rows(fsx_cache_desc* cache, int32_t layer, int3
   if (cache->layout & FSX_CACHE_SHARED)
     return fail(FSX_E_UNSUPPORTED, "a shared cache is a set of views of one agent's rings; replace its rows through a "
                                    "descriptor of that agent alone");
-  const int B = cache->batch;
   RowsArgs a{};
-  for (int b = 0; b < B; ++b) {
-    if (row_len[b] > cache->capacity && policy == FSX_APPEND_ERROR)
-      return fail(FSX_E_CAPACITY, "agent " + std::to_string(b) + ": more rows than the ring holds (policy FSX_APPEND_ERROR)");
-    if (row_len[b] > 0 && cache->capacity == 0) return fail(FSX_E_CAPACITY, "the ring has no slots");
-    const int64_t n = std::min(row_len[b], cache->capacity);
-    a.n[b] = (int32_t)n;
-    a.src[b] = row_start[b] + row_len[b] - n;
-    a.slot[b] = 0;
-    a.prefix[b + 1] = a.prefix[b] + n;
-  }
-  if (a.prefix[B] == 0) {
+  if ((rc = plan_replace(*cache, row_start, row_len, policy, a))) return rc;
+  if (a.prefix[a.B] == 0) {
     g_err.clear();
     return FSX_OK;
   }
@@ -1088,14 +1103,9 @@ extern "C" int fsx_cache_replace_rows(fsx_cache_desc* cache, int32_t layer, int3
   a.cv = cache_view(*cache);
   a.cv.layer = layer;
   a.k = const_cast<void*>(k_rows); a.v = const_cast<void*>(v_rows);
-  a.rows_f32 = rows_dtype == FSX_F32; a.layers = n_layers; a.B = B; a.total = total_rows; a.headroom = headroom;
+  a.rows_f32 = rows_dtype == FSX_F32; a.layers = n_layers; a.total = total_rows; a.headroom = headroom;
   HIP_TRY(launch_replace_rows(a, (hipStream_t)stream));
-  for (int b = 0; b < B; ++b)
-    if (row_len[b] > 0) {
-      cache->start[b] = 0;
-      cache->len[b] = a.n[b];
-      cache->pos[b] = row_len[b];
-    }
+  rings_replaced(cache, row_len, a);
   g_err.clear();
   return FSX_OK;
 }
@@ -1312,6 +1322,83 @@ extern "C" int fsx_backbone_append(fsx_backbone* bb, fsx_cache_desc* cache, cons
     }
     cache->pos[b] += n_rows;
   }
+  g_err.clear();
+  return FSX_OK;
+}
+
+extern "C" int fsx_backbone_rebuild(fsx_backbone* bb, fsx_cache_desc* cache, const void* tokens, const int64_t* n_tokens,
+                                    float* hidden, float headroom, int32_t policy, void* stream) {
+  if (!bb || !bb->ex) return fail(FSX_E_INVALID, "backbone handle is NULL");
+  fsx_expert* ex = bb->ex;
+  const fsx_expert_cfg& c = ex->cfg;
+  if (!n_tokens) return fail(FSX_E_INVALID, "n_tokens must be a non-NULL host array");
+  if (policy != FSX_APPEND_RING && policy != FSX_APPEND_ERROR) return fail(FSX_E_INVALID, "unknown append policy");
+  if (!(headroom >= 1.f && headroom <= 64.f)) return fail(FSX_E_INVALID, "headroom must be in 1..64");
+  int rc = validate_cache(ex, cache, cache ? cache->batch : 0);
+  if (rc) return rc;
+  if (cache->layout & FSX_CACHE_SHARED) return fail(FSX_E_UNSUPPORTED, "the rows of a shared cache cannot be replaced");
+  if (cache->dtype != FSX_BF16 && cache->dtype != FSX_FP8_E4M3)
+    return fail(FSX_E_UNSUPPORTED, "the backbone writes BF16 or FP8 caches");
+  const int B = cache->batch;
+  std::array<int64_t, FSX_MAX_BATCH> at{};
+  int64_t rows = 0;
+  for (int b = 0; b < B; ++b) {
+    if (n_tokens[b] < 0) return fail(FSX_E_INVALID, "n_tokens must be >= 0");
+    if (n_tokens[b] > ex->M_max - rows)
+      return fail(FSX_E_CAPACITY, "more than max_batch * max_new_rows = " + std::to_string(ex->M_max) + " tokens");
+    at[b] = rows;
+    rows += n_tokens[b];
+  }
+  RowsArgs ra{};
+  if ((rc = plan_replace(*cache, at.data(), n_tokens, policy, ra))) return rc;
+  if (rows == 0) {
+    g_err.clear();
+    return FSX_OK;
+  }
+  if (!tokens || !aligned16(tokens)) return fail(FSX_E_INVALID, "tokens must be non-NULL and 16-byte aligned");
+  if ((rc = check_row_buffers(cache, nullptr, nullptr))) return rc;
+  int dev = 0;
+  HIP_TRY(hipGetDevice(&dev));
+  if (dev != ex->device) return fail(FSX_E_INVALID, "current device differs from the one the backbone was created on");
+  hipStream_t s = (hipStream_t)stream;
+
+  TickParams tp{};
+  tp.B = B;
+  tp.M = tp.S = tp.T = (int)rows;
+  for (int b = 0; b < B; ++b) tp.chunk_prefix[b + 1] = (int)(at[b] + n_tokens[b]);  // every prompt starts at position 0
+  Dims dm{};
+  dm.d = c.d_model; dm.H = c.n_heads; dm.Dh = c.head_dim; dm.A = ex->A; dm.F = c.d_ffn; dm.n_layers = c.n_layers;
+  dm.n_out = c.n_out; dm.eps = c.rms_eps; dm.rope_base = c.rope_base; dm.head_kind = 0;
+  const Workspace& ws = ex->ws;
+  PromptArgs pa{};
+  pa.q = ws.q; pa.k = ws.kself; pa.v = ws.vself; pa.out = ws.attn;
+  pa.q_row = pa.k_row = pa.v_row = pa.o_row = dm.A;
+  pa.q_head = pa.k_head = pa.v_head = pa.o_head = dm.Dh;
+  pa.H = dm.H; pa.G = 1; pa.D = dm.Dh;
+  pa.q_f32 = 1;
+  pa.c = 1.f;  // the projection leaves its queries scaled, in log2 units
+  prompt_sequences(pa, B, at.data(), n_tokens, at.data(), n_tokens);
+  ra.cv = cache_view(*cache);
+  ra.k = ws.kself; ra.v = ws.vself;
+  ra.layers = 1; ra.total = rows; ra.headroom = headroom;
+  const int64_t spare = (int64_t)ex->items_max * 16 * dm.Dh * 4;  // the attention's partial states (att_o)
+  const int ks_o = gemm_split(tp.M, dm.d, dm.A), ks_d = gemm_split(tp.M, dm.d, dm.F);
+  HIP_TRY(launch_embed(tokens, c.dtype, ex->fw[0].attn_norm, tp, dm, ws, s, true));
+  for (int l = 0; l < c.n_layers; ++l) {
+    const FastWeights& w = ex->fw[l];
+    ra.cv.layer = l;
+    HIP_TRY(launch_gemm_qkv(w, tp, dm, ws, s, l > 0));
+    HIP_TRY(launch_prompt_attention(pa, ws.att_o, spare, s));
+    HIP_TRY(launch_replace_rows(ra, s));
+    HIP_TRY(launch_gemm_o(w, tp, dm, ws, ks_o, s));
+    HIP_TRY(launch_reduce_norm(tp, dm, ws, ks_o, w.ffn_norm, nullptr, s));
+    HIP_TRY(launch_gemm_gu(w, tp, dm, ws, s));
+    HIP_TRY(launch_gemm_down(w, tp, dm, ws, ks_d, s));
+    const float* gnext = l + 1 < c.n_layers ? ex->fw[l + 1].attn_norm : ex->final_norm;
+    HIP_TRY(launch_reduce_norm(tp, dm, ws, ks_d, gnext, hidden ? hidden + (int64_t)l * tp.M * dm.d : nullptr, s));
+  }
+  HIP_TRY(hipEventRecord(ex->done, s));
+  rings_replaced(cache, n_tokens, ra);
   g_err.clear();
   return FSX_OK;
 }

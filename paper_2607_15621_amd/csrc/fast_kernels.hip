@@ -82,12 +82,15 @@ hipError_t launch_pack(const uint16_t* a, const uint16_t* b, int N, int K, int k
 // Embed: h = tokens (fp32), x = bf16(h / rms(h)), rotary table cos/sin(p * base^(-2j/Dh)) in fp64.
 // One workgroup per token row.
 // =====================================================================================================
+// PACKED: agents of different lengths, agent b's tokens in rows chunk_prefix[b] .. chunk_prefix[b + 1] - 1.
+template <bool PACKED>
 __global__ __launch_bounds__(256) void k_embed(const void* __restrict__ tokens, int tok_dtype,
                                                const float* __restrict__ g0, TickParams tp, Dims dm,
                                                Workspace ws) {
   __shared__ float red[16];
-  const int m = blockIdx.x;
-  const int b = m / tp.S, t = m % tp.S;
+  const int m = blockIdx.x, lane = threadIdx.x & 63;
+  const int b = PACKED ? __popcll(__ballot(lane < tp.B && tp.chunk_prefix[lane + 1] <= m)) : m / tp.S;
+  const int t = PACKED ? m - tp.chunk_prefix[b] : m % tp.S;
   const int d = dm.d;
   float ss = 0.f;
   for (int n = threadIdx.x; n < d; n += blockDim.x) {
@@ -117,8 +120,9 @@ __global__ __launch_bounds__(256) void k_embed(const void* __restrict__ tokens, 
 }
 
 hipError_t launch_embed(const void* tokens, int tok_dtype, const float* g0, const TickParams& tp, const Dims& dm,
-                        const Workspace& ws, hipStream_t s) {
-  hipLaunchKernelGGL(k_embed, dim3(tp.M), dim3(256), 0, s, tokens, tok_dtype, g0, tp, dm, ws);
+                        const Workspace& ws, hipStream_t s, bool packed) {
+  const auto fn = packed ? k_embed<true> : k_embed<false>;
+  hipLaunchKernelGGL(fn, dim3(tp.M), dim3(256), 0, s, tokens, tok_dtype, g0, tp, dm, ws);
   return hipGetLastError();
 }
 

@@ -110,8 +110,9 @@ struct Dims {
 constexpr int RN_CHUNK = 512;
 __host__ __device__ inline bool wide_rows(const Dims& dm) { return dm.d >= 4 * RN_CHUNK && dm.d % RN_CHUNK == 0; }
 
+// packed: agents of different lengths, their rows by tp.chunk_prefix.
 hipError_t launch_embed(const void* tokens, int tok_dtype, const float* g0, const TickParams& tp, const Dims& dm,
-                        const Workspace& ws, hipStream_t s);
+                        const Workspace& ws, hipStream_t s, bool packed = false);
 // after_reduction: xb comes from a reduction (not from the embedding); for wide rows it is then unscaled and the
 // projection applies the RMSNorm row scales from the chunk sums of squares.
 hipError_t launch_gemm_qkv(const FastWeights& w, const TickParams& tp, const Dims& dm, const Workspace& ws,

@@ -31,7 +31,7 @@ SYMBOLS = ("fsx_expert_create", "fsx_expert_forward", "fsx_cache_append_rows", "
            "fsx_loop_create", "fsx_loop_tick", "fsx_loop_append", "fsx_loop_sync", "fsx_loop_destroy",
            "fsx_loop_last_error", "fsx_backbone_create", "fsx_backbone_append", "fsx_backbone_info",
            "fsx_backbone_destroy", "fsx_prompt_attention", "fsx_prompt_attention_workspace", "fsx_cache_replace_rows",
-           "fsx_cache_read_rows")
+           "fsx_cache_read_rows", "fsx_backbone_rebuild")
 
 
 class FsxError(RuntimeError):
@@ -127,10 +127,11 @@ def lib() -> ctypes.CDLL:
         L.fsx_backbone_create.argtypes = [ctypes.POINTER(BackboneCfg), ctypes.POINTER(LayerWeights), vp,
                                           ctypes.POINTER(vp)]
         L.fsx_backbone_append.argtypes = [vp, ctypes.POINTER(CacheDescC), vp, i32, i32, vp, i32, vp]
+        L.fsx_backbone_rebuild.argtypes = [vp, ctypes.POINTER(CacheDescC), vp, ctypes.POINTER(i64), vp, ctypes.c_float, i32, vp]
         L.fsx_backbone_info.argtypes = [vp, ctypes.POINTER(i64), ctypes.POINTER(i64)]
         L.fsx_backbone_destroy.argtypes = [vp]
         L.fsx_backbone_destroy.restype = None
-        for n in ("fsx_backbone_create", "fsx_backbone_append", "fsx_backbone_info"):
+        for n in ("fsx_backbone_create", "fsx_backbone_append", "fsx_backbone_info", "fsx_backbone_rebuild"):
             getattr(L, n).restype = ctypes.c_int
         P64 = ctypes.POINTER(i64)
         L.fsx_prompt_attention.argtypes = [ctypes.POINTER(PromptDesc), vp, vp, vp, vp, vp, i32, P64, P64, P64, P64, vp, i64,
@@ -140,7 +141,7 @@ def lib() -> ctypes.CDLL:
                                              ctypes.c_float, i32, vp]
         L.fsx_cache_read_rows.argtypes = [ctypes.POINTER(CacheDescC), i32, i32, P64, vp, vp, i32, i64, P64, P64, vp]
         for n in ("fsx_prompt_attention", "fsx_prompt_attention_workspace", "fsx_cache_replace_rows",
-                  "fsx_cache_read_rows"):
+                  "fsx_cache_read_rows", "fsx_backbone_rebuild"):
             getattr(L, n).restype = ctypes.c_int
         for n in ("fsx_expert_create", "fsx_expert_forward", "fsx_cache_append_rows", "fsx_expert_info",
                   "fsx_expert_status", "fsx_expert_trace", "fsx_probe_hbm_read"):
@@ -461,6 +462,15 @@ class Backbone:
                stream=None):
         _check(lib().fsx_backbone_append(ctypes.c_void_p(self.handle), ctypes.byref(cache.c), _ptr(tokens), batch,
                                          n_rows, _ptr(hidden), policy, _stream(stream)))
+
+    def rebuild(self, cache: CacheDesc, tokens, lengths, hidden=None, headroom: float = 1.0, policy: int = APPEND_RING,
+                stream=None):
+        """fsx_backbone_rebuild: whole prompts, tokens [sum of lengths][d], replace the rows of the agents with lengths > 0."""
+        n = PackedRows(lengths)
+        if n.n != cache.c.batch:
+            raise ValueError("a length of every agent of the cache")
+        _check(lib().fsx_backbone_rebuild(ctypes.c_void_p(self.handle), ctypes.byref(cache.c), _ptr(tokens), n.c_len,
+                                          _ptr(hidden), headroom, policy, _stream(stream)))
 
     def info(self):
         wb, wsb = ctypes.c_int64(), ctypes.c_int64()

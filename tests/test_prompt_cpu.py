@@ -71,6 +71,7 @@ def test_nulls():
     assert L.fsx_prompt_attention_workspace(ctypes.byref(d), 65, r.c_len, None, ctypes.byref(need)) == INVALID
     bad = fsx.PackedRows([-1])
     assert L.fsx_prompt_attention_workspace(ctypes.byref(d), 1, bad.c_len, None, ctypes.byref(need)) == INVALID
+    assert L.fsx_backbone_rebuild(None, None, None, None, None, 1.0, 0, None) == INVALID
 
 
 def test_nothing_to_do_needs_no_gpu():
