@@ -115,6 +115,15 @@ __device__ __forceinline__ void store_block(const PromptArgs& a, const f32x16& o
   }
 }
 
+// The value is computed here: neither the products nor the vector work that make it may move to the other side of a barrier,
+// which to the compiler concerns memory alone.
+__device__ __forceinline__ void here(f32x16& x) { asm volatile("" : "+v"(x)); }
+__device__ __forceinline__ void here(uint4& x) {
+  u32x4_t y = __builtin_bit_cast(u32x4_t, x);
+  asm volatile("" : "+v"(y));
+  x = __builtin_bit_cast(uint4, y);
+}
+
 // S^T of a tile of 32 KB keys, in LDS at kt.
 template <int D, int KB>
 __device__ __forceinline__ void tile_scores(const char* kt, const uint4 (&qf)[D / 16], int lane, f32x16 (&s)[KB]) {
@@ -218,9 +227,15 @@ __device__ __forceinline__ void add_tile(const char* kt, const char* vt, const u
                                          int lane, PromptState<D>& st) {
   f32x16 s[KB];
   uint4 pf[2 * KB];
+  // (the products first where another wave of the SIMD could take its vector work in between: 16 prompts of 1,024 tokens 213 us
+  // without, 202 with)
+  __builtin_amdgcn_s_setprio(1);
   tile_scores<D, KB>(kt, qf, lane, s);
+  __builtin_amdgcn_s_setprio(0);
   tile_softmax<D, KB>(s, c, lim, masked, lane >> 5, st, pf, [](int) {});
+  __builtin_amdgcn_s_setprio(1);
   tile_values<D, KB>(vt, pf, lane, st);
+  __builtin_amdgcn_s_setprio(0);
 }
 
 // Values that are not finite, in keys that some of the queries do not see: a product with the weight 0 would make NaN of them.
@@ -287,15 +302,6 @@ struct PromptRows {
   }
 };
 
-// The value is computed here: neither the products nor the vector work that make it may move to the other side of a barrier,
-// which to the compiler concerns memory alone.
-__device__ __forceinline__ void here(f32x16& x) { asm volatile("" : "+v"(x)); }
-__device__ __forceinline__ void here(uint4& x) {
-  u32x4_t y = __builtin_bit_cast(u32x4_t, x);
-  asm volatile("" : "+v"(y));
-  x = __builtin_bit_cast(uint4, y);
-}
-
 // Every wave of the workgroup has got here; memory operations stay on their side.
 __device__ __forceinline__ void meet() {
   asm volatile("" ::: "memory");
@@ -314,16 +320,93 @@ __device__ __forceinline__ uint32_t lds_address(const void* p) {
   return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)p;
 }
 
-// The eight waves, two per SIMD, work in turns, a barrier between the turns: while waves 0-3 run matrix instructions (the scores
+// Four waves take 128 rows and walk over the keys in step, one tile ahead; two such workgroups share a CU, and one
+// starts or ends while the other computes.
+template <int D>
+__global__ __launch_bounds__(256, 2) void k_prompt_tiles(PromptArgs a) {
+  constexpr int NW = 4, RB = 2 * D, TILE = PT_KEYS * RB, RPI = 1024 / RB, NI = PT_KEYS / RPI / NW;  // rows and loads per wave's load
+  __shared__ __align__(1024) char kt[2 * TILE], vt[2 * TILE];
+  __shared__ int again, first_bad[3 * D];
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
+  const int s = find_seq(a.item_prefix, a.n_seq, blockIdx.x, lane);
+  const int in_seq = blockIdx.x - a.item_prefix[s], Hk = a.H / a.G;
+  const int nk = a.nk[s], rows = a.nq[s] * a.G, tiles = (rows + NW * 32 - 1) / (NW * 32);
+  const int rt = __builtin_amdgcn_readfirstlane(in_seq / Hk), hk = in_seq - rt * Hk;
+  const int r0 = (tiles - 1 - rt) * NW * 32;  // the rows with the most keys first
+  const int off = nk - a.nq[s], n_tiles = __builtin_amdgcn_readfirstlane(max(0, (off + (min(r0 + NW * 32, rows) - 1) / a.G + PT_KEYS) / PT_KEYS));
+  if (threadIdx.x == 0) again = 0;
+
+  const int lr = lane / (RB / 16), lp = lane % (RB / 16);
+  const uint16_t* kbase = a.k + a.k0[s] * a.k_row + hk * a.k_head;
+  const uint16_t* vbase = a.v + a.k0[s] * a.v_row + hk * a.v_head;
+  const uint32_t kl = lds_address(kt), vl = lds_address(vt);
+  // the lane's piece of a load, the same in all of a wave's loads
+  const uint32_t kp = 16 * (lp ^ k_turn<D>(w * RPI + lr)), vp = 16 * (lp ^ v_turn<D>(w * RPI + lr));
+  const uint32_t kat = (uint32_t)lr * (uint32_t)a.k_row * 2 + kp, vat = (uint32_t)lr * (uint32_t)a.v_row * 2 + vp;
+  auto load = [&](int j, int n, uint32_t t, const uint16_t* base, int64_t stride, uint32_t at, uint32_t piece) {
+    const int i = w + NW * n, r = j * PT_KEYS + i * RPI;
+    if (r + RPI <= nk) {
+      dma16(base + r * stride, at, t + i * 1024);
+    } else {  // past the last key: that key again
+      const int r1 = min(r, nk - 1);
+      dma16(base + r1 * stride, (uint32_t)min(lr, nk - 1 - r1) * (uint32_t)stride * 2 + piece, t + i * 1024);
+    }
+  };
+  auto issue = [&](int j, int buf) {
+#pragma unroll
+    for (int n = 0; n < NI; ++n) {
+      load(j, n, kl + buf * TILE, kbase, a.k_row, kat, kp);
+      load(j, n, vl + buf * TILE, vbase, a.v_row, vat, vp);
+    }
+  };
+  if (n_tiles > 0) issue(0, 0);
+  const PromptRows pr(a, s, hk, r0 + 32 * w, lane);
+  uint4 qf[D / 16];
+  load_queries<D>(a, pr.row * a.q_row + pr.h * a.q_head, half, qf);
+  PromptState<D> st;
+  clear_state(st);
+  for (int j = 0; j < n_tiles; ++j) {
+    const int k0 = j * PT_KEYS, buf = j & 1;
+    vm_wait_all();
+    meet();  // tile j has landed, and every wave is done with the tile before
+    if (j + 1 < n_tiles) issue(j + 1, buf ^ 1);
+    if (k0 <= pr.last) add_tile<D, 2>(kt + buf * TILE, vt + buf * TILE, qf, a.c, pr.lim - k0, k0 + PT_KEYS - 1 > pr.first, lane, st);
+  }
+  __syncthreads();
+  if (!__all(all_finite(st))) again = 1;
+  __syncthreads();
+  if (again) {
+    for (int i = threadIdx.x; i < 3 * D; i += NW * 64) first_bad[i] = INT32_MAX;
+    clear_state(st);
+    for (int j = 0; j < n_tiles; ++j) {
+      const int k0 = j * PT_KEYS;
+      __syncthreads();
+      issue(j, 0);
+      vm_wait_all();
+      __syncthreads();
+      if (k0 + PT_KEYS - 1 > off + r0 / a.G) take_out_nonfinite<D>(vt, PT_KEYS, nk - k0, k0, first_bad, threadIdx.x, NW * 64);
+      __syncthreads();
+      add_tile<D, 2>(kt, vt, qf, a.c, pr.lim - k0, true, lane, st);
+    }
+    put_back_nonfinite(st, first_bad, pr.lim, half);
+  }
+  const float l = half_sum(st.l), inv = pr.lim >= 0 ? 1.f / l : 0.f;
+  const int64_t at = pr.row * a.o_row + pr.h * a.o_head;
+#pragma unroll
+  for (int b = 0; b < D / 32; ++b) store_block(a, st.o[b], b, at, pr.valid, inv, half);
+  if (a.lse && pr.valid && half == 0)
+    a.lse[pr.row * a.H + pr.h] = pr.lim >= 0 ? (st.m + __builtin_amdgcn_logf(l)) * (1.f / LOG2E) : -INFINITY;
+}
+
+// Long prompts with heads of 128 channels.  A workgroup of eight waves, two per SIMD, takes 256 rows; the waves work in turns, a barrier between the turns: while waves 0-3 run matrix instructions (the scores
 // of tile j + 1, then the values of tile j), waves 4-7 run the softmax of tile j on the vector units, and the other way round.
 // Waves 0-3 run softmax j in turn 2 j and the products in turn 2 j + 1, waves 4-7 one turn later.  V(j) is read in turns 2 j + 1
 // and 2 j + 2, K(j) in turns 2 j - 1 and 2 j (its first pieces one turn before that, ahead of the barrier).
 // Loads go out during a wave's softmax: V(j + 1) and K(j + 3) for waves 0-3 (turn 2 j), V(j + 2) and K(j + 4) for waves 4-7 (turn
 // 2 j + 1), over V(j - 2), K(j - 1), V(j - 1) and K(j) of three and four buffers; a wave waits for its own before it sends for the
 // next two turns later, and the barrier of that turn makes them known to all: V(j + 1) after turn 2 j + 2, K(j + 3) likewise.
-template <int D>
-__global__ __launch_bounds__(512, 2) void k_prompt_tiles(PromptArgs a) {
-  constexpr int NW = 8, RB = 2 * D, TILE = PT_KEYS * RB, RPI = 1024 / RB, NI = PT_KEYS / RPI / NW;  // rows and loads per wave's load
+__global__ __launch_bounds__(512, 2) void k_prompt_turns(PromptArgs a) {
+  constexpr int D = 128, NW = 8, RB = 2 * D, TILE = PT_KEYS * RB, RPI = 1024 / RB, NI = PT_KEYS / RPI / NW;  // rows and loads per wave's load
   constexpr int KS = D / 16, NV = D / 32, KAHEAD = 8;
   __shared__ __align__(1024) char kt[4 * TILE], vt[3 * TILE];
   __shared__ int again, first_bad[3 * D];
@@ -702,36 +785,52 @@ __global__ __launch_bounds__(2 * D * PM_GROUPS) void k_prompt_merge(PromptArgs a
     a.lse[pr.row * a.H + pr.h] = pr.lim >= 0 ? (m + __builtin_amdgcn_logf(l)) * (1.f / LOG2E) : -INFINITY;
 }
 
+// Whether the keys of the prompts (on average over their work) are many enough for the waves' turns to be worth the longer start
+// and end of their workgroups.  us with and without: 16 prompts of 1,024 tokens 229 and 202, four of 2,048 174 and 166, two of
+// 4,096 (32 heads over 8) 272 and 275, one of 8,000 477 and 497, one of 16,001 1,850 and 1,910.  With heads of 64 channels, whose
+// products are half as long, never: two prompts of 4,096 179 and 170.
+static bool long_prompts(const PromptArgs& a) {
+  double work = 0, keys = 0;
+  for (int i = 0; i < a.n_seq; ++i) {
+    const double w = (double)a.nq[i] * a.nk[i];
+    work += w;
+    keys += w * a.nk[i];
+  }
+  return a.D == 128 && keys >= 4096 * work;
+}
+
 // Which kernel, and in how many chunks, by what either would take on the chip's 256 CUs (us, measured):
-//   the row tiles: a workgroup per CU, 10 to start and end and 2 per tile of 64 keys where all CUs are at work (1.5 for a few);
+//   the row tiles: 128 rows to a workgroup, two workgroups per CU, 5 to start and end and 2.2 per tile of 64 keys where all CUs are
+//   at work (1.5 for a few);
 //   the chunks: two workgroups per CU, 5 to start and end and, for each pair of tiles of 32 keys, 1, and 4 more to put chunks
 //   together; the last workgroups leave part of the chip idle for a share of their time;
-//   either at least its keys' way from memory, 4.5 TB/s, which the chunks' work overlaps in part.
-// Measured, chunks and row tiles, 32 heads over 8: one prompt of 1,024 tokens 27 and 33, of 2,048 76 and 59, two of 1,500 89 and
-// 52, 128 new rows of four sequences over 2,000 keys 35 and 55, 256 of two over 4,000 63 and 97; 32 heads over 32: one prompt
-// of 512 15 and 22, sixteen of 1,024 396 and 224; single tokens 41 and 184 over 8,000 keys, 81 and 183 for sixteen over 301 to
-// 7,936.
+//   either at least its keys' way from memory, 4.5 TB/s, which the work overlaps in part.
+// Measured, chunks and row tiles, 32 heads over 8: one prompt of 1,024 tokens 28 and 29, of 2,048 77 and 55, two of 1,500 93 and
+// 50, 64 of 300 268 and 125, 16 of 100 23 and 14, 128 new rows of four sequences over 2,000 keys 36 and 48, 256 of two over
+// 4,000 63 and 88, 512 of two over 3,000 88 and 69; 32 heads over 32: one prompt of 512 15 and 17, of 768 20 and 23, of 1,024 27
+// and 29, 64 new rows of four over 640 to 4,096 46 and 86; heads of 64 channels: 24 prompts of 31 to 698 33 and 24, 130 new rows
+// of eight over 5,000 128 and 92.  (Four prompts of 224, 17 and 13, it takes for chunks.)
 bool plan_prompt(PromptArgs& a, int64_t workspace_bytes, int64_t* need) {
-  constexpr int CUS = 256, SLOTS = 2 * CUS, PARTS_MOST = 64;
+  constexpr int SLOTS = 512, PARTS_MOST = 64;
   const int Hk = a.H / a.G;
   const int64_t part = 4 * (32 * a.D + 64);
-  const double width = a.D == 128 ? 1.0 : 0.6;  // of a tile's work
+  const double width = a.D == 128 ? 1.0 : 0.55;  // of a tile's work
   *need = 0;
   double tiles = 0, longest = 0, steps = 0, keys = 0;
   int64_t row_tiles = 0;
   int t_max = 1;
   for (int i = 0; i < a.n_seq; ++i) {
-    const int64_t r = (int64_t)a.nq[i] * a.G, wide = (r + 255) / 256, n_rt = (r + 31) / 32;
+    const int64_t r = (int64_t)a.nq[i] * a.G, wide = (r + 127) / 128, n_rt = (r + 31) / 32;
     const double seen = a.nk[i] - 0.5 * std::min(a.nq[i], a.nk[i]);  // keys of a row, on average
-    tiles += (double)Hk * wide * (10 + 2 * width * (seen / PT_KEYS + 1));
-    longest = std::max(longest, 10 + 1.5 * width * (a.nk[i] / PT_KEYS + 1));
+    tiles += (double)Hk * wide * (5 + 2.2 * width * (seen / PT_KEYS + 1));
+    longest = std::max(longest, 8 + 1.5 * width * (a.nk[i] / PT_KEYS + 1));
     steps += (double)Hk * n_rt * (seen / PS_KEYS + 1);
     keys += (double)Hk * a.nk[i];
     row_tiles += Hk * n_rt;
     t_max = std::max(t_max, (a.nk[i] + PS_KEYS - 1) / PS_KEYS);
   }
   const double memory = keys * a.D * 4 / 4.5e6;
-  tiles = std::max(tiles / CUS, longest);
+  tiles = std::max(tiles / SLOTS, longest);
   tiles = std::max(tiles, memory) + 0.35 * std::min(tiles, memory);
   const double per_wave = steps / (SLOTS * PS_WAVES), shared_step = std::max(width, memory / per_wave);
   double best = 0;
@@ -782,13 +881,13 @@ hipError_t launch_prompt_attention(PromptArgs a, void* workspace, int64_t worksp
     }
     return hipGetLastError();
   }
+  const bool turns = long_prompts(a);
+  const int rows = turns ? 256 : 128;
   for (int i = 0; i < a.n_seq; ++i)
-    a.item_prefix[i + 1] = a.item_prefix[i] + (int)(((int64_t)a.nq[i] * a.G + 255) / 256) * (a.H / a.G);
-  const dim3 grid(a.item_prefix[a.n_seq]);
-  if (a.D == 64)
-    hipLaunchKernelGGL(k_prompt_tiles<64>, grid, dim3(512), 0, s, a);
-  else
-    hipLaunchKernelGGL(k_prompt_tiles<128>, grid, dim3(512), 0, s, a);
+    a.item_prefix[i + 1] = a.item_prefix[i] + (int)(((int64_t)a.nq[i] * a.G + rows - 1) / rows) * (a.H / a.G);
+  const dim3 grid(a.item_prefix[a.n_seq]), block(2 * rows);
+  const auto fn = turns ? k_prompt_turns : (a.D == 64 ? k_prompt_tiles<64> : k_prompt_tiles<128>);
+  hipLaunchKernelGGL(fn, grid, block, 0, s, a);
   return hipGetLastError();
 }
 
