@@ -310,10 +310,18 @@ void fsx_backbone_destroy(fsx_backbone* bb);
 /* ---- Whole prompts: a cache rebuilt from scratch (Sec. 3.3: on an instruction change, a notice, an episode's end, or a
  * history at the training window) ----
  * Packed rows: the rows of several sequences (agents) lie in one tensor, sequence i in rows start[i] .. start[i] + len[i] - 1
- * (HOST arrays).  The ranges need not touch or be in order; rows outside them are not touched. */
+ * (HOST arrays; at most 2^24 rows each).  The ranges need not touch or be in order; rows outside them are not touched. */
 
 /* The tensors of fsx_prompt_attention: element (row r, head h, channel c) of X is X[r * X_row + h * X_head + c].  Strides are
- * in elements, multiples of 8; buffers are 16-byte aligned. */
+ * in elements, multiples of 8 (k_row and v_row at most 2^27: FSX_E_UNSUPPORTED beyond); buffers are 16-byte aligned; the rows and
+ * heads of out must not overlap. */
+/* Kernels of fsx_prompt_attention (fsx_prompt_desc.kernel). */
+enum {
+  FSX_PROMPT_AUTO = 0,   /* by what each would take */
+  FSX_PROMPT_CHUNKS = 1, /* 32 rows to a workgroup, the keys in chunks where there is a workspace: few rows */
+  FSX_PROMPT_TILES = 2,  /* 128 rows to a workgroup */
+  FSX_PROMPT_TURNS = 3   /* 256 rows to a workgroup (head_dim 128; FSX_E_UNSUPPORTED otherwise): long prompts */
+};
 typedef struct {
   int32_t n_heads;      /* query heads */
   int32_t n_kv_heads;   /* key / value heads, a divisor of n_heads: query head h reads head h / (n_heads / n_kv_heads) */
@@ -321,12 +329,14 @@ typedef struct {
   int32_t q_dtype;      /* FSX_BF16, or FSX_F32 (rounded to bf16 as they are read); keys and values are FSX_BF16 */
   int32_t out_dtype;    /* FSX_BF16 or FSX_F32 */
   float scale;          /* scores = scale * q.k, > 0; 0 = 1 / sqrt(head_dim) */
+  int32_t kernel;       /* FSX_PROMPT_AUTO, or one of the kernels whatever the sizes */
   int64_t q_rows;       /* rows that q, out and lse hold */
   int64_t k_rows;       /* rows that k and v hold */
   int64_t q_row, q_head, k_row, k_head, v_row, v_head, out_row, out_head;
 } fsx_prompt_desc;
 
-/* Causal attention of n_seq packed sequences (1..FSX_MAX_BATCH) in one call.
+/* Causal attention of n_seq packed sequences (1..FSX_MAX_BATCH) in one call; query rows times n_heads at most 2^30
+ * (FSX_E_UNSUPPORTED beyond).
  * Sequence i has q_len[i] new tokens, the last ones of its k_len[i] keys: new token t sees the keys
  * j <= k_len[i] - q_len[i] + t.  k_len == q_len is a whole prompt, k_len > q_len new rows over a history (q_len = 1: the next
  * token); a token before the first key (k_len < q_len) sees nothing, its output is 0 and its lse -infinity.  Masked keys and

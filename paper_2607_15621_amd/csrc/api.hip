@@ -918,6 +918,8 @@ static int check_prompt_desc(const fsx_prompt_desc* d) {
   if (d->head_dim != 64 && d->head_dim != 128) return fail(FSX_E_UNSUPPORTED, "head_dim must be 64 or 128");
   if ((d->q_dtype != FSX_BF16 && d->q_dtype != FSX_F32) || (d->out_dtype != FSX_BF16 && d->out_dtype != FSX_F32))
     return fail(FSX_E_UNSUPPORTED, "q and out must be BF16 or F32");
+  if (d->kernel < FSX_PROMPT_AUTO || d->kernel > FSX_PROMPT_TURNS) return fail(FSX_E_INVALID, "kernel must be one of FSX_PROMPT_*");
+  if (d->kernel == FSX_PROMPT_TURNS && d->head_dim != 128) return fail(FSX_E_UNSUPPORTED, "FSX_PROMPT_TURNS needs a head_dim of 128");
   if (!(d->scale >= 0.f) || d->scale > 1e30f) return fail(FSX_E_INVALID, "scale must be positive, or 0 for 1 / sqrt(head_dim)");
   if (d->q_rows < 0 || d->k_rows < 0 || d->q_rows > (int64_t)1 << 40 || d->k_rows > (int64_t)1 << 40)
     return fail(FSX_E_INVALID, "q_rows and k_rows must be in 0..2^40");
@@ -969,7 +971,7 @@ extern "C" int fsx_prompt_attention_workspace(const fsx_prompt_desc* desc, int32
     if (q_len[i] < 0 || q_len[i] > MAX_PROMPT || k_len[i] < 0 || k_len[i] > MAX_PROMPT)
       return fail(FSX_E_INVALID, "length " + std::to_string(i) + " outside 0..2^24");
   PromptArgs a{};
-  a.H = desc->n_heads; a.G = desc->n_heads / desc->n_kv_heads; a.D = desc->head_dim;
+  a.H = desc->n_heads; a.G = desc->n_heads / desc->n_kv_heads; a.D = desc->head_dim; a.kernel = desc->kernel;
   prompt_sequences(a, n_seq, nullptr, q_len, nullptr, k_len);
   if (a.n_seq > 0) plan_prompt(a, INT64_MAX, bytes);
   g_err.clear();
@@ -1013,7 +1015,7 @@ extern "C" int fsx_prompt_attention(const fsx_prompt_desc* desc, const void* q, 
   a.q = q; a.k = (const uint16_t*)k; a.v = (const uint16_t*)v; a.out = out; a.lse = lse;
   a.q_row = d.q_row; a.q_head = d.q_head; a.k_row = d.k_row; a.k_head = d.k_head;
   a.v_row = d.v_row; a.v_head = d.v_head; a.o_row = d.out_row; a.o_head = d.out_head;
-  a.H = d.n_heads; a.G = d.n_heads / d.n_kv_heads; a.D = d.head_dim;
+  a.H = d.n_heads; a.G = d.n_heads / d.n_kv_heads; a.D = d.head_dim; a.kernel = d.kernel;
   a.q_f32 = d.q_dtype == FSX_F32; a.o_f32 = d.out_dtype == FSX_F32;
   a.c = (d.scale > 0.f ? d.scale : 1.0f / sqrtf((float)d.head_dim)) * LOG2E;
   prompt_sequences(a, n_seq, q_start, q_len, k_start, k_len);

@@ -337,9 +337,10 @@ __global__ __launch_bounds__(T) void k_replace_held(RowsArgs a) {
 }
 
 // Longer rows: the scales first, in a pass of their own, so these are read twice (four histories of fp32 rows, 2 layers: 362 us for
-// the scales and 460 for the codes, 5.6 TB/s both; written layer by layer in pieces of the memory-side cache's size 880).  They start at 0 (k_clear_scales); a workgroup takes a.block rows and 256 pieces of their width,
-// a thread the same piece of every row, and raises the scales of its heads (scale_of grows with the magnitude, and a maximum
-// does not depend on the order; positive floats compare as their bits).
+// the scales and 460 for the codes, 5.6 TB/s both; layer by layer, in pieces of the memory-side cache's size, 880 in all).  The
+// scales start at 0 (k_clear_scales); a workgroup takes a.block rows and 256 pieces of their width, a thread the same piece of
+// every row, and raises the scales of its heads (scale_of grows with the magnitude, and a maximum does not depend on the order;
+// positive floats compare as their bits).
 __global__ __launch_bounds__(256) void k_clear_scales(RowsArgs a) {
   const int i = blockIdx.x * 256 + threadIdx.x, H = a.cv.H, b = blockIdx.z, l = blockIdx.y;
   if (i >= 2 * H || a.n[b] == 0) return;

@@ -229,6 +229,7 @@ struct PromptArgs {
   int64_t q_row, q_head, k_row, k_head, v_row, v_head, o_row, o_head;  // elements
   int32_t H, G, D;      // query heads, query heads per key head, head width
   int32_t q_f32, o_f32;
+  int32_t kernel;       // FSX_PROMPT_*
   float c;              // scores in log2 units = c * q.k
   int32_t n_seq;
   int64_t q0[FSX_MAX_BATCH], k0[FSX_MAX_BATCH];

@@ -11,12 +11,11 @@
 
 namespace fsx {
 
-
 // The rows of a (sequence, key head) are its tokens' query heads of that key head, token by token: row r is token r / G, head
 // r % G of the group, so all query heads that share keys read them from one tile.
 //
-// A workgroup takes NW * 32 rows, a wave 32 of them, and walks over the keys in tiles of 64 that direct loads bring into LDS
-// one tile ahead.  Everything is held transposed, a query per lane column:
+// A wave takes 32 rows and walks over the keys in tiles that direct loads bring into LDS ahead of it; the waves of a workgroup share
+// them.  Everything is held transposed, a query per lane column:
 //   S^T = K Q^T   32x32x16 MFMA, A = 32 keys x 16 channels from LDS, B = the wave's queries, kept in registers;
 //   a lane then has 16 of 32 keys' scores of one query (lane l and l ^ 32 share query l % 32), so maximum and sum are lane
 //   operations and one exchange of halves;
@@ -811,13 +810,12 @@ static bool long_prompts(const PromptArgs& a) {
 // and 29, 64 new rows of four over 640 to 4,096 46 and 86; heads of 64 channels: 24 prompts of 31 to 698 33 and 24, 130 new rows
 // of eight over 5,000 128 and 92.  (Four prompts of 224, 17 and 13, it takes for chunks.)
 bool plan_prompt(PromptArgs& a, int64_t workspace_bytes, int64_t* need) {
-  constexpr int SLOTS = 512, PARTS_MOST = 64;
+  constexpr int SLOTS = 512;
   const int Hk = a.H / a.G;
   const int64_t part = 4 * (32 * a.D + 64);
   const double width = a.D == 128 ? 1.0 : 0.55;  // of a tile's work
   *need = 0;
   double tiles = 0, longest = 0, steps = 0, keys = 0;
-  int64_t row_tiles = 0;
   int t_max = 1;
   for (int i = 0; i < a.n_seq; ++i) {
     const int64_t r = (int64_t)a.nq[i] * a.G, wide = (r + 127) / 128, n_rt = (r + 31) / 32;
@@ -826,7 +824,6 @@ bool plan_prompt(PromptArgs& a, int64_t workspace_bytes, int64_t* need) {
     longest = std::max(longest, 8 + 1.5 * width * (a.nk[i] / PT_KEYS + 1));
     steps += (double)Hk * n_rt * (seen / PS_KEYS + 1);
     keys += (double)Hk * a.nk[i];
-    row_tiles += Hk * n_rt;
     t_max = std::max(t_max, (a.nk[i] + PS_KEYS - 1) / PS_KEYS);
   }
   const double memory = keys * a.D * 4 / 4.5e6;
@@ -834,7 +831,7 @@ bool plan_prompt(PromptArgs& a, int64_t workspace_bytes, int64_t* need) {
   tiles = std::max(tiles, memory) + 0.35 * std::min(tiles, memory);
   const double per_wave = steps / (SLOTS * PS_WAVES), shared_step = std::max(width, memory / per_wave);
   double best = 0;
-  for (int k = 1; k <= PARTS_MOST; ++k) {
+  for (const int k : {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 48, 64}) {  // chunks of the longest keys
     const int chunk = std::max(2 * PS_WAVES, (t_max + k - 1) / k);
     int64_t items = 0;
     bool split = false;
@@ -843,7 +840,7 @@ bool plan_prompt(PromptArgs& a, int64_t workspace_bytes, int64_t* need) {
       items += (int64_t)n_rt * Hk * n;
       split = split || n > 1;
     }
-    if (split && items * part > workspace_bytes) break;
+    if (split && (items * part > workspace_bytes || items > INT32_MAX)) break;
     const double rounds = std::max(1.0, (double)items / SLOTS), pair = (double)chunk / PS_WAVES;
     const double work = 5 * rounds + width * (rounds > 1 ? std::max(per_wave, pair) : pair);
     const double tail = rounds > 1 ? 0.15 * pair : 0.4 * std::max(0.0, pair - steps / items / PS_WAVES);
@@ -853,7 +850,7 @@ bool plan_prompt(PromptArgs& a, int64_t workspace_bytes, int64_t* need) {
     a.chunk = chunk;
     *need = split ? items * part : 0;
   }
-  if (tiles <= best || row_tiles * PARTS_MOST > INT32_MAX) {
+  if (a.kernel == FSX_PROMPT_AUTO ? tiles <= best : a.kernel != FSX_PROMPT_CHUNKS) {
     *need = 0;
     return false;
   }
@@ -881,7 +878,7 @@ hipError_t launch_prompt_attention(PromptArgs a, void* workspace, int64_t worksp
     }
     return hipGetLastError();
   }
-  const bool turns = long_prompts(a);
+  const bool turns = a.kernel == FSX_PROMPT_AUTO ? long_prompts(a) : a.kernel == FSX_PROMPT_TURNS;
   const int rows = turns ? 256 : 128;
   for (int i = 0; i < a.n_seq; ++i)
     a.item_prefix[i + 1] = a.item_prefix[i] + (int)(((int64_t)a.nq[i] * a.G + rows - 1) / rows) * (a.H / a.G);

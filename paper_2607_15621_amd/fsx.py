@@ -22,6 +22,7 @@ APPEND_RING, APPEND_ERROR = 0, 1
 CACHE_HEAD_MAJOR, CACHE_TOKEN_MAJOR, CACHE_SHARED = 0, 1, 2
 FLAG_GENERIC, FLAG_MULTI_LAUNCH, FLAG_TRACE = 1, 2, 4
 HEAD_MEAN_LINEAR, HEAD_QUERY_MLP = 0, 1
+PROMPT_AUTO, PROMPT_CHUNKS, PROMPT_TILES, PROMPT_TURNS = 0, 1, 2, 3
 MAX_BATCH = 64
 STATUS = {0: "FSX_OK", 1: "FSX_E_INVALID", 2: "FSX_E_UNSUPPORTED", 3: "FSX_E_CAPACITY", 4: "FSX_E_OOM",
           5: "FSX_E_HIP"}
@@ -73,7 +74,8 @@ class LoopTickInfo(ctypes.Structure):
 
 class PromptDesc(ctypes.Structure):
     _fields_ = [("n_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
-                ("q_dtype", ctypes.c_int32), ("out_dtype", ctypes.c_int32), ("scale", ctypes.c_float)] + \
+                ("q_dtype", ctypes.c_int32), ("out_dtype", ctypes.c_int32), ("scale", ctypes.c_float),
+                ("kernel", ctypes.c_int32)] + \
                [(n, ctypes.c_int64) for n in ("q_rows", "k_rows", "q_row", "q_head", "k_row", "k_head", "v_row", "v_head",
                                               "out_row", "out_head")]
 
@@ -329,7 +331,7 @@ def _dtype_of(t) -> int:
     return _dtypes[t.dtype]
 
 
-def _prompt_desc(q, k, v, out, scale: float) -> PromptDesc:
+def _prompt_desc(q, k, v, out, scale: float, kernel: int) -> PromptDesc:
     """Tensors [rows][heads][head_dim], their last dimension dense."""
     for t in (q, k, v, out):
         if t.dim() != 3 or (t.stride(2) != 1 and t.numel()):
@@ -338,12 +340,12 @@ def _prompt_desc(q, k, v, out, scale: float) -> PromptDesc:
         raise ValueError("k and v, q and out must have the same shapes, and all one head_dim")
     if _dtype_of(k) != BF16 or _dtype_of(v) != BF16:
         raise ValueError("k and v must be bfloat16")
-    return PromptDesc(q.shape[1], k.shape[1], q.shape[2], _dtype_of(q), _dtype_of(out), scale, q.shape[0], k.shape[0],
+    return PromptDesc(q.shape[1], k.shape[1], q.shape[2], _dtype_of(q), _dtype_of(out), scale, kernel, q.shape[0], k.shape[0],
                       *q.stride()[:2], *k.stride()[:2], *v.stride()[:2], *out.stride()[:2])
 
 
 def prompt_attention(q, k, v, out, q_rows: PackedRows, k_rows: Optional[PackedRows] = None, scale: float = 0.0, lse=None,
-                     workspace=None, stream=None):
+                     workspace=None, stream=None, kernel: int = PROMPT_AUTO):
     """fsx_prompt_attention: causal attention of packed sequences.  q, out [rows][n_heads][head_dim], k, v
     [rows][n_kv_heads][head_dim] (any row and head strides); lse [rows][n_heads] float32, dense, or None; workspace a
     device tensor of prompt_attention_workspace bytes, or None (keys are then not split over workgroups)."""
@@ -351,7 +353,7 @@ def prompt_attention(q, k, v, out, q_rows: PackedRows, k_rows: Optional[PackedRo
         raise ValueError("lse must be a dense float32 [rows][n_heads]")
     if k_rows is not None and k_rows.n != q_rows.n:
         raise ValueError("as many sequences of keys as of queries")
-    d = _prompt_desc(q, k, v, out, scale)
+    d = _prompt_desc(q, k, v, out, scale, kernel)
     _check(lib().fsx_prompt_attention(ctypes.byref(d), _ptr(q), _ptr(k), _ptr(v), _ptr(out), _ptr(lse), q_rows.n,
                                       q_rows.c_start, q_rows.c_len, k_rows.c_start if k_rows is not None else None,
                                       k_rows.c_len if k_rows is not None else None, _ptr(workspace),
@@ -359,11 +361,11 @@ def prompt_attention(q, k, v, out, q_rows: PackedRows, k_rows: Optional[PackedRo
                                       _stream(stream)))
 
 
-def prompt_attention_workspace(q, k, q_rows: PackedRows, k_rows: Optional[PackedRows] = None) -> int:
+def prompt_attention_workspace(q, k, q_rows: PackedRows, k_rows: Optional[PackedRows] = None, kernel: int = PROMPT_AUTO) -> int:
     """fsx_prompt_attention_workspace: bytes of the workspace that the call can use (0: none)."""
     if k_rows is not None and k_rows.n != q_rows.n:
         raise ValueError("as many sequences of keys as of queries")
-    d, need = _prompt_desc(q, k, k, q, 0.0), ctypes.c_int64()
+    d, need = _prompt_desc(q, k, k, q, 0.0, kernel), ctypes.c_int64()
     _check(lib().fsx_prompt_attention_workspace(ctypes.byref(d), q_rows.n, q_rows.c_len,
                                                 k_rows.c_len if k_rows is not None else None, ctypes.byref(need)))
     return need.value

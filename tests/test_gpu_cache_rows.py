@@ -54,7 +54,8 @@ def scale_of(x, headroom):
 
 
 def codes_of(x, scale):
-    q = torch.from_numpy(x.numpy() / scale.numpy()[None, :, None])  # one fp32 division, correctly rounded
+    with np.errstate(invalid="ignore"):
+        q = torch.from_numpy(x.numpy() / scale.numpy()[None, :, None])  # one fp32 division, correctly rounded
     code = q.clamp(-448.0, 448.0).to(FP8).view(U8)
     return torch.where(q.isnan(), torch.where(torch.signbit(q), 0xFF, 0x7F).to(U8), code)
 
@@ -185,6 +186,23 @@ def test_quotients_next_to_a_border_of_two_codes(top):
         flat[:len(rows)] = rows.clamp(-head, head)
         v[0, 1:, h] = flat.view(63, 128)
     replace_and_check(r, (64,), [v, -v])
+
+
+@pytest.mark.parametrize("source", [BF16, F32])
+@pytest.mark.parametrize("lens", [(60, 0, 64), (300, 0, 250), (700, 0, 1000)], ids=str)
+def test_more_heads_than_workgroups(lens, source):
+    """Workgroups go from one head's rows to the next; some of the rows hold what is not finite, some only zeros or tiny ones."""
+    L, H, D = 3, 96, 64
+    r = Rings([0] * 3, max(lens), L=L, H=H, D=D, layout=TOKEN)
+    rows = packed_rows(L, sum(lens), H, D, source, seed=sum(lens))
+    g = torch.Generator().manual_seed(1)
+    for t in rows:
+        for value in (float("nan"), float("inf"), -float("inf")):
+            at = [torch.randint(0, n, (20,), generator=g) for n in t.shape]
+            t[tuple(at)] = value
+        t[1, :, 5:60:7] = 0
+        t[2, :, 3:90:11] *= 1e-30
+    replace_and_check(r, lens, rows)
 
 
 @pytest.mark.parametrize("shape", [(1, 1, 1), (1, 2, 3), (3, 1, 40), (16, 1, 5)])

@@ -12,7 +12,7 @@ INVALID, UNSUPPORTED, CAPACITY = 1, 2, 3
 
 
 def desc(**kw):
-    d = dict(n_heads=4, n_kv_heads=2, head_dim=128, q_dtype=fsx.BF16, out_dtype=fsx.BF16, scale=0.0, q_rows=100, k_rows=200,
+    d = dict(n_heads=4, n_kv_heads=2, head_dim=128, q_dtype=fsx.BF16, out_dtype=fsx.BF16, scale=0.0, kernel=0, q_rows=100, k_rows=200,
              q_row=512, q_head=128, k_row=256, k_head=128, v_row=256, v_head=128, out_row=512, out_head=128)
     d.update(kw)
     return fsx.PromptDesc(*(d[n] for n, _ in fsx.PromptDesc._fields_))
@@ -31,7 +31,8 @@ def attend(d=None, q=PTR, k=PTR, v=PTR, out=PTR, q_rows=((0, 30), (30, 70)), k_r
     (dict(n_kv_heads=3), INVALID, "n_kv_heads"), (dict(n_heads=0), INVALID, "n_heads"), (dict(n_heads=2000), INVALID, "n_heads"),
     (dict(head_dim=96), UNSUPPORTED, "head_dim"), (dict(q_dtype=fsx.FP8_E4M3), UNSUPPORTED, "q and out"),
     (dict(out_dtype=7), UNSUPPORTED, "q and out"), (dict(scale=-1.0), INVALID, "scale"), (dict(scale=float("nan")), INVALID, "scale"),
-    (dict(scale=float("inf")), INVALID, "scale"), (dict(q_row=516), INVALID, "strides"), (dict(k_head=-8), INVALID, "strides"),
+    (dict(scale=float("inf")), INVALID, "scale"), (dict(kernel=4), INVALID, "kernel"), (dict(kernel=-1), INVALID, "kernel"),
+    (dict(kernel=3, head_dim=64), UNSUPPORTED, "TURNS"), (dict(k_row=1 << 28), UNSUPPORTED, "2^27"), (dict(q_row=516), INVALID, "strides"), (dict(k_head=-8), INVALID, "strides"),
     (dict(v_row=1 << 62), INVALID, "strides"), (dict(out_head=64), INVALID, "overlap"), (dict(out_row=504), INVALID, "overlap"),
     (dict(out_row=128, out_head=12792), INVALID, "overlap"), (dict(out_row=0), INVALID, "overlap"), (dict(q_rows=-1), INVALID, "q_rows"),
     (dict(q_rows=99), INVALID, "queries"), (dict(k_rows=199), INVALID, "keys")])
