@@ -322,26 +322,28 @@ _dtypes = {}
 
 
 def _dtype_of(t) -> int:
-    if not _dtypes:
+    code = _dtypes.get(t.dtype)
+    if code is None:
         import torch
 
         _dtypes.update({torch.float32: F32, torch.bfloat16: BF16})
-    if t.dtype not in _dtypes:
-        raise ValueError(f"tensors of dtype {t.dtype} are not taken here: float32 or bfloat16")
-    return _dtypes[t.dtype]
+        code = _dtypes.get(t.dtype)
+        if code is None:
+            raise ValueError(f"tensors of dtype {t.dtype} are not taken here: float32 or bfloat16")
+    return code
 
 
 def _prompt_desc(q, k, v, out, scale: float, kernel: int) -> PromptDesc:
     """Tensors [rows][heads][head_dim], their last dimension dense."""
-    for t in (q, k, v, out):
-        if t.dim() != 3 or (t.stride(2) != 1 and t.numel()):
-            raise ValueError("q, k, v and out must be [rows][heads][head_dim] with a dense last dimension")
-    if k.shape != v.shape or q.shape != out.shape or q.shape[2] != k.shape[2]:
-        raise ValueError("k and v, q and out must have the same shapes, and all one head_dim")
+    sq, sk, so, tq, tk, tv, to = q.shape, k.shape, out.shape, q.stride(), k.stride(), v.stride(), out.stride()
+    if len(sq) != 3 or len(sk) != 3 or sk != v.shape or sq != so or sq[2] != sk[2]:
+        raise ValueError("q and out must be [rows][heads][head_dim], k and v too, with as many channels")
+    if not tq[2] == tk[2] == tv[2] == to[2] == 1:
+        raise ValueError("q, k, v and out must have a dense last dimension")
     if _dtype_of(k) != BF16 or _dtype_of(v) != BF16:
         raise ValueError("k and v must be bfloat16")
-    return PromptDesc(q.shape[1], k.shape[1], q.shape[2], _dtype_of(q), _dtype_of(out), scale, kernel, q.shape[0], k.shape[0],
-                      *q.stride()[:2], *k.stride()[:2], *v.stride()[:2], *out.stride()[:2])
+    return PromptDesc(sq[1], sk[1], sq[2], _dtype_of(q), _dtype_of(out), scale, kernel, sq[0], sk[0], tq[0], tq[1], tk[0], tk[1],
+                      tv[0], tv[1], to[0], to[1])
 
 
 def prompt_attention(q, k, v, out, q_rows: PackedRows, k_rows: Optional[PackedRows] = None, scale: float = 0.0, lse=None,
@@ -375,12 +377,15 @@ def _row_tensors(cache: CacheDesc, n_layers: int, k_rows, v_rows, rows: PackedRo
     """Dtype and total rows of packed rows [n_layers][total_rows][H][Dh] (either tensor may be None)."""
     if rows.n != cache.c.batch:
         raise ValueError("rows of every agent of the cache")
-    given = [t for t in (k_rows, v_rows) if t is not None]
-    for t in given:
-        if t.dim() != 4 or not t.is_contiguous() or t.shape != given[0].shape or t.dtype != given[0].dtype or \
-                tuple(t.shape[2:]) != (cache.c.n_heads, cache.c.head_dim) or t.shape[0] != n_layers:
-            raise ValueError("packed rows must be dense [n_layers][rows][n_heads][head_dim] tensors of one dtype")
-    return (_dtype_of(given[0]), given[0].shape[1]) if given else (BF16, int((rows.start + rows.len).max(initial=0)))
+    some = k_rows if k_rows is not None else v_rows
+    if some is None:
+        return BF16, int((rows.start + rows.len).max(initial=0))
+    shape = some.shape
+    if len(shape) != 4 or shape[0] != n_layers or shape[2] != cache.c.n_heads or shape[3] != cache.c.head_dim or \
+            not some.is_contiguous() or \
+            (v_rows is not None and (v_rows.shape != shape or v_rows.dtype != some.dtype or not v_rows.is_contiguous())):
+        raise ValueError("packed rows must be dense [n_layers][rows][n_heads][head_dim] tensors of one dtype")
+    return _dtype_of(some), shape[1]
 
 
 def cache_replace_rows(cache: CacheDesc, layer: int, n_layers: int, k_rows, v_rows, rows: PackedRows, headroom: float = 1.0,
