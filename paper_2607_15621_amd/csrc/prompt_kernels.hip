@@ -47,6 +47,7 @@ __device__ __forceinline__ int v_turn(int row) { return D == 128 ? 2 * (row & 7)
 
 // Sequence and place in it of item i, items of sequence s being prefix[s] .. prefix[s + 1] - 1.
 __device__ __forceinline__ int find_seq(const int32_t* prefix, int n_seq, int i, int lane) {
+  if (n_seq == 1) return 0;  // (arguments are cold in every launch: a round trip of about a microsecond)
   return __popcll(__ballot(lane < n_seq && prefix[min(lane + 1, FSX_MAX_BATCH)] <= i));
 }
 
@@ -319,10 +320,14 @@ __device__ __forceinline__ uint32_t lds_address(const void* p) {
   return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)p;
 }
 
-// Four waves take 128 rows and walk over the keys in step, one tile ahead; two such workgroups share a CU, and one
-// starts or ends while the other computes.
+// Four waves take 128 rows and walk over the keys in step, one tile ahead; two such workgroups share a CU (three with heads of 64
+// channels: 16 prompts of 1,024 tokens 119 us with two, 105 with three, 145 with four, which spill), and one starts or ends while
+// the other computes.
+// Bound: LDS.  Of a tile a wave reads 32 KB for 32 products' 1,024 cycles, the transposing reads at half the rate of the others, and the
+// tiles are written besides: 2,000 of the 4,100 cycles that two workgroups take for a tile each, beside 2,048 of products; without LDS
+// reads and tile loads the longest prompt took 1,210 us instead of 1,890.
 template <int D>
-__global__ __launch_bounds__(256, 2) void k_prompt_tiles(PromptArgs a) {
+__global__ __launch_bounds__(256, D == 64 ? 3 : 2) void k_prompt_tiles(PromptArgs a) {
   constexpr int NW = 4, RB = 2 * D, TILE = PT_KEYS * RB, RPI = 1024 / RB, NI = PT_KEYS / RPI / NW;  // rows and loads per wave's load
   __shared__ __align__(1024) char kt[2 * TILE], vt[2 * TILE];
   __shared__ int again, first_bad[3 * D];
@@ -813,7 +818,7 @@ bool plan_prompt(PromptArgs& a, int64_t workspace_bytes, int64_t* need) {
   constexpr int SLOTS = 512;
   const int Hk = a.H / a.G;
   const int64_t part = 4 * (32 * a.D + 64);
-  const double width = a.D == 128 ? 1.0 : 0.55;  // of a tile's work
+  const double width = a.D == 128 ? 1.0 : 0.5;  // of a tile's work
   *need = 0;
   double tiles = 0, longest = 0, steps = 0, keys = 0;
   int t_max = 1;
