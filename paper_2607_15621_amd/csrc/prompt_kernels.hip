@@ -45,11 +45,28 @@ __device__ __forceinline__ int k_turn(int row) { return D == 128 ? row & 15 : (r
 template <int D>
 __device__ __forceinline__ int v_turn(int row) { return D == 128 ? 2 * (row & 7) : 2 * (row & 3); }
 
-// Sequence and place in it of item i, items of sequence s being prefix[s] .. prefix[s + 1] - 1.
-__device__ __forceinline__ int find_seq(const int32_t* prefix, int n_seq, int i, int lane) {
-  if (n_seq == 1) return 0;  // (arguments are cold in every launch: a round trip of about a microsecond)
-  return __popcll(__ballot(lane < n_seq && prefix[min(lane + 1, FSX_MAX_BATCH)] <= i));
-}
+// The sequence of item i (items of sequence s being prefix[s] .. prefix[s + 1] - 1) and the item's place in it.  One sequence
+// per lane: a round trip for all of it; loaded by sequence they were two or three more, a microsecond each, the arguments being cold in
+// every launch (one row of 16 sequences, up to 8k keys: 64.6 -> 61.8 us; four of 64 over long histories 46.6 -> 44.4).
+struct PromptSeq {
+  int place, nq, nk, n_split, first_item;
+  int64_t q0, k0;
+  __device__ __forceinline__ PromptSeq(const PromptArgs& a, const int32_t* prefix, int i, int lane) {
+    static_assert(FSX_MAX_BATCH == WAVE, "a sequence per lane");
+    const int at = prefix[lane], end = prefix[lane + 1], items = a.item_prefix[lane], q = a.nq[lane], k = a.nk[lane], n = a.n_split[lane];
+    const int64_t qs = a.q0[lane], ks = a.k0[lane];
+    const int s = __popcll(__ballot(lane < a.n_seq && end <= i));
+    auto pick = [&](int v) { return __builtin_amdgcn_readlane(v, s); };
+    auto pick64 = [&](int64_t v) { return (int64_t)((uint64_t)(uint32_t)pick((int)(v >> 32)) << 32 | (uint32_t)pick((int)v)); };
+    place = i - pick(at);
+    nq = pick(q);
+    nk = pick(k);
+    n_split = pick(n);
+    first_item = pick(items);
+    q0 = pick64(qs);
+    k0 = pick64(ks);
+  }
+};
 
 // max / sum with lane l ^ 32
 __device__ __forceinline__ float half_max(float v) {
@@ -291,10 +308,10 @@ struct PromptRows {
   int h, lim;   // query head; last key seen
   bool valid;
   int first, last;  // least and largest last key of the wave's rows (none: INT32_MAX, -1)
-  __device__ __forceinline__ PromptRows(const PromptArgs& a, int s, int hk, int r0, int lane) {
-    const int rows = a.nq[s] * a.G, off = a.nk[s] - a.nq[s], r = r0 + (lane & 31), rc = min(r, rows - 1), t = rc / a.G;
+  __device__ __forceinline__ PromptRows(const PromptArgs& a, const PromptSeq& s, int hk, int r0, int lane) {
+    const int rows = s.nq * a.G, off = s.nk - s.nq, r = r0 + (lane & 31), rc = min(r, rows - 1), t = rc / a.G;
     valid = r < rows;
-    row = a.q0[s] + t;
+    row = s.q0 + t;
     h = hk * a.G + rc - t * a.G;
     lim = off + t;
     first = r0 < rows ? off + r0 / a.G : INT32_MAX;
@@ -324,25 +341,25 @@ __device__ __forceinline__ uint32_t lds_address(const void* p) {
 // channels: 16 prompts of 1,024 tokens 119 us with two, 105 with three, 145 with four, which spill), and one starts or ends while
 // the other computes.
 // Bound: LDS.  Of a tile a wave reads 32 KB for 32 products' 1,024 cycles, the transposing reads at half the rate of the others, and the
-// tiles are written besides: 2,000 of the 4,100 cycles that two workgroups take for a tile each, beside 2,048 of products; without LDS
-// reads and tile loads the longest prompt took 1,210 us instead of 1,890.
+// tiles are written besides: 2,000 of the 4,100 cycles that two workgroups take for a tile each, beside 2,048 of products; in k_prompt_turns,
+// whose reads are the same, the longest prompt took 1,210 us instead of 1,890 without LDS reads and tile loads.
 template <int D>
 __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void k_prompt_tiles(PromptArgs a) {
   constexpr int NW = 4, RB = 2 * D, TILE = PT_KEYS * RB, RPI = 1024 / RB, NI = PT_KEYS / RPI / NW;  // rows and loads per wave's load
   __shared__ __align__(1024) char kt[2 * TILE], vt[2 * TILE];
   __shared__ int again, first_bad[3 * D];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
-  const int s = find_seq(a.item_prefix, a.n_seq, blockIdx.x, lane);
-  const int in_seq = blockIdx.x - a.item_prefix[s], Hk = a.H / a.G;
-  const int nk = a.nk[s], rows = a.nq[s] * a.G, tiles = (rows + NW * 32 - 1) / (NW * 32);
+  const PromptSeq s(a, a.item_prefix, blockIdx.x, lane);
+  const int in_seq = s.place, Hk = a.H / a.G;
+  const int nk = s.nk, rows = s.nq * a.G, tiles = (rows + NW * 32 - 1) / (NW * 32);
   const int rt = __builtin_amdgcn_readfirstlane(in_seq / Hk), hk = in_seq - rt * Hk;
   const int r0 = (tiles - 1 - rt) * NW * 32;  // the rows with the most keys first
-  const int off = nk - a.nq[s], n_tiles = __builtin_amdgcn_readfirstlane(max(0, (off + (min(r0 + NW * 32, rows) - 1) / a.G + PT_KEYS) / PT_KEYS));
+  const int off = nk - s.nq, n_tiles = __builtin_amdgcn_readfirstlane(max(0, (off + (min(r0 + NW * 32, rows) - 1) / a.G + PT_KEYS) / PT_KEYS));
   if (threadIdx.x == 0) again = 0;
 
   const int lr = lane / (RB / 16), lp = lane % (RB / 16);
-  const uint16_t* kbase = a.k + a.k0[s] * a.k_row + hk * a.k_head;
-  const uint16_t* vbase = a.v + a.k0[s] * a.v_row + hk * a.v_head;
+  const uint16_t* kbase = a.k + s.k0 * a.k_row + hk * a.k_head;
+  const uint16_t* vbase = a.v + s.k0 * a.v_row + hk * a.v_head;
   const uint32_t kl = lds_address(kt), vl = lds_address(vt);
   // the lane's piece of a load, the same in all of a wave's loads
   const uint32_t kp = 16 * (lp ^ k_turn<D>(w * RPI + lr)), vp = 16 * (lp ^ v_turn<D>(w * RPI + lr));
@@ -416,17 +433,17 @@ __global__ __launch_bounds__(512, 2) void k_prompt_turns(PromptArgs a) {
   __shared__ int again, first_bad[3 * D];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
   const bool second = w >= NW / 2;
-  const int s = find_seq(a.item_prefix, a.n_seq, blockIdx.x, lane);
-  const int in_seq = blockIdx.x - a.item_prefix[s], Hk = a.H / a.G;
-  const int nk = a.nk[s], rows = a.nq[s] * a.G, tiles = (rows + NW * 32 - 1) / (NW * 32);
+  const PromptSeq s(a, a.item_prefix, blockIdx.x, lane);
+  const int in_seq = s.place, Hk = a.H / a.G;
+  const int nk = s.nk, rows = s.nq * a.G, tiles = (rows + NW * 32 - 1) / (NW * 32);
   const int hk = in_seq % Hk, r0 = (tiles - 1 - in_seq / Hk) * NW * 32;  // the rows with the most keys first
   const PromptRows pr(a, s, hk, r0 + 32 * w, lane);
-  const int off = nk - a.nq[s], n_tiles = max(0, (off + (min(r0 + NW * 32, rows) - 1) / a.G + PT_KEYS) / PT_KEYS);
+  const int off = nk - s.nq, n_tiles = max(0, (off + (min(r0 + NW * 32, rows) - 1) / a.G + PT_KEYS) / PT_KEYS);
   if (threadIdx.x == 0) again = 0;
 
   const int lr = lane / (RB / 16), lp = lane % (RB / 16);
-  const uint16_t* kbase = a.k + a.k0[s] * a.k_row + hk * a.k_head;
-  const uint16_t* vbase = a.v + a.k0[s] * a.v_row + hk * a.v_head;
+  const uint16_t* kbase = a.k + s.k0 * a.k_row + hk * a.k_head;
+  const uint16_t* vbase = a.v + s.k0 * a.v_row + hk * a.v_head;
   const uint32_t kl = lds_address(kt), vl = lds_address(vt);
   // the lane's piece of a load, the same in all of a wave's loads
   const uint32_t kp = 16 * (lp ^ k_turn<D>(w * RPI + lr)), vp = 16 * (lp ^ v_turn<D>(w * RPI + lr));
@@ -596,9 +613,9 @@ __global__ __launch_bounds__(PS_WAVES * 64, 1) void k_prompt_split(PromptArgs a)
   __shared__ int first_bad[PS_WAVES][3 * D];
   __shared__ float sm[PS_WAVES][32], sl[PS_WAVES][32];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
-  const int s = find_seq(a.item_prefix, a.n_seq, blockIdx.x, lane);
-  const int Hk = a.H / a.G, nk = a.nk[s], rows = a.nq[s] * a.G, n_rt = (rows + 31) / 32;
-  int i = blockIdx.x - a.item_prefix[s];
+  const PromptSeq s(a, a.item_prefix, blockIdx.x, lane);
+  const int Hk = a.H / a.G, nk = s.nk, rows = s.nq * a.G, n_rt = (rows + 31) / 32;
+  int i = s.place;
   const int hk = i % Hk;
   i /= Hk;
   const int r0 = 32 * (n_rt - 1 - i % n_rt), split = i / n_rt;
@@ -609,8 +626,8 @@ __global__ __launch_bounds__(PS_WAVES * 64, 1) void k_prompt_split(PromptArgs a)
   load_queries<D>(a, pr.row * a.q_row + pr.h * a.q_head, half, qf);
 
   const int lr = lane / (RB / 16), lp = lane % (RB / 16);
-  const uint16_t* kbase = a.k + a.k0[s] * a.k_row + hk * a.k_head;
-  const uint16_t* vbase = a.v + a.k0[s] * a.v_row + hk * a.v_head;
+  const uint16_t* kbase = a.k + s.k0 * a.k_row + hk * a.k_head;
+  const uint16_t* vbase = a.v + s.k0 * a.v_row + hk * a.v_head;
   auto issue = [&](int j, char* kt, char* vt) {
 #pragma unroll
     for (int n = 0; n < NI; ++n) {
@@ -677,7 +694,7 @@ __global__ __launch_bounds__(PS_WAVES * 64, 1) void k_prompt_split(PromptArgs a)
     f[x] = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(sm[x][q] - m);
     l += sl[x][q] * f[x];
   }
-  const bool whole = a.n_split[s] == 1;
+  const bool whole = s.n_split == 1;
   const float inv = pr.lim >= 0 ? 1.f / l : 0.f;
   float* part = a.part + (int64_t)blockIdx.x * part_floats<D>();
 #pragma unroll
@@ -719,11 +736,11 @@ __global__ __launch_bounds__(2 * D * PM_GROUPS) void k_prompt_merge(PromptArgs a
   __shared__ float xm[PM_GROUPS - 1][32], xl[PM_GROUPS - 1][32];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, q = lane & 31;
   const int blk = w % NB, group = w / NB;
-  const int s = find_seq(a.merge_prefix, a.n_seq, blockIdx.x, lane);
-  const int Hk = a.H / a.G, n_rt = (a.nq[s] * a.G + 31) / 32, i = blockIdx.x - a.merge_prefix[s], hk = i % Hk;
+  const PromptSeq s(a, a.merge_prefix, blockIdx.x, lane);
+  const int Hk = a.H / a.G, n_rt = (s.nq * a.G + 31) / 32, i = s.place, hk = i % Hk;
   const PromptRows pr(a, s, hk, 32 * (n_rt - 1 - i / Hk), lane);
   const int n_tiles = max(0, (pr.last + PS_KEYS) / PS_KEYS), n = max(1, (n_tiles + a.chunk - 1) / a.chunk);
-  const float* part = a.part + (int64_t)(a.item_prefix[s] + i) * part_floats<D>();
+  const float* part = a.part + (int64_t)(s.first_item + i) * part_floats<D>();
   const int64_t step = (int64_t)n_rt * Hk * part_floats<D>();
   float m = -INFINITY, l = 0.f;
   f32x16 o{};
