@@ -46,8 +46,8 @@ template <int D>
 __device__ __forceinline__ int v_turn(int row) { return D == 128 ? 2 * (row & 7) : 2 * (row & 3); }
 
 // The sequence of item i (items of sequence s being prefix[s] .. prefix[s + 1] - 1) and the item's place in it.  One sequence
-// per lane: a round trip for all of it; loaded by sequence they were two or three more, a microsecond each, the arguments being cold in
-// every launch (one row of 16 sequences, up to 8k keys: 64.6 -> 61.8 us; four of 64 over long histories 46.6 -> 44.4).
+// per lane: a round trip for all of it; loaded by sequence they were two or three more, a microsecond each, the arguments being
+// cold in every launch (one row of 16 sequences, up to 8k keys: 64.6 -> 61.8 us; four of 64 over long histories 46.6 -> 44.4).
 struct PromptSeq {
   int place, nq, nk, n_split, first_item;
   int64_t q0, k0;
@@ -340,9 +340,10 @@ __device__ __forceinline__ uint32_t lds_address(const void* p) {
 // Four waves take 128 rows and walk over the keys in step, one tile ahead; two such workgroups share a CU (three with heads of 64
 // channels: 16 prompts of 1,024 tokens 119 us with two, 105 with three, 145 with four, which spill), and one starts or ends while
 // the other computes.
-// Bound: LDS.  Of a tile a wave reads 32 KB for 32 products' 1,024 cycles, the transposing reads at half the rate of the others, and the
-// tiles are written besides: 2,000 of the 4,100 cycles that two workgroups take for a tile each, beside 2,048 of products; in k_prompt_turns,
-// whose reads are the same, the longest prompt took 1,210 us instead of 1,890 without LDS reads and tile loads.
+// Bound: LDS.  Of a tile a wave reads 32 KB for 32 products' 1,024 cycles, the transposing reads at half the rate of the
+// others, and the tiles are written besides: 2,000 of the 4,100 cycles that two workgroups take for a tile each, beside 2,048
+// of products; in k_prompt_turns, whose reads are the same, the longest prompt took 1,210 us instead of 1,890 without LDS reads
+// and tile loads.
 template <int D>
 __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void k_prompt_tiles(PromptArgs a) {
   constexpr int NW = 4, RB = 2 * D, TILE = PT_KEYS * RB, RPI = 1024 / RB, NI = PT_KEYS / RPI / NW;  // rows and loads per wave's load
@@ -419,8 +420,9 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void k_prompt_tiles(PromptArg
     a.lse[pr.row * a.H + pr.h] = pr.lim >= 0 ? (st.m + __builtin_amdgcn_logf(l)) * (1.f / LOG2E) : -INFINITY;
 }
 
-// Long prompts with heads of 128 channels.  A workgroup of eight waves, two per SIMD, takes 256 rows; the waves work in turns, a barrier between the turns: while waves 0-3 run matrix instructions (the scores
-// of tile j + 1, then the values of tile j), waves 4-7 run the softmax of tile j on the vector units, and the other way round.
+// Long prompts with heads of 128 channels.  A workgroup of eight waves, two per SIMD, takes 256 rows; the waves work in turns,
+// a barrier between the turns: while waves 0-3 run matrix instructions (the scores of tile j + 1, then the values of tile j),
+// waves 4-7 run the softmax of tile j on the vector units, and the other way round.
 // Waves 0-3 run softmax j in turn 2 j and the products in turn 2 j + 1, waves 4-7 one turn later.  V(j) is read in turns 2 j + 1
 // and 2 j + 2, K(j) in turns 2 j - 1 and 2 j (its first pieces one turn before that, ahead of the barrier).
 // Loads go out during a wave's softmax: V(j + 1) and K(j + 3) for waves 0-3 (turn 2 j), V(j + 2) and K(j + 4) for waves 4-7 (turn
@@ -597,9 +599,9 @@ __global__ __launch_bounds__(512, 2) void k_prompt_turns(PromptArgs a) {
 // =====================================================================================================
 // Few rows: a workgroup takes 32 rows and `chunk` tiles of 32 keys, which its two waves share out, each with its own two
 // buffers in LDS and no barrier; at the end they merge their states.  (Two workgroups of two waves fit a CU and start and end
-// apart: 64 new rows of four vehicles 54 us with four waves, 48 with two, 51 with one.)  Where the keys are in several chunks, the workgroups'
-// states (of rows that exist) go to the workspace (16-byte piece p of lane l of block b at float4 (4 b + p) 64 + l, then maxima and sums), and
-// k_prompt_merge puts them together in the order of the chunks.
+// apart: 64 new rows of four vehicles 54 us with four waves, 48 with two, 51 with one.)  Where the keys are in several chunks,
+// the workgroups' states (of rows that exist) go to the workspace (16-byte piece p of lane l of block b at float4 (4 b + p) 64
+// + l, then maxima and sums), and k_prompt_merge puts them together in the order of the chunks.
 // =====================================================================================================
 constexpr int PS_WAVES = 2, PS_KEYS = 32;
 

@@ -286,6 +286,24 @@ def test_read_head_widths(D):
     read_and_check(r, (33, 40), BF16)
 
 
+@pytest.mark.parametrize("out", [BF16, F32])
+@pytest.mark.parametrize("scale", [1.0, 0.037, 2.0 ** -126, 7e5])
+def test_every_code_is_read_as_the_format_says(scale, out):
+    """All 256 codes, the two that are not a number among them."""
+    r = Rings([16], 16, L=1, H=1, D=16)
+    codes = torch.arange(256).to(U8).view(16, 16)
+    r.k.copy_(codes.view(1, 1, 1, 16, 16))
+    r.scale[0].fill_(scale)
+    got = torch.empty((1, 16, 1, 16), dtype=out, device="cuda")
+    torch.cuda.synchronize()
+    fsx.cache_read_rows(r.desc, 0, 1, got, None, fsx.PackedRows((16,)))
+    torch.cuda.synchronize()
+    want = (codes.view(FP8).float() * torch.tensor(scale)).to(out)
+    got, nan = got.cpu().view(16, 16), want.isnan()
+    assert int(nan.sum()) == 2 and torch.equal(got.isnan(), nan)
+    assert torch.equal(bits(got)[~nan], bits(want)[~nan])
+
+
 def test_read_a_shared_cache():
     """Agents of one set of rings, each through its own start and length."""
     r = Rings([10, 25, 3], 40, layout=HEAD | fsx.CACHE_SHARED, starts=[0, 30, 39], agents=1)

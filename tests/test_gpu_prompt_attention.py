@@ -361,3 +361,25 @@ def test_a_workspace_of_any_size_gives_the_output():
         torch.cuda.synchronize()
         c.check(out, lse)
         assert bool((ws[size:] == 0x7F).all()), "behind the workspace"
+
+
+def test_two_calls_at_once():
+    """Calls on two streams, a workspace each, against the same calls one after the other."""
+    calls = []
+    for seed in (1, 2):
+        c = Case((64, 1, 300), (900, 3000, 300), heads=8, kv_heads=2, seed=seed)
+        t = [c.place(x) for x in (c.hq, c.hk, c.hv)]
+        need = fsx.prompt_attention_workspace(t[0], t[1], c.q_rows, c.k_rows)
+        calls.append((c, t, [torch.empty_like(t[0]) for _ in range(6)], torch.empty(max(16, need), dtype=torch.uint8, device="cuda"),
+                      torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    for i in range(6):
+        for c, t, out, ws, stream in calls:
+            fsx.prompt_attention(*t, out[i], c.q_rows, c.k_rows, workspace=ws, stream=stream)
+    torch.cuda.synchronize()
+    for c, t, out, ws, stream in calls:
+        want = torch.empty_like(t[0])
+        fsx.prompt_attention(*t, want, c.q_rows, c.k_rows, workspace=ws)
+        torch.cuda.synchronize()
+        for o in out:
+            assert torch.equal(o.view(torch.int16), want.view(torch.int16))
