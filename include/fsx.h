@@ -312,9 +312,6 @@ void fsx_backbone_destroy(fsx_backbone* bb);
  * Packed rows: the rows of several sequences (agents) lie in one tensor, sequence i in rows start[i] .. start[i] + len[i] - 1
  * (HOST arrays; at most 2^24 rows each).  The ranges need not touch or be in order; rows outside them are not touched. */
 
-/* The tensors of fsx_prompt_attention: element (row r, head h, channel c) of X is X[r * X_row + h * X_head + c].  Strides are
- * in elements, multiples of 8 (k_row and v_row at most 2^27: FSX_E_UNSUPPORTED beyond); buffers are 16-byte aligned; the rows and
- * heads of out must not overlap. */
 /* Kernels of fsx_prompt_attention (fsx_prompt_desc.kernel). */
 enum {
   FSX_PROMPT_AUTO = 0,   /* by what each would take */
@@ -322,6 +319,9 @@ enum {
   FSX_PROMPT_TILES = 2,  /* 128 rows to a workgroup */
   FSX_PROMPT_TURNS = 3   /* 256 rows to a workgroup (head_dim 128; FSX_E_UNSUPPORTED otherwise): long prompts */
 };
+/* The tensors of fsx_prompt_attention: element (row r, head h, channel c) of X is X[r * X_row + h * X_head + c].  Strides are
+ * in elements, multiples of 8 (k_row and v_row at most 2^27: FSX_E_UNSUPPORTED beyond); buffers are 16-byte aligned; the rows and
+ * heads of out must not overlap. */
 typedef struct {
   int32_t n_heads;      /* query heads */
   int32_t n_kv_heads;   /* key / value heads, a divisor of n_heads: query head h reads head h / (n_heads / n_kv_heads) */
