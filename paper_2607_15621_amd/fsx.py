@@ -472,10 +472,18 @@ class Backbone:
 
     def rebuild(self, cache: CacheDesc, tokens, lengths, hidden=None, headroom: float = 1.0, policy: int = APPEND_RING,
                 stream=None):
-        """fsx_backbone_rebuild: whole prompts, tokens [sum of lengths][d], replace the rows of the agents with lengths > 0."""
+        """fsx_backbone_rebuild: whole prompts, tokens [sum of lengths][d] bfloat16 (rows behind them are not read), replace the
+        rows of the agents with lengths > 0; hidden [n_layers][sum of lengths][d] float32, or None.  Both dense."""
         n = PackedRows(lengths)
         if n.n != cache.c.batch:
             raise ValueError("a length of every agent of the cache")
+        rows, d = int(n.len.sum()), self.cfg.d_model
+        if tokens is not None and (tokens.dim() != 2 or tokens.shape[0] < rows or tokens.shape[1] != d or
+                                   _dtype_of(tokens) != BF16 or not tokens.is_contiguous()):
+            raise ValueError("tokens must be a dense bfloat16 [sum of lengths][d_model]")
+        if hidden is not None and (tuple(hidden.shape) != (self.cfg.n_layers, rows, d) or _dtype_of(hidden) != F32 or
+                                   not hidden.is_contiguous()):
+            raise ValueError("hidden must be a dense float32 [n_layers][sum of lengths][d_model]")
         _check(lib().fsx_backbone_rebuild(ctypes.c_void_p(self.handle), ctypes.byref(cache.c), _ptr(tokens), n.c_len,
                                           _ptr(hidden), headroom, policy, _stream(stream)))
 

@@ -169,3 +169,28 @@ def test_binding_checks_its_tensors():
         fsx.cache_read_rows(c, 0, 3, rows, rows, fsx.PackedRows([5, 4]))
     with pytest.raises(ValueError):
         fsx.cache_read_rows(c, 0, 3, rows, rows, fsx.PackedRows([5, 0, 4]), first=[0])
+
+
+def backbone(d=256, layers=2):
+    """A binding without a handle: calls that pass the binding's own checks are refused by the library."""
+    bb = fsx.Backbone.__new__(fsx.Backbone)
+    bb.handle, bb.cfg = 0, fsx.BackboneCfg(layers, d, 2, 128, 512, 4, 3, fsx.BF16, 10000.0, 1e-6)
+    return bb
+
+
+@pytest.mark.parametrize("tokens,hidden,word", [
+    ((8, 256), None, "tokens"), ((9, 128), None, "tokens"), ((9, 2, 128), None, "tokens"), ((9, 256, "float32"), None, "tokens"),
+    ((9, 256, "t"), None, "tokens"), ((9, 256), (2, 8, 256), "hidden"), ((9, 256), (1, 9, 256), "hidden"),
+    ((9, 256), (2, 9, 256, "bfloat16"), "hidden"), ((9, 256), (2, 9, 256, "t"), "hidden")], ids=str)
+def test_rebuild_checks_its_tensors(tokens, hidden, word):
+    import torch
+
+    def make(shape, dtype):
+        sizes, how = [n for n in shape if not isinstance(n, str)], [n for n in shape if isinstance(n, str)]
+        if how == ["t"]:
+            return torch.zeros(sizes[:-2] + sizes[:-3:-1], dtype=dtype).transpose(-1, -2)
+        return torch.zeros(sizes, dtype=getattr(torch, how[0]) if how else dtype)
+
+    with pytest.raises(ValueError, match=word):
+        backbone().rebuild(cache(), make(tokens, torch.bfloat16), (5, 0, 4),
+                           make(hidden, torch.float32) if hidden else None, stream=0)
