@@ -349,10 +349,12 @@ def _prompt_desc(q, k, v, out, scale: float, kernel: int) -> PromptDesc:
 def prompt_attention(q, k, v, out, q_rows: PackedRows, k_rows: Optional[PackedRows] = None, scale: float = 0.0, lse=None,
                      workspace=None, stream=None, kernel: int = PROMPT_AUTO):
     """fsx_prompt_attention: causal attention of packed sequences.  q, out [rows][n_heads][head_dim], k, v
-    [rows][n_kv_heads][head_dim] (any row and head strides); lse [rows][n_heads] float32, dense, or None; workspace a
+    [rows][n_kv_heads][head_dim] (any row and head strides); lse [rows][n_heads] float32, dense, or None; workspace a dense
     device tensor of prompt_attention_workspace bytes, or None (keys are then not split over workgroups)."""
     if lse is not None and (_dtype_of(lse) != F32 or tuple(lse.shape) != tuple(q.shape[:2]) or not lse.is_contiguous()):
         raise ValueError("lse must be a dense float32 [rows][n_heads]")
+    if workspace is not None and not workspace.is_contiguous():
+        raise ValueError("workspace must be a dense tensor")
     if k_rows is not None and k_rows.n != q_rows.n:
         raise ValueError("as many sequences of keys as of queries")
     d = _prompt_desc(q, k, v, out, scale, kernel)

@@ -194,3 +194,12 @@ def test_rebuild_checks_its_tensors(tokens, hidden, word):
     with pytest.raises(ValueError, match=word):
         backbone().rebuild(cache(), make(tokens, torch.bfloat16), (5, 0, 4),
                            make(hidden, torch.float32) if hidden else None, stream=0)
+
+
+def test_workspace_must_be_dense():
+    import torch
+
+    q, k = torch.zeros(8, 4, 128, dtype=torch.bfloat16), torch.zeros(8, 2, 128, dtype=torch.bfloat16)
+    for ws in (torch.zeros(64, 2)[:, 0], torch.zeros(1).expand(1 << 20)):
+        with pytest.raises(ValueError, match="workspace"):
+            fsx.prompt_attention(q, k, k, q, fsx.PackedRows([8]), workspace=ws, stream=0)
