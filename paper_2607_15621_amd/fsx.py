@@ -333,6 +333,30 @@ def _dtype_of(t) -> int:
     return code
 
 
+def _stream_on(stream, *tensors) -> int:
+    """The stream's handle, for a call on these tensors (some may be None).  The library's kernels run on the current device: a
+    tensor of another one, or of the host, is refused."""
+    device = None
+    for t in tensors:
+        if t is not None:
+            at = t.get_device()
+            if at < 0 or (device is not None and at != device):
+                raise ValueError("tensors must be on the current device")
+            device = at
+    if device is None:
+        return _stream(stream)
+    import torch
+
+    if stream is None:
+        stream = torch.cuda.current_stream()
+        current = stream.device_index
+    else:
+        current = torch.cuda.current_device()
+    if current != device:
+        raise ValueError("tensors must be on the current device")
+    return _stream(stream)
+
+
 def _prompt_desc(q, k, v, out, scale: float, kernel: int) -> PromptDesc:
     """Tensors [rows][heads][head_dim], their last dimension dense."""
     sq, sk, so, tq, tk, tv, to = q.shape, k.shape, out.shape, q.stride(), k.stride(), v.stride(), out.stride()
@@ -362,7 +386,7 @@ def prompt_attention(q, k, v, out, q_rows: PackedRows, k_rows: Optional[PackedRo
                                       q_rows.c_start, q_rows.c_len, k_rows.c_start if k_rows is not None else None,
                                       k_rows.c_len if k_rows is not None else None, _ptr(workspace),
                                       workspace.numel() * workspace.element_size() if workspace is not None else 0,
-                                      _stream(stream)))
+                                      _stream_on(stream, q, k, v, out, lse, workspace)))
 
 
 def prompt_attention_workspace(q, k, q_rows: PackedRows, k_rows: Optional[PackedRows] = None, kernel: int = PROMPT_AUTO) -> int:
@@ -396,7 +420,7 @@ def cache_replace_rows(cache: CacheDesc, layer: int, n_layers: int, k_rows, v_ro
     packed rows [n_layers][total][H][Dh]; an fp8 cache's scales are found from them."""
     dtype, total = _row_tensors(cache, n_layers, k_rows, v_rows, rows)
     _check(lib().fsx_cache_replace_rows(ctypes.byref(cache.c), layer, n_layers, _ptr(k_rows), _ptr(v_rows), dtype, total,
-                                        rows.c_start, rows.c_len, headroom, policy, _stream(stream)))
+                                        rows.c_start, rows.c_len, headroom, policy, _stream_on(stream, k_rows, v_rows)))
 
 
 def cache_read_rows(cache: CacheDesc, layer: int, n_layers: int, k_rows, v_rows, rows: PackedRows, first=None, stream=None):
@@ -409,7 +433,8 @@ def cache_read_rows(cache: CacheDesc, layer: int, n_layers: int, k_rows, v_rows,
             raise ValueError("a first row of every agent of the cache")
     _check(lib().fsx_cache_read_rows(ctypes.byref(cache.c), layer, n_layers,
                                      first.ctypes.data_as(ctypes.POINTER(ctypes.c_int64)) if first is not None else None,
-                                     _ptr(k_rows), _ptr(v_rows), dtype, total, rows.c_start, rows.c_len, _stream(stream)))
+                                     _ptr(k_rows), _ptr(v_rows), dtype, total, rows.c_start, rows.c_len,
+                                     _stream_on(stream, k_rows, v_rows)))
 
 
 class Loop:
@@ -487,7 +512,7 @@ class Backbone:
                                    not hidden.is_contiguous()):
             raise ValueError("hidden must be a dense float32 [n_layers][sum of lengths][d_model]")
         _check(lib().fsx_backbone_rebuild(ctypes.c_void_p(self.handle), ctypes.byref(cache.c), _ptr(tokens), n.c_len,
-                                          _ptr(hidden), headroom, policy, _stream(stream)))
+                                          _ptr(hidden), headroom, policy, _stream_on(stream, tokens, hidden)))
 
     def info(self):
         wb, wsb = ctypes.c_int64(), ctypes.c_int64()

@@ -203,3 +203,19 @@ def test_workspace_must_be_dense():
     for ws in (torch.zeros(64, 2)[:, 0], torch.zeros(1).expand(1 << 20)):
         with pytest.raises(ValueError, match="workspace"):
             fsx.prompt_attention(q, k, k, q, fsx.PackedRows([8]), workspace=ws, stream=0)
+
+
+def test_host_tensors_are_refused():
+    """Tensors of the host, or of a device that is not the current one, would be read by the wrong device."""
+    import torch
+
+    q, k = torch.zeros(8, 4, 128, dtype=torch.bfloat16), torch.zeros(8, 2, 128, dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="current device"):
+        fsx.prompt_attention(q, k, k, q, fsx.PackedRows([8]), stream=0)
+    rows = torch.zeros(3, 9, 2, 128, dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="current device"):
+        fsx.cache_replace_rows(cache(), 0, 3, rows, rows, fsx.PackedRows([5, 0, 4]), stream=0)
+    with pytest.raises(ValueError, match="current device"):
+        fsx.cache_read_rows(cache(), 0, 3, None, rows, fsx.PackedRows([5, 0, 4]), stream=0)
+    with pytest.raises(ValueError, match="current device"):
+        backbone().rebuild(cache(), torch.zeros(9, 256, dtype=torch.bfloat16), (5, 0, 4), stream=0)
