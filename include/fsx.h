@@ -335,8 +335,8 @@ typedef struct {
   int64_t q_row, q_head, k_row, k_head, v_row, v_head, out_row, out_head;
 } fsx_prompt_desc;
 
-/* Causal attention of n_seq packed sequences (1..FSX_MAX_BATCH) in one call; query rows times n_heads at most 2^30
- * (FSX_E_UNSUPPORTED beyond).
+/* Causal attention of n_seq packed sequences (1..FSX_MAX_BATCH) in one call; query rows times n_heads at most 2^30,
+ * with FSX_PROMPT_CHUNKS 2^29 (FSX_E_UNSUPPORTED beyond).
  * Sequence i has q_len[i] new tokens, the last ones of its k_len[i] keys: new token t sees the keys
  * j <= k_len[i] - q_len[i] + t.  k_len == q_len is a whole prompt, k_len > q_len new rows over a history (q_len = 1: the next
  * token); a token before the first key (k_len < q_len) sees nothing, its output is 0 and its lse -infinity.  Masked keys and
@@ -354,7 +354,7 @@ typedef struct {
 int fsx_prompt_attention(const fsx_prompt_desc* desc, const void* q, const void* k, const void* v, void* out, float* lse,
                          int32_t n_seq, const int64_t* q_start, const int64_t* q_len, const int64_t* k_start,
                          const int64_t* k_len, void* workspace, int64_t workspace_bytes, void* stream);
-/* The most workspace the call would use (0: none); reads desc and the lengths only. */
+/* The most workspace the call would use (0: none); reads desc and the lengths only, and refuses what the call refuses of them. */
 int fsx_prompt_attention_workspace(const fsx_prompt_desc* desc, int32_t n_seq, const int64_t* q_len, const int64_t* k_len,
                                    int64_t* bytes);
 

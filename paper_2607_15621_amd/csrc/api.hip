@@ -932,6 +932,16 @@ static int check_prompt_desc(const fsx_prompt_desc* d) {
   return FSX_OK;
 }
 
+// Query rows times heads: a launch holds fewer than 2^32 threads, and has two or, in chunks, four of them per row and head.
+static int check_prompt_rows(const fsx_prompt_desc& d, int n_seq, const int64_t* q_len) {
+  int64_t rows = 0;
+  for (int i = 0; i < n_seq; ++i) rows += q_len[i];
+  const int bits = d.kernel == FSX_PROMPT_CHUNKS ? 29 : 30;
+  if (rows * d.n_heads > (int64_t)1 << bits)
+    return fail(FSX_E_UNSUPPORTED, "query rows * n_heads beyond 2^" + std::to_string(bits));
+  return FSX_OK;
+}
+
 // Rows and heads of the output must not overlap, whichever of the two strides is the larger.
 static int check_out_strides(const fsx_prompt_desc& d) {
   const bool head_major = d.out_head > d.out_row;
@@ -962,7 +972,7 @@ extern "C" int fsx_prompt_attention_workspace(const fsx_prompt_desc* desc, int32
                                               const int64_t* k_len, int64_t* bytes) {
   if (!bytes) return fail(FSX_E_INVALID, "bytes is NULL");
   *bytes = 0;
-  const int rc = check_prompt_desc(desc);
+  int rc = check_prompt_desc(desc);
   if (rc) return rc;
   if (n_seq < 1 || n_seq > FSX_MAX_BATCH) return fail(FSX_E_INVALID, "n_seq must be in 1..64");
   if (!q_len) return fail(FSX_E_INVALID, "q_len is NULL");
@@ -970,6 +980,7 @@ extern "C" int fsx_prompt_attention_workspace(const fsx_prompt_desc* desc, int32
   for (int i = 0; i < n_seq; ++i)
     if (q_len[i] < 0 || q_len[i] > MAX_PROMPT || k_len[i] < 0 || k_len[i] > MAX_PROMPT)
       return fail(FSX_E_INVALID, "length " + std::to_string(i) + " outside 0..2^24");
+  if ((rc = check_prompt_rows(*desc, n_seq, q_len))) return rc;
   PromptArgs a{};
   a.H = desc->n_heads; a.G = desc->n_heads / desc->n_kv_heads; a.D = desc->head_dim; a.kernel = desc->kernel;
   prompt_sequences(a, n_seq, nullptr, q_len, nullptr, k_len);
@@ -1011,7 +1022,7 @@ extern "C" int fsx_prompt_attention(const fsx_prompt_desc* desc, const void* q, 
   if (!q || !out || (keys > 0 && (!k || !v))) return fail(FSX_E_INVALID, "q, k, v and out must be non-NULL");
   if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out))
     return fail(FSX_E_INVALID, "q, k, v and out must be 16-byte aligned");
-  if (rows * d.n_heads > (int64_t)1 << 30) return fail(FSX_E_UNSUPPORTED, "query rows * n_heads beyond 2^30");
+  if ((rc = check_prompt_rows(d, n_seq, q_len))) return rc;
   a.q = q; a.k = (const uint16_t*)k; a.v = (const uint16_t*)v; a.out = out; a.lse = lse;
   a.q_row = d.q_row; a.q_head = d.q_head; a.k_row = d.k_row; a.k_head = d.k_head;
   a.v_row = d.v_row; a.v_head = d.v_head; a.o_row = d.out_row; a.o_head = d.out_head;

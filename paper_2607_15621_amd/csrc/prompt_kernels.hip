@@ -854,22 +854,23 @@ bool plan_prompt(PromptArgs& a, int64_t workspace_bytes, int64_t* need) {
   tiles = std::max(tiles / SLOTS, longest);
   tiles = std::max(tiles, memory) + 0.35 * std::min(tiles, memory);
   const double per_wave = steps / (SLOTS * PS_WAVES), shared_step = std::max(width, memory / per_wave);
-  double best = 0;
+  double best = INFINITY;
   for (const int k : {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 48, 64}) {  // chunks of the longest keys
     const int chunk = std::max(2 * PS_WAVES, (t_max + k - 1) / k);
-    int64_t items = 0;
-    bool split = false;
+    int64_t items = 0, merges = 0;
     for (int i = 0; i < a.n_seq; ++i) {
       const int n_rt = (int)(((int64_t)a.nq[i] * a.G + 31) / 32), n = std::max(1, ((a.nk[i] + PS_KEYS - 1) / PS_KEYS + chunk - 1) / chunk);
       items += (int64_t)n_rt * Hk * n;
-      split = split || n > 1;
+      if (n > 1) merges += (int64_t)n_rt * Hk;
     }
-    if (split && (items * part > workspace_bytes || items > INT32_MAX)) break;
+    const bool split = merges > 0;
+    // (a launch holds fewer than 2^32 threads)
+    if (items > UINT32_MAX / (PS_WAVES * 64) || merges > UINT32_MAX / (2 * a.D * PM_GROUPS) || (split && items * part > workspace_bytes)) break;
     const double rounds = std::max(1.0, (double)items / SLOTS), pair = (double)chunk / PS_WAVES;
     const double work = 5 * rounds + width * (rounds > 1 ? std::max(per_wave, pair) : pair);
     const double tail = rounds > 1 ? 0.15 * pair : 0.4 * std::max(0.0, pair - steps / items / PS_WAVES);
     const double cost = std::max(memory, work) + 0.35 * std::min(memory, work) + tail * shared_step + (split ? 4 : 0);
-    if (k > 1 && cost >= best) continue;
+    if (cost >= best) continue;
     best = cost;
     a.chunk = chunk;
     *need = split ? items * part : 0;

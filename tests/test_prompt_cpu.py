@@ -219,3 +219,26 @@ def test_host_tensors_are_refused():
         fsx.cache_read_rows(cache(), 0, 3, None, rows, fsx.PackedRows([5, 0, 4]), stream=0)
     with pytest.raises(ValueError, match="current device"):
         backbone().rebuild(cache(), torch.zeros(9, 256, dtype=torch.bfloat16), (5, 0, 4), stream=0)
+
+
+def workspace_of(d, lens):
+    need, r = ctypes.c_int64(5), fsx.PackedRows(lens)
+    return fsx.lib().fsx_prompt_attention_workspace(ctypes.byref(d), r.n, r.c_len, None, ctypes.byref(need)), need.value
+
+
+@pytest.mark.parametrize("heads,lens,kernel,code", [
+    (1024, [1 << 24] * 64, fsx.PROMPT_AUTO, UNSUPPORTED), (1024, [1 << 24] * 64, fsx.PROMPT_CHUNKS, UNSUPPORTED),
+    (1024, [1 << 24] * 64, fsx.PROMPT_TURNS, UNSUPPORTED), (1024, [(1 << 20) + 1], fsx.PROMPT_TILES, UNSUPPORTED),
+    (1024, [1 << 20], fsx.PROMPT_TILES, 0), (1024, [1 << 20], fsx.PROMPT_AUTO, 0),
+    # a workgroup of two waves per 32 rows and head: a launch holds fewer than 2^32 threads
+    (1024, [(1 << 19) + 1], fsx.PROMPT_CHUNKS, UNSUPPORTED), (1024, [1 << 19], fsx.PROMPT_CHUNKS, 0),
+    (32, [1 << 24, 1], fsx.PROMPT_CHUNKS, UNSUPPORTED), (32, [1 << 24, 1], fsx.PROMPT_AUTO, 0)])
+def test_sizes_that_a_call_refuses_have_no_workspace(heads, lens, kernel, code):
+    d = desc(n_heads=heads, n_kv_heads=heads, kernel=kernel, q_rows=1 << 31, k_rows=1 << 31, q_row=128 * heads, out_row=128 * heads)
+    got, need = workspace_of(d, lens)
+    assert got == code and need >= 0
+    if code:
+        assert need == 0 and "2^" in fsx.last_error()
+        r = [(i << 24, n) for i, n in enumerate(lens)]
+        got, msg = attend(d, q_rows=r, k_rows=None)
+        assert got == code and "2^" in msg, msg
