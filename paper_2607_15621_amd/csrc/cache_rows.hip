@@ -385,10 +385,12 @@ __global__ __launch_bounds__(256) void k_row_tops(RowsArgs a) {
               __float_as_uint(scale_of(__uint_as_float(tops[threadIdx.x]), a.headroom)));
 }
 
-// Rows per workgroup, so that there are about `wgs` workgroups, and the workgroups of the agents before.
+// Rows per workgroup, so that there are about `wgs` workgroups, and the workgroups of the agents before.  A launch holds fewer than
+// 2^32 threads, 2^24 workgroups of 256 (one with more runs the rest of its threads by 2^32, without an error), so from 2^27 rows on
+// a workgroup takes more of them.
 static int plan_blocks(RowsArgs& a, int64_t per_row_wgs, int64_t wgs, int least, int most) {
   const int64_t rows = a.prefix[a.B];
-  a.block = (int)std::max<int64_t>(least, std::min<int64_t>(most, rows * per_row_wgs / wgs));
+  a.block = (int)std::max({(int64_t)least, std::min<int64_t>(most, rows * per_row_wgs / wgs), (rows >> 23) + 1});
   for (int b = 0; b < a.B; ++b) a.block_prefix[b + 1] = a.block_prefix[b] + (a.n[b] + a.block - 1) / a.block;
   return a.block_prefix[a.B];
 }

@@ -350,3 +350,40 @@ def test_appended_rows_take_the_found_scales():
             want = torch.cat([rows[i][:, src:src + n].float(), dev[i][b].float()], 1)
             got, s = back[i].cpu()[:, at:at + n + 4], scale[i][b][:, None, :, None]
             assert bool(((got - want).abs() <= 2.0 ** -4 * want.abs().clamp_min(2.0 ** -6 * s) * (1 + 1e-6)).all())
+
+
+@pytest.mark.parametrize("dtype,lens", [(BF16, (3,)), (U8, (3,)), (F32, (2, 1))], ids=str)
+def test_more_than_65535_layers(dtype, lens):
+    """The layers are a launch's second dimension."""
+    L = 65_600
+    r = Rings([0] * len(lens), 3, L=L, H=1, D=16, dtype=dtype, layout=TOKEN)
+    rows = packed_rows(L, sum(lens), 1, 16, BF16, seed=3)
+    dev, at = [t.cuda() for t in rows], fsx.PackedRows(lens)
+    fsx.cache_replace_rows(r.desc, 0, L, *dev, at)
+    back = [torch.empty_like(t) for t in dev]
+    fsx.cache_read_rows(r.desc, 0, L, *back, at)
+    torch.cuda.synchronize()
+    for i in range(2):
+        if dtype is not U8:
+            assert torch.equal(bits(back[i]), bits(rows[i]))
+            continue
+        x = rows[i].float()
+        top = x.abs().amax((1, 2, 3), keepdim=True).numpy()
+        scale = torch.from_numpy(np.maximum(top / np.float32(448.0), np.float32(2.0 ** -126)))
+        code = torch.from_numpy(x.numpy() / scale.numpy()).to(FP8)
+        assert torch.equal(r.scale[i].cpu().flatten(), scale.flatten())
+        assert torch.equal(bits(back[i]), bits((code.float() * scale).to(BF16)))
+
+
+def test_more_rows_than_a_launch_has_threads_for():
+    """17 agents' windows of one ring of 2^24 rows, 2^24 workgroups of 16 rows and more: a launch holds fewer than 2^32 threads."""
+    n, agents = 1 << 24, 17
+    k = torch.arange(n * 4, dtype=torch.int32, device="cuda").view(BF16).view(1, 1, n, 1, 8).repeat(1, 1, 1, 1, 2)
+    cache = fsx.CacheDesc(k, k, fsx.BF16, 1, 1, 16, n, [n] * agents, starts=[5 * b for b in range(agents)],
+                          layout=TOKEN | fsx.CACHE_SHARED)
+    out = torch.zeros(1, n * agents, 1, 16, dtype=BF16, device="cuda")
+    fsx.cache_read_rows(cache, 0, 1, out, None, fsx.PackedRows([n] * agents))
+    torch.cuda.synchronize()
+    want, got = k.view(n, 8, 2).view(torch.int32), out.view(agents, n, 8, 2).view(torch.int32)
+    for b in range(agents):
+        assert torch.equal(got[b], want.roll(-5 * b, 0)), b
