@@ -330,9 +330,14 @@ __device__ __forceinline__ void meet() {
 
 // Direct load of 16 bytes per lane from base + at (bytes) to LDS at lds + 16 lane.  In assembly, so that the compiler does not
 // take every LDS read that might meet it for one that has to wait: the waits are the kernel's own (vm_wait_all, then meet).
+// (m0 is named, so that a value of the compiler's own is not thought to outlast the statement; that it is a reserved register is
+// what the warning would say.)
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
 __device__ __forceinline__ void dma16(const void* base, uint32_t at, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(at), "s"(base) : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(at), "s"(base) : "memory", "m0");
 }
+#pragma clang diagnostic pop
 __device__ __forceinline__ uint32_t lds_address(const void* p) {
   return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)p;
 }

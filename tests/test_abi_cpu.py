@@ -69,3 +69,14 @@ def test_query_head_limit_is_the_one_its_message_names():
         codes[hidden] = fsx.lib().fsx_expert_create(ctypes.byref(cfg), None, None, None, None, ctypes.byref(out)), fsx.last_error()
     assert codes[148][0] == 1 and "layers" in codes[148][1]  # the sizes are accepted, the missing layers are not
     assert codes[149][0] == 2 and "at most 16384" in codes[149][1] and "LDS" not in codes[149][1]
+
+
+def test_assembly_that_writes_m0_names_it():
+    csrc, seen = os.path.join(ROOT, "paper_2607_15621_amd", "csrc"), 0
+    for name in sorted(os.listdir(csrc)):
+        for asm in re.findall(r"\basm volatile\((.*?)\);", open(os.path.join(csrc, name)).read(), flags=re.S):
+            code, _, rest = asm.partition('" ::')
+            if re.search(r"\bs_\w+ m0\b", code):
+                seen += 1
+                assert '"m0"' in rest, f"{name}: {asm}"
+    assert seen
