@@ -1,0 +1,150 @@
+"""Rebuilds (fsx_backbone_rebuild) of the lengths that a deployment has: thousands of packed rows, through every kernel of the prompt
+attention, with narrow and wide rows, against the forward in 64 bits.
+
+The weights of the synthetic backbone (N(0, 0.02^2)) give scores of a few tenths, an almost uniform softmax that hardly shows what
+the attention does.  Here its projections are four times as large: scores have a standard deviation of (0.08 sqrt(d))^2, 3 to 16 at
+the widths below, and the reference with a softmax in another base is shown to differ by more than the tolerance allows.  Scores
+as large as 60 move by 60 x 2^-8 = 0.2 when queries and keys are rounded to bf16, so the reference, in 64 bits otherwise, rounds
+to bf16 where the backbone does: projection inputs, scaled queries, keys, values, attention outputs and SwiGLU outputs; and each layer starts
+from the hidden states that the call gave for the layer before, as roundings of one layer would come back in the next one's scores.
+What is left are the probabilities' rounding (2^-9 of a value) and elements that fp32 sums round to the other side, 2^-8 of an
+element each; the tolerance is the incremental forward's, relative to the largest magnitude."""
+
+from __future__ import annotations
+
+import math
+import re
+
+import numpy as np
+import pytest
+import torch
+
+import synth
+from harness import Cache, record
+from paper_2607_15621_amd import fsx
+from test_gpu_backbone import TOL, bb_workload
+
+pytestmark = pytest.mark.gpu
+
+BF16, F64 = torch.bfloat16, torch.float64
+
+
+class Backbone:
+    def __init__(self, wl, max_batch, max_new_rows):
+        self.wl = wl
+        host, _, _ = synth.make_weights(wl)
+        for lw in host:
+            for n in ("wq", "wk", "wv", "wo"):
+                lw[n] = lw[n] * np.float32(4)  # exact in bf16
+        dev = [{k: torch.from_numpy(v).to("cuda", torch.float32 if k in ("attn_norm", "ffn_norm") else BF16) for k, v in lw.items()}
+               for lw in host]
+        self.bb = fsx.Backbone(fsx.BackboneCfg(wl.n_layers, wl.d_model, wl.n_heads, 128, wl.d_ffn, max_new_rows, max_batch, fsx.BF16,
+                                               wl.rope_base, wl.rms_eps), dev)
+        torch.cuda.synchronize()
+        self.layers = [{k: v.to(F64) for k, v in lw.items()} for lw in dev]
+
+    def prompts(self, n, seed=0):
+        g = torch.Generator().manual_seed(1000 * self.wl.wid + seed)
+        return torch.randn(n, self.wl.d_model, generator=g).to("cuda", BF16)
+
+    def forward(self, inputs, base=2.0):
+        """One prompt's inputs of every layer (the tokens, then hidden states) [n][d] through the layers: (keys, values
+        [layers][n][H][128], hidden [layers][n][d]).  The queries are scaled to log2 units; base: what the softmax takes powers of."""
+        wl, n = self.wl, inputs[0].shape[0]
+        H, at = wl.n_heads, torch.arange(n, device="cuda", dtype=F64)
+        ang = at[:, None] * wl.rope_base ** (-torch.arange(64, device="cuda", dtype=F64) / 64)
+        cos, sin = ang.cos()[:, None], ang.sin()[:, None]
+        wide = wl.d_model >= 2048 and wl.d_model % 512 == 0  # rounded before the norm's scale, but for the embeddings
+
+        def rounded(x):
+            return x.float().to(BF16).to(F64)
+
+        def project(h, gain, first, *weights):
+            r = 1 / (h.square().mean(1, keepdim=True) + wl.rms_eps).sqrt()
+            x, scale = (rounded(h), r) if wide and not first else (rounded(h * r), 1.0)
+            return [(x @ (w * gain).t()) * scale for w in weights]
+
+        def rotate(x):
+            a, b = x[..., :64], x[..., 64:]
+            return torch.cat([a * cos - b * sin, a * sin + b * cos], -1)
+
+        later = torch.ones(n, n, dtype=torch.bool, device="cuda").triu(1)
+        ks, vs, hs = [], [], []
+        for i, (h, lw) in enumerate(zip(inputs, self.layers)):
+            h = h.to(F64)
+            q, k, v = (x.view(n, H, 128) for x in project(h, lw["attn_norm"], i == 0, lw["wq"], lw["wk"], lw["wv"]))
+            q, k, v = rounded(rotate(q) * (math.log2(math.e) / math.sqrt(128))), rounded(rotate(k)), rounded(v)
+            out = torch.empty(n, H, 128, dtype=F64, device="cuda")
+            for j in range(H):
+                s = (q[:, j] @ k[:, j].t()).mul_(math.log(base)).masked_fill_(later, -math.inf)
+                out[:, j] = s.softmax(1) @ v[:, j]
+            h = h + rounded(out.view(n, -1)) @ lw["wo"].t()
+            gate, up = project(h, lw["ffn_norm"], False, lw["w_gate"], lw["w_up"])
+            h = h + rounded(gate * gate.sigmoid() * up) @ lw["w_down"].t()
+            ks.append(k)
+            vs.append(v)
+            hs.append(h)
+        return [torch.stack(x) for x in (ks, vs, hs)]
+
+
+def kernels_of(call):
+    """Names of the prompt attention's kernels that the call launches."""
+    with torch.profiler.profile(activities=[torch.profiler.ProfilerActivity.CUDA], acc_events=True) as p:
+        call()
+        torch.cuda.synchronize()
+    return sorted({m.group(1) for m in (re.search(r"k_prompt_(\w+)", e.key) for e in p.key_averages()) if m})
+
+
+def read_back(cache, lens):
+    wl = cache.wl
+    out = [torch.empty(wl.n_layers, sum(lens), wl.n_heads, 128, device="cuda") for _ in "kv"]
+    fsx.cache_read_rows(cache.desc, 0, wl.n_layers, *out, fsx.PackedRows(lens))
+    return out
+
+
+def rel(got, want):
+    return float((got.to(F64) - want).abs().max() / want.abs().max())
+
+
+def rebuild_and_check(r, lens, kernels):
+    wl = r.wl
+    cache, tok = Cache(wl), r.prompts(sum(lens))
+    hid = torch.full((wl.n_layers, sum(lens), wl.d_model), float("nan"), device="cuda")
+    assert kernels_of(lambda: r.bb.rebuild(cache.desc, tok, lens, hid)) == kernels
+    rows = read_back(cache, lens)
+    torch.cuda.synchronize()
+    at = 0
+    for b, n in enumerate(lens):
+        if n == 0:
+            continue
+        assert [int(x[b]) for x in (cache.desc.start, cache.desc.len, cache.desc.pos)] == [0, n, n]
+        if b > 3 and b + 1 < len(lens):
+            at += n
+            continue  # the first ones and the last one
+        inputs = [tok[at:at + n], *hid[:-1, at:at + n]]
+        k, v, h = r.forward(inputs)
+        for got, want, what in zip(rows, (k, v), ("keys", "values")):
+            got = got[:, at:at + n].to(F64)
+            if wl.cache_dtype == "fp8":  # half a code step more, 2^-4 of a magnitude
+                worst = float(((got - want).abs() - 2.0 ** -4 * want.abs()).max() / want.abs().max())
+            else:
+                worst = rel(got, want)
+            record(b, worst, TOL * (1.07 if wl.cache_dtype == "fp8" else 1.0), what=f"rebuilt {what}, max|d| / max|ref|")
+        record(b, max(rel(hid[l, at:at + n], h[l]) for l in range(wl.n_layers)), TOL, what="worst layer hidden, max|d| / max|ref|")
+        if n > 100 and b == 0:
+            wrong = r.forward(inputs, base=math.e)[2]
+            assert min(rel(wrong[l], h[l]) for l in range(wl.n_layers)) > 3 * TOL, "the reference does not show what the attention does"
+        at += n
+
+
+@pytest.mark.parametrize("lens,H,d,F,kernels", [
+    ((1000,), 4, 512, 1024, ["merge", "split"]), ((700, 0, 1), 2, 2048, 512, ["merge", "split"]), ((512,) * 8, 8, 512, 512, ["split"]),
+    ((224,) * 16, 16, 512, 1024, ["tiles"]), ((300,) * 13, 8, 2048, 1024, ["tiles"]), ((4000, 90), 16, 2560, 512, ["tiles"]),
+    ((4096,), 16, 1024, 1024, ["turns"]), ((4096,), 16, 2048, 512, ["turns"])],
+    ids=lambda x: f"{len(x)}x{x[0]}" if isinstance(x, tuple) else ("-".join(x) if isinstance(x, list) else str(x)))
+@pytest.mark.parametrize("cache_dtype", ["bf16", "fp8"])
+def test_long_rebuilds(lens, H, d, F, kernels, cache_dtype):
+    wl = bb_workload(850 + len(lens), lengths=(0,) * len(lens), n_new=4, capacity=max(lens), d=d, H=H, F=F, cache_dtype=cache_dtype)
+    r = Backbone(wl, 64, 64)
+    rebuild_and_check(r, lens, kernels)
+    r.bb.close()
