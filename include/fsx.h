@@ -273,6 +273,8 @@ typedef struct {
   int32_t dtype;         /* FSX_BF16 */
   float rope_base;       /* rotary base of the backbone (LLaMA: 10000) */
   float rms_eps;
+  int32_t max_prompt_rows;  /* tokens of all agents together in one fsx_backbone_rebuild, up to 2^20 (times n_heads: 2^30); the
+                             * workspace holds the larger of this and max_batch * max_new_rows, so 0 is that product */
 } fsx_backbone_cfg;
 
 /* Pack the backbone's layers (fsx_layer_weights as for the expert: wq, wk, wv [H*Dh][d], wo [d][H*Dh], w_gate,
@@ -294,8 +296,9 @@ int fsx_backbone_append(fsx_backbone* bb, fsx_cache_desc* cache, const void* tok
  * different lengths through the layers, in one call, their rotated keys and values replacing the agents' rows
  * (fsx_prompt_attention and fsx_cache_replace_rows per layer).
  *   tokens    DEVICE [sum of n_tokens][d] bf16 embeddings, agent after agent, at positions 0 .. n_tokens[b]-1
- *   n_tokens  HOST [cache->batch]; an agent with 0 is left as it is.  Their sum is at most max_batch * max_new_rows
- *             (FSX_E_CAPACITY): the rows that the workspace holds
+ *   n_tokens  HOST [cache->batch]; an agent with 0 is left as it is.  Their sum is at most the rows that the
+ *             workspace holds, max_prompt_rows or max_batch * max_new_rows (FSX_E_CAPACITY beyond); cache->batch may be
+ *             more than max_batch
  *   hidden    DEVICE [n_layers][sum of n_tokens][d] fp32 output of every layer, or NULL
  *   headroom, policy  as fsx_cache_replace_rows (an FP8 cache gets new scales, found from the rows).  The attention is over
  *             the rows as computed, before they are encoded

@@ -105,9 +105,10 @@ static int validate_cfg(const fsx_expert_cfg* c) {
 }
 
 // backbone: the layers only (no final norm, no head), run as one launch per phase with causal own rows (the
-// backbone's incremental forward, fsx_backbone_*).
+// backbone's incremental forward, fsx_backbone_*); prompt_rows: rows that the workspace holds at least.
 static int create_impl(const fsx_expert_cfg* cfg, const fsx_layer_weights* layers, const float* final_norm,
-                       const fsx_head_weights* head, void* stream, fsx_expert** out, bool backbone) {
+                       const fsx_head_weights* head, void* stream, fsx_expert** out, bool backbone,
+                       int prompt_rows = 0) {
   if (!out) return fail(FSX_E_INVALID, "out is NULL");
   *out = nullptr;
   int rc = validate_cfg(cfg);
@@ -134,7 +135,7 @@ static int create_impl(const fsx_expert_cfg* cfg, const fsx_layer_weights* layer
   const int A = H * Dh;
   ex->A = A;
   ex->S_max = c.n_expert_tokens + c.max_frame_tokens;
-  ex->M_max = c.max_batch * ex->S_max;
+  ex->M_max = std::max(c.max_batch * ex->S_max, prompt_rows);
   const bool fused_ok = c.dtype == FSX_BF16 && Dh == 128 && d % 32 == 0 && F % 32 == 0;
   ex->path = (fused_ok && !(c.flags & FSX_FLAG_GENERIC)) ? 0 : 1;
   ex->backbone = backbone;
@@ -1203,7 +1204,7 @@ extern "C" int fsx_expert_info(const fsx_expert* ex, int32_t* path, int64_t* wei
   return FSX_OK;
 }
 
-extern "C" const char* fsx_version(void) { return "0.2.0"; }
+extern "C" const char* fsx_version(void) { return "0.3.0"; }
 
 extern "C" int fsx_probe_hbm_read(const void* buf, int64_t bytes, int32_t mode, uint32_t* sink, void* stream) {
   if (!buf || !sink) return fail(FSX_E_INVALID, "buf and sink must be non-NULL");
@@ -1230,13 +1231,16 @@ extern "C" int fsx_backbone_create(const fsx_backbone_cfg* cfg, const fsx_layer_
   if (!cfg) return fail(FSX_E_INVALID, "cfg is NULL");
   if (cfg->dtype != FSX_BF16) return fail(FSX_E_UNSUPPORTED, "the backbone runs bf16 weights");
   if (cfg->max_new_rows < 1 || cfg->max_new_rows > 64) return fail(FSX_E_INVALID, "max_new_rows must be in 1..64");
+  if (cfg->max_prompt_rows < 0 || cfg->max_prompt_rows > 1 << 20) return fail(FSX_E_INVALID, "max_prompt_rows must be in 0..2^20");
+  if ((int64_t)cfg->max_prompt_rows * cfg->n_heads > (int64_t)1 << 30)
+    return fail(FSX_E_UNSUPPORTED, "max_prompt_rows * n_heads beyond 2^30");
   fsx_expert_cfg c{};
   c.n_layers = cfg->n_layers; c.d_model = cfg->d_model; c.n_heads = cfg->n_heads; c.head_dim = cfg->head_dim;
   c.d_ffn = cfg->d_ffn; c.n_expert_tokens = cfg->max_new_rows; c.n_out = 2; c.max_batch = cfg->max_batch;
   c.max_frame_tokens = 0; c.dtype = cfg->dtype; c.rope_base = cfg->rope_base; c.rms_eps = cfg->rms_eps;
   c.flags = FSX_FLAG_MULTI_LAUNCH; c.head_kind = FSX_HEAD_MEAN_LINEAR;
   fsx_expert* ex = nullptr;
-  const int rc = create_impl(&c, layers, nullptr, nullptr, stream, &ex, true);
+  const int rc = create_impl(&c, layers, nullptr, nullptr, stream, &ex, true, cfg->max_prompt_rows);
   if (rc) return rc;
   fsx_backbone* bb = new fsx_backbone();
   bb->ex = ex;
@@ -1358,7 +1362,8 @@ extern "C" int fsx_backbone_rebuild(fsx_backbone* bb, fsx_cache_desc* cache, con
   for (int b = 0; b < B; ++b) {
     if (n_tokens[b] < 0) return fail(FSX_E_INVALID, "n_tokens must be >= 0");
     if (n_tokens[b] > ex->M_max - rows)
-      return fail(FSX_E_CAPACITY, "more than max_batch * max_new_rows = " + std::to_string(ex->M_max) + " tokens");
+      return fail(FSX_E_CAPACITY, "more tokens than the workspace holds, " + std::to_string(ex->M_max) +
+                                      " (max_prompt_rows or max_batch * max_new_rows)");
     at[b] = rows;
     rows += n_tokens[b];
   }

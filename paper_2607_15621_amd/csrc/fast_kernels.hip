@@ -438,9 +438,9 @@ __global__ __launch_bounds__((CW + 4) * 64) void k_gemm_rows(GemmArgs g, int n_r
 template <int MT, int NT, int KCB, int RING, int EPI, int CW = 4, bool ALL = false>
 static hipError_t launch_rows(const GemmArgs& g, hipStream_t s) {
   const int n_rb = (g.M + MT * 16 - 1) / (MT * 16), n_cg = (g.N / 16 + CW * NT - 1) / (CW * NT);
-  const int combos = n_cg * g.ksplit;
-  hipLaunchKernelGGL((k_gemm_rows<MT, NT, KCB, RING, EPI, CW, ALL>), dim3((unsigned)((combos + 7) / 8 * 8 * n_rb)), dim3((CW + 4) * 64), 0, s,
-                     g, n_rb);
+  const int64_t wgs = (int64_t)(n_cg * g.ksplit + 7) / 8 * 8 * n_rb;
+  if (wgs > UINT32_MAX / ((CW + 4) * 64)) return hipErrorInvalidConfiguration;  // a launch holds fewer than 2^32 threads
+  hipLaunchKernelGGL((k_gemm_rows<MT, NT, KCB, RING, EPI, CW, ALL>), dim3((unsigned)wgs), dim3((CW + 4) * 64), 0, s, g, n_rb);
   return hipGetLastError();
 }
 

@@ -63,7 +63,7 @@ class BackboneCfg(ctypes.Structure):
     _fields_ = [("n_layers", ctypes.c_int32), ("d_model", ctypes.c_int32), ("n_heads", ctypes.c_int32),
                 ("head_dim", ctypes.c_int32), ("d_ffn", ctypes.c_int32), ("max_new_rows", ctypes.c_int32),
                 ("max_batch", ctypes.c_int32), ("dtype", ctypes.c_int32), ("rope_base", ctypes.c_float),
-                ("rms_eps", ctypes.c_float)]
+                ("rms_eps", ctypes.c_float), ("max_prompt_rows", ctypes.c_int32)]
 
 
 class LoopTickInfo(ctypes.Structure):

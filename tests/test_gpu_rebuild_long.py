@@ -30,7 +30,7 @@ BF16, F64 = torch.bfloat16, torch.float64
 
 
 class Backbone:
-    def __init__(self, wl, max_batch, max_new_rows):
+    def __init__(self, wl, max_batch, max_new_rows, max_prompt_rows=0):
         self.wl = wl
         host, _, _ = synth.make_weights(wl)
         for lw in host:
@@ -39,7 +39,7 @@ class Backbone:
         dev = [{k: torch.from_numpy(v).to("cuda", torch.float32 if k in ("attn_norm", "ffn_norm") else BF16) for k, v in lw.items()}
                for lw in host]
         self.bb = fsx.Backbone(fsx.BackboneCfg(wl.n_layers, wl.d_model, wl.n_heads, 128, wl.d_ffn, max_new_rows, max_batch, fsx.BF16,
-                                               wl.rope_base, wl.rms_eps), dev)
+                                               wl.rope_base, wl.rms_eps, max_prompt_rows), dev)
         torch.cuda.synchronize()
         self.layers = [{k: v.to(F64) for k, v in lw.items()} for lw in dev]
 
@@ -147,4 +147,23 @@ def test_long_rebuilds(lens, H, d, F, kernels, cache_dtype):
     wl = bb_workload(850 + len(lens), lengths=(0,) * len(lens), n_new=4, capacity=max(lens), d=d, H=H, F=F, cache_dtype=cache_dtype)
     r = Backbone(wl, 64, 64)
     rebuild_and_check(r, lens, kernels)
+    r.bb.close()
+
+
+@pytest.mark.parametrize("agents,lens,max_prompt_rows,H,d,kernels", [
+    (1, (224,), 224, 8, 512, ["split"]), (1, (100, 0, 124), 224, 8, 2048, ["split"]), (16, (1024,) * 16, 16_384, 8, 512, ["tiles"]),
+    (1, (16_001,), 16_001, 8, 512, ["turns"])], ids=["224", "100+124", "16x1024", "16001"])
+def test_prompts_beyond_the_frames_that_a_handle_appends(agents, lens, max_prompt_rows, H, d, kernels):
+    """A deployment's handle, four new rows per call: its prompts are longer than what it appends."""
+    wl = bb_workload(870, lengths=(0,) * len(lens), n_new=4, capacity=max(lens) + 4, d=d, H=H, F=512)
+    r = Backbone(wl, agents, 4, max_prompt_rows)
+    rebuild_and_check(r, lens, kernels)
+    cache = Cache(wl)
+    before = [list(x) for x in (cache.desc.start, cache.desc.len, cache.desc.pos)]
+    with pytest.raises(fsx.FsxError, match=str(max_prompt_rows)) as e:
+        r.bb.rebuild(cache.desc, r.prompts(sum(lens) + 1), (lens[0] + 1, *lens[1:]))
+    assert e.value.code == 3 and before == [list(x) for x in (cache.desc.start, cache.desc.len, cache.desc.pos)]
+    with pytest.raises(fsx.FsxError) as e:  # appends keep their limit
+        r.bb.append(cache.desc, r.prompts(5 * len(lens)), len(lens), 5)
+    assert e.value.code == 3
     r.bb.close()

@@ -242,3 +242,11 @@ def test_sizes_that_a_call_refuses_have_no_workspace(heads, lens, kernel, code):
         r = [(i << 24, n) for i, n in enumerate(lens)]
         got, msg = attend(d, q_rows=r, k_rows=None)
         assert got == code and "2^" in msg, msg
+
+
+@pytest.mark.parametrize("rows,heads,code", [(-1, 2, INVALID), ((1 << 20) + 1, 2, INVALID), (1 << 20, 2048, UNSUPPORTED)])
+def test_rows_of_a_rebuild_are_limited_at_create(rows, heads, code):
+    cfg = fsx.BackboneCfg(1, 256, heads, 128, 512, 4, 1, fsx.BF16, 10000.0, 1e-6, rows)
+    out = ctypes.c_void_p(1)
+    assert fsx.lib().fsx_backbone_create(ctypes.byref(cfg), None, None, ctypes.byref(out)) == code
+    assert out.value is None and "max_prompt_rows" in fsx.last_error()
