@@ -439,6 +439,23 @@ def run_workload(name: str, steps: int, warmup: int, multi_launch: bool, cold_st
     return wl, r, extra
 
 
+LLAMA_7B = (32, 4096, 32, 128, 11008)  # layers, width, heads, head width, SwiGLU width
+
+
+def llama_layers(g):
+    """Synthetic LLaMA-7B layers, N(0, 0.02^2), drawn on the GPU."""
+    import torch
+
+    nl, d, H, Dh, F = LLAMA_7B
+
+    def w(*shape):
+        return (torch.randn(shape, generator=g, device="cuda") * 0.02).to(torch.bfloat16)
+
+    return [{"wq": w(H * Dh, d), "wk": w(H * Dh, d), "wv": w(H * Dh, d), "wo": w(d, H * Dh), "w_gate": w(F, d), "w_up": w(F, d),
+             "w_down": w(d, F), "attn_norm": torch.ones(d, device="cuda"), "ffn_norm": torch.ones(d, device="cuda")}
+            for _ in range(nl)]
+
+
 def run_backbone(batches=(1, 16), n_new: int = 4, steps: int = 10, warmup: int = 2):
     """The backbone's incremental forward (the producer of the appended rows) at LLaMA-7B shapes -- 32 layers, width
     4096, 32 x 128 heads, SwiGLU 11008, synthetic weights N(0, 0.02^2) drawn on the GPU -- appending n_new tokens per
@@ -449,19 +466,11 @@ def run_backbone(batches=(1, 16), n_new: int = 4, steps: int = 10, warmup: int =
 
     from paper_2607_15621_amd import fsx
 
-    nl, d, H, Dh, F = 32, 4096, 32, 128, 11008
     g = torch.Generator(device="cuda")
     g.manual_seed(2024)
     bf = torch.bfloat16
-
-    def w(*shape):
-        return (torch.randn(shape, generator=g, device="cuda") * 0.02).to(bf)
-
-    layers = []
-    for _ in range(nl):
-        layers.append({"wq": w(H * Dh, d), "wk": w(H * Dh, d), "wv": w(H * Dh, d), "wo": w(d, H * Dh),
-                       "w_gate": w(F, d), "w_up": w(F, d), "w_down": w(d, F),
-                       "attn_norm": torch.ones(d, device="cuda"), "ffn_norm": torch.ones(d, device="cuda")})
+    nl, d, H, Dh, F = LLAMA_7B
+    layers = llama_layers(g)
     cfg = fsx.BackboneCfg(nl, d, H, Dh, F, n_new, max(batches), fsx.BF16, 10000.0, 1e-6)
     bb = fsx.Backbone(cfg, layers)
     torch.cuda.synchronize()
@@ -489,6 +498,63 @@ def run_backbone(batches=(1, 16), n_new: int = 4, steps: int = 10, warmup: int =
     bb.close()
     torch.cuda.empty_cache()
     return out
+
+
+# Whole prompts through fsx_backbone_rebuild: the paper's 224-row history, longer ones, and many vehicles.
+REBUILDS = ((224,), (1000,), (4096,), (224,) * 16, (1024,) * 16)
+
+
+def run_rebuild(steps: int, warmup: int, out_md: str, command: str):
+    """Times of a cache rebuilt from whole prompts at LLaMA-7B shapes, against appends of 64 rows at a time from empty rings."""
+    import torch
+
+    from paper_2607_15621_amd import fsx
+
+    g = torch.Generator(device="cuda")
+    g.manual_seed(2024)
+    nl, d, H, Dh, F = LLAMA_7B
+    agents = max(len(lens) for lens in REBUILDS)
+    bb = fsx.Backbone(fsx.BackboneCfg(nl, d, H, Dh, F, 64, agents, fsx.BF16, 10000.0, 1e-6, max(sum(lens) for lens in REBUILDS)),
+                      llama_layers(g))
+    torch.cuda.empty_cache()
+    info, stream = bb.info(), torch.cuda.current_stream()
+    out = ["# Caches rebuilt from whole prompts", "",
+           f"`fsx_backbone_rebuild` at LLaMA-7B shapes ({nl} layers, width {d}, {H} heads x {Dh}, SwiGLU {F}), synthetic weights, seeded "
+           f"synthetic tokens; {steps} back-to-back calls timed with HIP events after {warmup} warm-up calls. FLOPs: two per weight "
+           "and row, and four per channel of every visible (row, key) pair and head. Appends: the same rows by "
+           "`fsx_backbone_append`, at most 64 per agent and call, from empty rings into a bf16 cache. "
+           f"Workspace of the handle ({max(sum(lens) for lens in REBUILDS):,} rows): {info['workspace_bytes'] / 2 ** 30:.2f} GiB.", "",
+           f"Command: `{command}`", "",
+           "| agents | rows per agent | bf16 cache, ms | TFLOP/s | fp8 cache, ms | as appends, ms |", "|---:|---:|---:|---:|---:|---:|"]
+    for lens in REBUILDS:
+        B, n = len(lens), lens[0]
+        tok = torch.randn(B * n, d, generator=g, device="cuda").to(torch.bfloat16)
+        flops = B * (n * info["weight_bytes"] + nl * H * 2 * n * (n + 1) * Dh)  # a weight is two bytes
+        ms = {}
+        for dtype, torch_type in ((fsx.BF16, torch.bfloat16), (fsx.FP8_E4M3, torch.uint8)):
+            k, v = (torch.zeros(B, nl, H, n, Dh, dtype=torch_type, device="cuda") for _ in "kv")
+            scales = [torch.ones(B, nl, H, device="cuda") if dtype == fsx.FP8_E4M3 else None for _ in "kv"]
+            desc = fsx.CacheDesc(k, v, dtype, nl, H, Dh, n, [0] * B, k_scale=scales[0], v_scale=scales[1])
+            ms[dtype] = 1e3 * time_launches(lambda: bb.rebuild(desc, tok, lens, stream=stream), stream, steps, warmup)
+            if dtype == fsx.BF16:
+                rows = tok.view(B, n, d)
+                parts = [rows[:, i:i + 64].contiguous() for i in range(0, n, 64)]
+
+                def appends():
+                    for x in (desc.start, desc.len, desc.pos):
+                        x[:] = [0] * B
+                    for p in parts:
+                        bb.append(desc, p, B, p.shape[1], None, fsx.APPEND_RING, stream)
+
+                ms["appends"] = 1e3 * time_launches(appends, stream, steps, warmup)
+            del k, v, desc
+        out.append(f"| {B} | {n:,} | {ms[fsx.BF16]:.2f} | {flops / ms[fsx.BF16] / 1e9:.0f} | {ms[fsx.FP8_E4M3]:.2f} | {ms['appends']:.1f} |")
+        print(f"# rebuild {B} x {n}: {out[-1]}", file=sys.stderr, flush=True)
+        del tok
+        torch.cuda.empty_cache()
+    bb.close()
+    with open(out_md, "w") as f:
+        f.write("\n".join(out) + "\n")
 
 
 # Tick time across cache lengths (one agent) and agent counts (1,024 rows each) of the full-size expert, bf16 cache,
@@ -682,6 +748,7 @@ def main():
     ap.add_argument("--sweep", metavar="MD", help="time the tick across cache lengths and agent counts and write "
                     "the table to MD")
     ap.add_argument("--sweep-cache", choices=("bf16", "fp8"), default="bf16", help="cache element type of --sweep")
+    ap.add_argument("--rebuild", metavar="MD", help="time caches rebuilt from whole prompts and write the table to MD")
     ap.add_argument("--phase-trace", metavar="MD", help="per-phase times of the workloads' ticks from the kernel's "
                     "timestamps, written to MD")
     args = ap.parse_args()
@@ -719,6 +786,10 @@ def main():
         run_sweep(args.steps, args.warmup, args.sweep, " ".join(["python", "bench.py"] + argv), args.sweep_cache)
         torch.cuda.synchronize()
         torch.cuda.empty_cache()
+        return
+    if args.rebuild:
+        argv = [os.path.basename(x) if x == args.rebuild else x for x in sys.argv[1:]]
+        run_rebuild(args.steps, args.warmup, args.rebuild, " ".join(["python", "bench.py"] + argv))
         return
     stream = torch.cuda.current_stream()
     names = [n for n in args.workload.split(",") if n]
