@@ -264,7 +264,8 @@ const char* fsx_loop_last_error(void);
  * Every K ticks the current frame's tokens go through the frozen backbone (LLaMA-7B: 32 layers, width 4096, 32
  * heads x 128, SwiGLU 11008) as an incremental forward over its cache: at every layer each new token attends to
  * the cached rows and to the new tokens up to itself, and its rotated key and value become the layer's appended
- * row.  The cost does not depend on the history length beyond the attention over the cached rows. */
+ * row.  The cost does not depend on the history length beyond the attention over the cached rows.  Calls that overlap on one
+ * backbone handle (from two streams or two captured graphs) race on its workspace. */
 typedef struct fsx_backbone fsx_backbone;
 typedef struct {
   int32_t n_layers, d_model, n_heads, head_dim, d_ffn;  /* head_dim 128; d_model and d_ffn multiples of 32 */
@@ -352,7 +353,8 @@ typedef struct {
  *   workspace DEVICE, 16-byte aligned, at most workspace_bytes of it are used, for the partial results of keys that are
  *             split over workgroups where the queries are few; with less than fsx_prompt_attention_workspace says the keys
  *             are split less, with none (NULL, 0) not at all.  Calls that overlap must not share one.
- * Scores, softmax statistics and sums are fp32; the probabilities are rounded to bf16 for the matrix instructions.
+ * Scores, softmax statistics and sums are fp32; the probabilities are rounded to bf16 for the matrix instructions.  A weight is
+ * at most 2^8 until the end divides by their sum, so values beyond 2^119 / (keys seen) may overflow a sum.
  * Deterministic: the same arguments give the same bits. */
 int fsx_prompt_attention(const fsx_prompt_desc* desc, const void* q, const void* k, const void* v, void* out, float* lse,
                          int32_t n_seq, const int64_t* q_start, const int64_t* q_len, const int64_t* k_start,
@@ -385,8 +387,8 @@ int fsx_cache_replace_rows(fsx_cache_desc* cache, int32_t layer, int32_t n_layer
  *                   go to row_start[b] .. row_start[b] + row_len[b] - 1 (HOST [cache->batch]; the ranges must not overlap);
  *                   either may be NULL and is then not read
  * FP8_E4M3 rows are code * scale in fp32, rounded once to rows_dtype; other rows are copied or rounded once.  first + row_len
- * beyond the agent's valid rows is FSX_E_CAPACITY.  Shared caches are read through each agent's own start and len.  head_dim
- * as fsx_cache_replace_rows. */
+ * beyond the agent's valid rows is FSX_E_CAPACITY; an agent with row_len 0 is passed over.  Shared caches are read through each
+ * agent's own start and len.  head_dim as fsx_cache_replace_rows. */
 int fsx_cache_read_rows(const fsx_cache_desc* cache, int32_t layer, int32_t n_layers, const int64_t* first, void* k_rows,
                         void* v_rows, int32_t rows_dtype, int64_t total_rows, const int64_t* row_start,
                         const int64_t* row_len, void* stream);

@@ -37,9 +37,10 @@ __device__ __forceinline__ uint2 lds_column4(const char* p) {
   return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p)));
 }
 
-// Where 16-byte piece p of a tile's row lies: in row-piece p ^ k_turn (keys) or p ^ v_turn (values), so that the 16 rows (four
-// rows, two pieces each) that a read takes at once lie in different banks.  With the pieces in order the reads of 32 rows
-// took 16 times (values: twice) as long.
+// Where 16-byte piece p of a tile's row lies: in row-piece p ^ k_turn (keys) or p ^ v_turn (values), so that the reads of a column
+// of rows are spread over the banks.  With the pieces in order the reads of 32 rows took 16 times (values: twice) as long.  Reads
+// of keys, and of values 64 channels wide, meet no bank twice; a read of values 128 wide takes four rows and four pieces at once,
+// of which rows 0 and 1, and 2 and 3, share banks: four cycles instead of two (SQ_LDS_BANK_CONFLICT: 2 per such read).
 template <int D>
 __device__ __forceinline__ int k_turn(int row) { return D == 128 ? row & 15 : (row >> 1) & 7; }
 template <int D>
@@ -88,7 +89,9 @@ struct PromptState {
   float m, l;
 };
 
-// The wave's queries as the B operand: step s, lane l: channels 16 s + 8 (l / 32) .. + 7 of query l % 32.
+// The wave's queries as the B operand: step s, lane l: channels 16 s + 8 (l / 32) .. + 7 of query l % 32.  Where they come in fp32
+// they are rounded to bf16 (at most 2^-8 of each, as the keys that they meet were: fp32 matrix instructions run at a sixteenth of
+// the rate).
 template <int D>
 __device__ __forceinline__ void load_queries(const PromptArgs& a, int64_t at, int half, uint4 (&qf)[D / 16]) {
   if (a.q_f32) {
@@ -168,8 +171,10 @@ __device__ __forceinline__ void tile_scores(const char* kt, const uint4 (&qf)[D 
 // The tile's probabilities (B operand of the second product) from its scores, and the state's maximum and sum.  lim: the last
 // key (counted from the tile's first) that the lane's query sees; masked: whether some query does not see all of them.  between(i)
 // runs after the exponentials of the i-th 16-key step.
-// The maximum that the exponents are taken from is raised only where they would pass 2^8 (the sums are fp32, and a probability's
-// rounding to bf16 is relative), so the exponentials need not wait for the tile's own maximum; a tile that raises it does them again.
+// The probabilities are rounded to bf16, at most 2^-8 of each, for a second product on the bf16 matrix instructions (fp32 ones run
+// at a sixteenth of the rate); their sum is taken before the rounding, in fp32.
+// The maximum that the exponents are taken from is raised only where they would pass 2^8 (sums in fp32 and relative roundings do not
+// mind), so the exponentials need not wait for the tile's own maximum; a tile that raises it does them again.
 template <int D, int KB, class Between>
 __device__ __forceinline__ void tile_softmax(f32x16 (&s)[KB], float c, int lim, bool masked, int half, PromptState<D>& st, uint4 (&pf)[2 * KB],
                                              Between between) {
@@ -343,12 +348,13 @@ __device__ __forceinline__ uint32_t lds_address(const void* p) {
 }
 
 // Four waves take 128 rows and walk over the keys in step, one tile ahead; two such workgroups share a CU (three with heads of 64
-// channels: 16 prompts of 1,024 tokens 119 us with two, 105 with three, 145 with four, which spill), and one starts or ends while
-// the other computes.
-// Bound: LDS.  Of a tile a wave reads 32 KB for 32 products' 1,024 cycles, the transposing reads at half the rate of the
-// others, and the tiles are written besides: 2,000 of the 4,100 cycles that two workgroups take for a tile each, beside 2,048
-// of products; in k_prompt_turns, whose reads are the same, the longest prompt took 1,210 us instead of 1,890 without LDS reads
-// and tile loads.
+// channels: 16 prompts of 1,024 tokens 119 us with two, 105 with three, 145 with four, which spill in the main loop; here 9 and,
+// with 128 channels, 13 registers spill on the way through the second run over the tiles), and one starts or ends while the other
+// computes.
+// Bound: no unit is full.  16 prompts of 1,024 tokens (208 us at 2.07 GHz): matrix units 32 % of the cycles, LDS reads 24 %, a third
+// of those in bank conflicts of the values; a wave spends 30 % of its cycles waiting to issue.  What is left is the chain of a
+// tile (scores, softmax, values), which two waves per SIMD cover in part, and the start and end of workgroups.  In k_prompt_turns
+// (matrix units 56 %, LDS 42 %) the longest prompt took 1,210 us instead of 1,890 without LDS reads and tile loads.
 template <int D>
 __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void k_prompt_tiles(PromptArgs a) {
   constexpr int NW = 4, RB = 2 * D, TILE = PT_KEYS * RB, RPI = 1024 / RB, NI = PT_KEYS / RPI / NW;  // rows and loads per wave's load

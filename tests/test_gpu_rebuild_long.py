@@ -4,11 +4,11 @@ attention, with narrow and wide rows, against the forward in 64 bits.
 The weights of the synthetic backbone (N(0, 0.02^2)) give scores of a few tenths, an almost uniform softmax that hardly shows what
 the attention does.  Here its projections are four times as large: scores have a standard deviation of (0.08 sqrt(d))^2, 3 to 16 at
 the widths below, and the reference with a softmax in another base is shown to differ by more than the tolerance allows.  Scores
-as large as 60 move by 60 x 2^-8 = 0.2 when queries and keys are rounded to bf16, so the reference, in 64 bits otherwise, rounds
+as large as 60 move by up to 60 x 2^-7 = 0.5 when queries and keys are rounded to bf16, so the reference, in 64 bits otherwise, rounds
 to bf16 where the backbone does: projection inputs, scaled queries, keys, values, attention outputs and SwiGLU outputs; and each layer starts
 from the hidden states that the call gave for the layer before, as roundings of one layer would come back in the next one's scores.
-What is left are the probabilities' rounding (2^-9 of a value) and elements that fp32 sums round to the other side, 2^-8 of an
-element each; the tolerance is the incremental forward's, relative to the largest magnitude."""
+What is left are the probabilities' rounding (at most 2^-8 of each, most of it averaged over the keys) and elements that fp32 sums
+round to the other side, 2^-7 of an element each; the tolerance is the incremental forward's, relative to the largest magnitude."""
 
 from __future__ import annotations
 
