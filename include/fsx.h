@@ -376,7 +376,7 @@ int fsx_prompt_attention_workspace(const fsx_prompt_desc* desc, int32_t n_seq, c
  *                   FSX_E_CAPACITY and nothing is written
  * The ring state of a replaced agent becomes start 0, len = the rows kept, pos = row_len, on the host before returning; layers
  * may be replaced one call at a time (each sets the same state), and the cache is whole again after the last.  head_dim must
- * be a multiple of 16 of at most 512; a shared cache is refused with FSX_E_UNSUPPORTED. */
+ * be a multiple of 16 of at most 512, batch * n_layers * n_heads at most 2^29; a shared cache is refused with FSX_E_UNSUPPORTED. */
 int fsx_cache_replace_rows(fsx_cache_desc* cache, int32_t layer, int32_t n_layers, const void* k_rows, const void* v_rows,
                            int32_t rows_dtype, int64_t total_rows, const int64_t* row_start, const int64_t* row_len,
                            float headroom, int32_t policy, void* stream);
@@ -388,7 +388,7 @@ int fsx_cache_replace_rows(fsx_cache_desc* cache, int32_t layer, int32_t n_layer
  *                   either may be NULL and is then not read
  * FP8_E4M3 rows are code * scale in fp32, rounded once to rows_dtype; other rows are copied or rounded once.  first + row_len
  * beyond the agent's valid rows is FSX_E_CAPACITY; an agent with row_len 0 is passed over.  Shared caches are read through each
- * agent's own start and len.  head_dim as fsx_cache_replace_rows. */
+ * agent's own start and len.  head_dim and the number of heads as fsx_cache_replace_rows. */
 int fsx_cache_read_rows(const fsx_cache_desc* cache, int32_t layer, int32_t n_layers, const int64_t* first, void* k_rows,
                         void* v_rows, int32_t rows_dtype, int64_t total_rows, const int64_t* row_start,
                         const int64_t* row_len, void* stream);

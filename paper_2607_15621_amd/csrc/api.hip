@@ -1055,6 +1055,8 @@ static int check_rows(const fsx_cache_desc* c, int32_t layer, int32_t n_layers, 
   if (rc) return rc;
   if (c->n_layers <= 0 || c->n_heads <= 0 || c->head_dim <= 0) return fail(FSX_E_INVALID, "cache geometry must be positive");
   if (c->head_dim % 16 || c->head_dim > 512) return fail(FSX_E_UNSUPPORTED, "head_dim must be a multiple of 16 of at most 512");
+  if ((__int128)c->batch * c->n_layers * c->n_heads > 1 << 29)
+    return fail(FSX_E_UNSUPPORTED, "more than 2^29 agents x layers x heads");
   if (layer < 0 || n_layers < 1 || layer > c->n_layers - n_layers)
     return fail(FSX_E_INVALID, "layers outside 0..n_layers-1 of the cache");
   if (rows_dtype != FSX_BF16 && rows_dtype != FSX_F32) return fail(FSX_E_INVALID, "rows must be BF16 or F32");

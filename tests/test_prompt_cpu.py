@@ -250,3 +250,11 @@ def test_rows_of_a_rebuild_are_limited_at_create(rows, heads, code):
     out = ctypes.c_void_p(1)
     assert fsx.lib().fsx_backbone_create(ctypes.byref(cfg), None, None, ctypes.byref(out)) == code
     assert out.value is None and "max_prompt_rows" in fsx.last_error()
+
+
+@pytest.mark.parametrize("H,L", [(1 << 20, 1 << 10), (1 << 16, 1 << 16)])
+def test_caches_with_more_scales_than_an_index_holds_are_refused(H, L):
+    c = cache(H=H, L=L, D=16, cap=1, lengths=(0, 0, 0))
+    for code, msg in (replace(c, lens=(1, 0, 0), total=1, n_layers=L), read(cache(H=H, L=L, D=16, cap=1, lengths=(1, 0, 0)), lens=(1, 0, 0),
+                                                                            total=1, n_layers=L)):
+        assert code == UNSUPPORTED and "2^29" in msg, msg
