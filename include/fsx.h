@@ -393,6 +393,119 @@ int fsx_cache_read_rows(const fsx_cache_desc* cache, int32_t layer, int32_t n_la
                         void* v_rows, int32_t rows_dtype, int64_t total_rows, const int64_t* row_start,
                         const int64_t* row_len, void* stream);
 
+/* ---- Rotary positions with several axes ----
+ * Channel pair j of every head is turned by the angle positions[axis[j]] * freq[j]: (x_a, x_b) becomes
+ * (x_a cos - x_b sin, x_b cos + x_a sin).  One axis is a token's place in a text; three are the time, height and width of a piece
+ * of a frame.  Queries and keys that lie side by side in a row are turned in one call, before fsx_prompt_attention or
+ * fsx_pages_write. */
+enum {
+  FSX_ROTARY_HALVES = 0,   /* pair j is channels (j, j + n_pairs), as in fsx_expert_cfg.rope_base and fsx_backbone_cfg */
+  FSX_ROTARY_ADJACENT = 1  /* pair j is channels (2 j, 2 j + 1) */
+};
+typedef struct {
+  int32_t dtype;        /* of x and y: FSX_BF16 or FSX_F32 */
+  int32_t n_heads;      /* 1..4096 */
+  int32_t head_dim;     /* 2..1024 */
+  int32_t n_pairs;      /* 1..128, 2 * n_pairs <= head_dim; channels from 2 * n_pairs on stay as they are */
+  int32_t layout;       /* FSX_ROTARY_* */
+  int32_t n_axes;       /* 1..256 */
+  int32_t inverse;      /* 1: turned back by the angles (the gradient of the rotation), else 0 */
+  const int32_t* axis;  /* HOST [n_pairs], 0..n_axes-1 */
+  const double* freq;   /* HOST [n_pairs], radians per step, of any sign, at most 2^20 */
+  int64_t x_row, x_head, y_row, y_head;  /* strides in elements: row r, head h, channel c of x is x[r * x_row + h * x_head + c] */
+  int64_t pos_axis, pos_row;             /* strides of positions in elements: axis a of row r is positions[a * pos_axis + r * pos_row] */
+} fsx_rotary_desc;
+/* Rows 0..n_rows-1 (at most 2^26) of x into y, DEVICE.  y may be x, with the same strides; otherwise they must not overlap (heads of
+ * the same rows may: a row's queries and keys beside what was not turned), and no element of y lie twice.
+ *   positions DEVICE int32, of any sign and size.  The angle's place in its turn is exact whatever the position (off by less than
+ *             2^-32 turns and the rounding of freq); sine and cosine are fp32, off by at most 2^-22, products and sums fp32,
+ *             rounded once to dtype */
+int fsx_rotary_rows(const fsx_rotary_desc* desc, const void* x, void* y, const int32_t* positions, int64_t n_rows, void* stream);
+
+/* ---- Pages: caches of many sequences in one pool ----
+ * Where the sequences of a batch grow, fork (several plans from one history) and drop rows from their middle (the oldest frames
+ * behind the instruction), rings of one capacity each waste memory.  A pool holds pages of page_rows cached rows of every layer; a
+ * sequence is a list of pages and a length, its row i being row i mod page_rows of its page i / page_rows.  Forked sequences share
+ * pages; before a sequence's new rows are written, a shared last page is copied.
+ *
+ * The handle keeps the lists twice: on the host, where the calls that change them (extend, fork, keep, free) check and account, and
+ * on the device, where fsx_pages_write and fsx_pages_attention read them.  Those calls change the host's lists before they return
+ * and enqueue the device's on `stream`; on an error nothing is enqueued and no list changes (FSX_E_HIP apart: the handle then refuses
+ * further calls).  They are refused while `stream` is captured into a graph (FSX_E_UNSUPPORTED: a replay would undo later changes);
+ * fsx_pages_write and fsx_pages_attention may be captured, and read the lists and lengths as they stand when they run, so a captured
+ * decoding step is: fsx_pages_extend, then the replay.
+ * Work of a handle must be ordered: calls from one thread at a time, on one stream or on streams that the caller orders. */
+typedef struct fsx_pages fsx_pages;
+typedef struct {
+  int32_t dtype;          /* FSX_BF16, or FSX_FP8_E4M3 with a scale for every row of a head (stored value = code * scale) */
+  int32_t n_layers;       /* 1..1024 */
+  int32_t n_kv_heads;     /* 1..1024 */
+  int32_t head_dim;       /* 64 or 128 (FSX_E_UNSUPPORTED otherwise) */
+  int32_t page_rows;      /* 16, 32, 64, 128 or 256 */
+  int32_t n_pages;        /* pages of the pool, at least 1; the tensors' rows may pass 2^31 elements */
+  int32_t max_seqs;       /* sequences 0..max_seqs-1, at most 65536 */
+  int32_t max_seq_pages;  /* pages of one sequence, max_seq_pages * page_rows at most 2^28; max_seqs * max_seq_pages at most 2^28 */
+  void* k;                /* DEVICE [n_layers][n_pages][n_kv_heads][page_rows][head_dim], 16-byte aligned, the caller's; must */
+  void* v;                /* outlive the handle.  Rows that no sequence has may hold anything, infinities and NaN included */
+  float* k_scale;         /* FP8 only: DEVICE [n_layers][n_pages][n_kv_heads][page_rows], 16-byte aligned */
+  float* v_scale;
+} fsx_pages_cfg;
+/* All pages free, all sequences empty.  The lists' device memory is the handle's; `stream` is synchronised. */
+int fsx_pages_create(const fsx_pages_cfg* cfg, void* stream, fsx_pages** out);
+/* Frees the lists once the device is idle; NULL is a no-op. */
+void fsx_pages_destroy(fsx_pages* pages);
+/* Room for rows[i] (0: none) more rows at the end of sequence seqs[i] (none twice; HOST [n]), whose contents fsx_pages_write sets.
+ * The lowest free pages are taken, in the order of seqs.  A last page that is shared and not full is first copied, its used rows
+ * bit for bit in all layers (of several sharers in one call the last keeps it if no other sequence has it).
+ * FSX_E_CAPACITY: too few free pages, or a sequence would pass max_seq_pages. */
+int fsx_pages_extend(fsx_pages* pages, int32_t n, const int32_t* seqs, const int32_t* rows, void* stream);
+/* Sequence dst[i], which has no rows, gets the first rows[i] (NULL: all) rows of src[i]: shared pages, nothing is copied.  No dst
+ * twice, and none that is also a src; a src may be forked several times. */
+int fsx_pages_fork(fsx_pages* pages, int32_t n, const int32_t* src, const int32_t* dst, const int32_t* rows, void* stream);
+/* Sequence seqs[i] (none twice) keeps rows first[r] .. first[r] + count[r] - 1 of its n_ranges[i] ranges and no others; they close
+ * up, and pages that are no longer needed become free.  first and count hold the ranges of all sequences one after the other,
+ * ascending and apart within each (at most 256 for a sequence: FSX_E_UNSUPPORTED beyond).  One range from 0 cuts the end off and moves nothing.  Rows are moved
+ * in place in pages that the sequence has alone; shared pages from the first moved row on are replaced, which takes free pages
+ * (FSX_E_CAPACITY).  Rows keep their rotary positions, scales and bits. */
+int fsx_pages_keep(fsx_pages* pages, int32_t n, const int32_t* seqs, const int32_t* n_ranges, const int32_t* first,
+                   const int32_t* count, void* stream);
+/* The sequences (none twice) have no rows any more; pages that no other has become free.  An empty sequence stays empty. */
+int fsx_pages_free(fsx_pages* pages, int32_t n, const int32_t* seqs, void* stream);
+/* The lists as the host has them (any pointer may be NULL): len HOST [max_seqs], table HOST [max_seqs][max_seq_pages] (-1: no page),
+ * the number of free pages. */
+int fsx_pages_tables(const fsx_pages* pages, int32_t* len, int32_t* table, int64_t* free_pages);
+/* Packed rows of sequences as in fsx_prompt_attention (row_start, row_len HOST [n]): the row_len[i] rows become the last rows of
+ * seqs[i] (none twice), in layers layer .. layer + n_layers - 1.  Element (layer l, row r, head h, channel c) of k_rows is
+ * k_rows[l * k_layer + r * k_row + h * k_head + c], 16-byte aligned, strides multiples of 8.
+ * BF16 pages: a copy, or one rounding (rows_dtype FSX_F32).  FP8 pages: per row and head scale = max(amax / 448, 2^-126) in fp32,
+ * amax the row's largest finite magnitude (1 where that is 0), and the codes of fsx_cache_append_rows_quantize with it.
+ * FSX_E_INVALID: a sequence has fewer rows, or some of the rows lie in a page that another sequence has too (extend first). */
+typedef struct {
+  int32_t rows_dtype;  /* FSX_BF16 or FSX_F32 */
+  int32_t layer, n_layers;
+  int64_t total_rows;  /* rows that k_rows and v_rows hold */
+  int64_t k_layer, k_row, k_head, v_layer, v_row, v_head;
+} fsx_pages_rows;
+int fsx_pages_write(fsx_pages* pages, const fsx_pages_rows* desc, const void* k_rows, const void* v_rows, int32_t n,
+                    const int32_t* seqs, const int64_t* row_start, const int64_t* row_len, void* stream);
+/* Attention of one new token of each of n sequences (1..65536; a sequence may be named more than once) over all its rows in `layer`,
+ * the token's own among them once it is written.  Row i of q (n_heads query heads, a multiple of the pool's n_kv_heads: head h reads
+ * key head h / (n_heads / n_kv_heads)) belongs to seqs[i].  A sequence without rows gives 0, and a lse of -infinity.
+ *   desc      as in fsx_prompt_attention: n_heads, n_kv_heads and head_dim (equal to the pool's), q_dtype, out_dtype, scale, q_rows
+ *             (at least n), q_row, q_head, out_row, out_head; the other fields are not read
+ *   lse       DEVICE [n][n_heads] fp32, to merge with another part by, or NULL
+ *   workspace DEVICE, 16-byte aligned, for the parts of long sequences, at most workspace_bytes of it are used; with less than
+ *             fsx_pages_attention_workspace says, the sequences are cut into fewer parts, with none (NULL, 0) into one.  Calls that
+ *             overlap must not share one.
+ * How many parts follows from the lengths at the time of the call; a replay in a graph cuts the lengths it finds into as many.
+ * Numerics as fsx_prompt_attention (fp8 rows are decoded exactly, their scales applied in fp32: a value's to its weight before that is
+ * rounded to bf16).  Deterministic: the same arguments and lengths give the same bits. */
+int fsx_pages_attention(fsx_pages* pages, const fsx_prompt_desc* desc, int32_t layer, const void* q, void* out, float* lse,
+                        int32_t n, const int32_t* seqs, void* workspace, int64_t workspace_bytes, void* stream);
+/* The most workspace the call would use now (0: none). */
+int fsx_pages_attention_workspace(const fsx_pages* pages, const fsx_prompt_desc* desc, int32_t n, const int32_t* seqs,
+                                  int64_t* bytes);
+
 /* Synchronise `stream` and report whether the ticks enqueued on this handle completed: FSX_OK, or
  * FSX_E_HIP if a tick kernel gave up on a wait (its waypoints were then written as NaN).  The
  * failure is reported once per failed tick and cleared by reporting it. */

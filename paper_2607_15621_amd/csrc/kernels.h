@@ -4,10 +4,17 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <string>
+#include <vector>
+
 #include "../../include/fsx.h"
 #include "head_device.h"
+#include "page_lists.h"
 
 namespace fsx {
+
+// Sets the calling thread's message of fsx_last_error ("" clears it) and returns code.
+int set_error(int code, const std::string& msg);
 
 // Per-forward description of the agents, passed by value in kernel arguments.
 struct TickParams {
@@ -262,6 +269,89 @@ struct RowsArgs {
 };
 hipError_t launch_replace_rows(const RowsArgs& a, hipStream_t s);
 hipError_t launch_read_rows(const RowsArgs& a, hipStream_t s);
+
+// ------------------------------------------------------------------ rotary positions
+constexpr int ROTARY_PAIRS = 128;
+struct RotaryArgs {
+  const void* x;
+  void* y;
+  const int32_t* pos;
+  int64_t x_row, x_head, y_row, y_head, pos_axis, pos_row;  // elements
+  int64_t rows;
+  int32_t heads, dim, pairs, f32, adjacent, inverse;
+  int32_t copy_rest;                // channels past the pairs are copied (y is not x)
+  int32_t block;                    // rows of a workgroup
+  uint64_t turn[ROTARY_PAIRS];      // turns per step of the pair's axis, mod 1, in units of 2^-64
+  uint8_t axis[ROTARY_PAIRS];
+};
+hipError_t launch_rotary(RotaryArgs a, hipStream_t s);
+
+// ------------------------------------------------------------------ pages
+// A pool of pages [layers][pages][Hk][P][D] and, on the device, every sequence's list [sequences][most] and length.
+struct PagePool {
+  void* k;
+  void* v;
+  float* k_scale;  // [layers][pages][Hk][P], fp8 only
+  float* v_scale;
+  const int32_t* table;
+  const int32_t* len;
+  int32_t layers, pages, Hk, P, shift, D, fp8, most;  // P = 1 << shift
+};
+// Entries of lists and lengths, and pages copied.
+constexpr int PAGE_RUNS = 80, PAGE_COPIES = 150;
+struct PageUpdateArgs {
+  PagePool pool;
+  int32_t* table;  // written; copied entries come from pool.table
+  int32_t* len;    // NULL: lengths stay
+  int32_t n_runs, n_copies;
+  PageRun runs[PAGE_RUNS];
+  PageCopy copies[PAGE_COPIES];
+};
+hipError_t launch_page_update(const PagePool& pool, int32_t* table, int32_t* len, const std::vector<PageRun>& runs,
+                              const std::vector<PageCopy>& copies, hipStream_t s);
+// Rows that close up: row i of the outcome, from `start` on, is row i - to + first of the last range with to <= i.
+constexpr int PAGE_MOVES = 64, PAGE_RANGES = 256;
+struct PageMoveArgs {
+  PagePool pool;
+  const int32_t* to_table;
+  int32_t n_moves;
+  PageMove moves[PAGE_MOVES];
+  PageRange ranges[PAGE_RANGES];  // count: the first row's place in the outcome
+};
+hipError_t launch_page_move(const PagePool& pool, const int32_t* to_table, const std::vector<PageMove>& moves,
+                            const std::vector<PageRange>& ranges, hipStream_t s);
+// Packed rows into the last rows of sequences.
+constexpr int PAGE_WRITES = 128;
+struct PageWriteArgs {
+  PagePool pool;
+  const void* k;
+  const void* v;
+  int64_t k_layer, k_row, k_head, v_layer, v_row, v_head;  // elements
+  int32_t rows_f32, layer, n_layers;
+  int32_t n, block;      // entries; rows of a workgroup
+  int64_t start[PAGE_WRITES];
+  int32_t seq[PAGE_WRITES], rows[PAGE_WRITES], block_prefix[PAGE_WRITES + 1];
+};
+hipError_t launch_page_write(PageWriteArgs a, int n, const int32_t* seqs, const int64_t* start, const int64_t* rows, hipStream_t s);
+// One new token of every entry's sequence over its pages.
+constexpr int PAGE_QUERIES = 256;
+struct PageAttentionArgs {
+  PagePool pool;
+  const void* q;
+  void* out;
+  float* lse;            // [n][H] or NULL
+  float* part;           // states of the workgroups
+  int64_t q_row, q_head, o_row, o_head;  // elements
+  int32_t H, G, layer, q_f32, o_f32;
+  float c;               // scores in log2 units = c * q.k
+  int32_t n, row;        // entries, and the row of the first
+  int32_t seq[PAGE_QUERIES];
+  int32_t prefix[PAGE_QUERIES + 1];  // parts of the entries before
+};
+// Parts of every entry's keys and the workspace's bytes, at most workspace_bytes.
+int64_t plan_page_attention(const PagePool& pool, int H, int n, const int32_t* seqs, const int32_t* host_len, int64_t workspace_bytes,
+                            std::vector<int32_t>& parts);
+hipError_t launch_page_attention(PageAttentionArgs a, int n, const int32_t* seqs, const std::vector<int32_t>& parts, hipStream_t s);
 
 // ------------------------------------------------------------------ simple per-op path (any dtype)
 struct GenericWeights {

@@ -23,6 +23,7 @@ CACHE_HEAD_MAJOR, CACHE_TOKEN_MAJOR, CACHE_SHARED = 0, 1, 2
 FLAG_GENERIC, FLAG_MULTI_LAUNCH, FLAG_TRACE = 1, 2, 4
 HEAD_MEAN_LINEAR, HEAD_QUERY_MLP = 0, 1
 PROMPT_AUTO, PROMPT_CHUNKS, PROMPT_TILES, PROMPT_TURNS = 0, 1, 2, 3
+ROTARY_HALVES, ROTARY_ADJACENT = 0, 1
 MAX_BATCH = 64
 STATUS = {0: "FSX_OK", 1: "FSX_E_INVALID", 2: "FSX_E_UNSUPPORTED", 3: "FSX_E_CAPACITY", 4: "FSX_E_OOM",
           5: "FSX_E_HIP"}
@@ -32,7 +33,9 @@ SYMBOLS = ("fsx_expert_create", "fsx_expert_forward", "fsx_cache_append_rows", "
            "fsx_loop_create", "fsx_loop_tick", "fsx_loop_append", "fsx_loop_sync", "fsx_loop_destroy",
            "fsx_loop_last_error", "fsx_backbone_create", "fsx_backbone_append", "fsx_backbone_info",
            "fsx_backbone_destroy", "fsx_prompt_attention", "fsx_prompt_attention_workspace", "fsx_cache_replace_rows",
-           "fsx_cache_read_rows", "fsx_backbone_rebuild")
+           "fsx_cache_read_rows", "fsx_backbone_rebuild", "fsx_rotary_rows", "fsx_pages_create", "fsx_pages_destroy",
+           "fsx_pages_extend", "fsx_pages_fork", "fsx_pages_keep", "fsx_pages_free", "fsx_pages_tables", "fsx_pages_write",
+           "fsx_pages_attention", "fsx_pages_attention_workspace")
 
 
 class FsxError(RuntimeError):
@@ -78,6 +81,23 @@ class PromptDesc(ctypes.Structure):
                 ("kernel", ctypes.c_int32)] + \
                [(n, ctypes.c_int64) for n in ("q_rows", "k_rows", "q_row", "q_head", "k_row", "k_head", "v_row", "v_head",
                                               "out_row", "out_head")]
+
+
+class RotaryDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("dtype", "n_heads", "head_dim", "n_pairs", "layout", "n_axes", "inverse")] + \
+               [("axis", ctypes.POINTER(ctypes.c_int32)), ("freq", ctypes.POINTER(ctypes.c_double))] + \
+               [(n, ctypes.c_int64) for n in ("x_row", "x_head", "y_row", "y_head", "pos_axis", "pos_row")]
+
+
+class PagesCfg(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("dtype", "n_layers", "n_kv_heads", "head_dim", "page_rows", "n_pages", "max_seqs",
+                                              "max_seq_pages")] + \
+               [(n, ctypes.c_void_p) for n in ("k", "v", "k_scale", "v_scale")]
+
+
+class PagesRows(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("rows_dtype", "layer", "n_layers")] + \
+               [(n, ctypes.c_int64) for n in ("total_rows", "k_layer", "k_row", "k_head", "v_layer", "v_row", "v_head")]
 
 
 class CacheDescC(ctypes.Structure):
@@ -144,6 +164,22 @@ def lib() -> ctypes.CDLL:
         L.fsx_cache_read_rows.argtypes = [ctypes.POINTER(CacheDescC), i32, i32, P64, vp, vp, i32, i64, P64, P64, vp]
         for n in ("fsx_prompt_attention", "fsx_prompt_attention_workspace", "fsx_cache_replace_rows",
                   "fsx_cache_read_rows", "fsx_backbone_rebuild"):
+            getattr(L, n).restype = ctypes.c_int
+        P32 = ctypes.POINTER(i32)
+        L.fsx_rotary_rows.argtypes = [ctypes.POINTER(RotaryDesc), vp, vp, vp, i64, vp]
+        L.fsx_pages_create.argtypes = [ctypes.POINTER(PagesCfg), vp, ctypes.POINTER(vp)]
+        L.fsx_pages_destroy.argtypes = [vp]
+        L.fsx_pages_destroy.restype = None
+        L.fsx_pages_extend.argtypes = [vp, i32, P32, P32, vp]
+        L.fsx_pages_fork.argtypes = [vp, i32, P32, P32, P32, vp]
+        L.fsx_pages_keep.argtypes = [vp, i32, P32, P32, P32, P32, vp]
+        L.fsx_pages_free.argtypes = [vp, i32, P32, vp]
+        L.fsx_pages_tables.argtypes = [vp, P32, P32, P64]
+        L.fsx_pages_write.argtypes = [vp, ctypes.POINTER(PagesRows), vp, vp, i32, P32, P64, P64, vp]
+        L.fsx_pages_attention.argtypes = [vp, ctypes.POINTER(PromptDesc), i32, vp, vp, vp, i32, P32, vp, i64, vp]
+        L.fsx_pages_attention_workspace.argtypes = [vp, ctypes.POINTER(PromptDesc), i32, P32, P64]
+        for n in ("fsx_rotary_rows", "fsx_pages_create", "fsx_pages_extend", "fsx_pages_fork", "fsx_pages_keep", "fsx_pages_free",
+                  "fsx_pages_tables", "fsx_pages_write", "fsx_pages_attention", "fsx_pages_attention_workspace"):
             getattr(L, n).restype = ctypes.c_int
         for n in ("fsx_expert_create", "fsx_expert_forward", "fsx_cache_append_rows", "fsx_expert_info",
                   "fsx_expert_status", "fsx_expert_trace", "fsx_probe_hbm_read"):
@@ -435,6 +471,185 @@ def cache_read_rows(cache: CacheDesc, layer: int, n_layers: int, k_rows, v_rows,
                                      first.ctypes.data_as(ctypes.POINTER(ctypes.c_int64)) if first is not None else None,
                                      _ptr(k_rows), _ptr(v_rows), dtype, total, rows.c_start, rows.c_len,
                                      _stream_on(stream, k_rows, v_rows)))
+
+
+class RotaryPlan:
+    """Which axis channel pair j of a head belongs to, and its radians per step; layout ROTARY_HALVES (pairs (j, j + pairs)) or
+    ROTARY_ADJACENT (pairs (2j, 2j+1))."""
+
+    def __init__(self, axis, freq, layout: int = ROTARY_HALVES):
+        self.axis = np.array(axis, dtype=np.int32).reshape(-1)
+        self.freq = np.array(freq, dtype=np.float64).reshape(-1)
+        if len(self.axis) != len(self.freq):
+            raise ValueError("as many axes as frequencies: one of each for every pair")
+        self.layout = layout
+        self.c_axis = self.axis.ctypes.data_as(ctypes.POINTER(ctypes.c_int32))
+        self.c_freq = self.freq.ctypes.data_as(ctypes.POINTER(ctypes.c_double))
+
+    @classmethod
+    def sections(cls, pairs: Sequence[int], base: float = 10000.0, joint: bool = True, layout: int = ROTARY_HALVES) -> "RotaryPlan":
+        """Axis i gets the next pairs[i] pairs.  joint: one ladder base^(-j / pairs of all axes) over all pairs; else each axis has
+        its own, base^(-j / pairs[i])."""
+        pairs = [int(n) for n in pairs]
+        steps = np.arange(sum(pairs)) / max(1, sum(pairs)) if joint else np.concatenate([np.arange(n) / max(1, n) for n in pairs])
+        return cls(np.repeat(np.arange(len(pairs)), pairs), float(base) ** -steps, layout)
+
+
+def rotary_rows(x, out, positions, plan: RotaryPlan, inverse: bool = False, stream=None):
+    """fsx_rotary_rows: x, out [rows][heads][channels] bfloat16 or float32 (any row and head strides; out may be x), positions
+    [axes][rows] int32 (any strides).  inverse: turned back, the gradient of the rotation."""
+    sx, tx, ty = x.shape, x.stride(), out.stride()
+    if len(sx) != 3 or out.shape != sx or out.dtype != x.dtype or tx[2] != 1 or ty[2] != 1:
+        raise ValueError("x and out must be [rows][heads][channels] of one dtype, with a dense last dimension")
+    if positions.dim() != 2 or positions.shape[1] != sx[0] or positions.element_size() != 4 or positions.is_floating_point():
+        raise ValueError("positions must be int32 [axes][rows]")
+    tp = positions.stride()
+    d = RotaryDesc(_dtype_of(x), sx[1], sx[2], len(plan.axis), plan.layout, positions.shape[0], int(inverse), plan.c_axis, plan.c_freq,
+                   tx[0], tx[1], ty[0], ty[1], tp[0], tp[1])
+    _check(lib().fsx_rotary_rows(ctypes.byref(d), _ptr(x), _ptr(out), _ptr(positions), sx[0], _stream_on(stream, x, out, positions)))
+
+
+def _int32s(values, what: str):
+    """A dense int32 array and its pointer."""
+    a = values if isinstance(values, np.ndarray) and values.dtype == np.int32 and values.ndim == 1 and values.flags.c_contiguous else \
+        np.array(values, dtype=np.int64).reshape(-1)
+    if a.dtype != np.int32:
+        if a.size and (a.min() < -2 ** 31 or a.max() >= 2 ** 31):
+            raise ValueError(f"{what} outside 32 bits")
+        a = a.astype(np.int32)
+    return a, a.ctypes.data_as(ctypes.POINTER(ctypes.c_int32))
+
+
+class RowRanges:
+    """Ranges (first, count) of rows that each of several sequences keeps."""
+
+    def __init__(self, ranges):
+        self.n = len(ranges)
+        flat = [x for r in ranges for x in r]
+        self.counts, self.c_counts = _int32s([len(r) for r in ranges], "counts")
+        self.first, self.c_first = _int32s([a for a, _ in flat], "first rows")
+        self.count, self.c_count = _int32s([n for _, n in flat], "rows")
+
+
+class Pages:
+    """fsx_pages: caches of many sequences in one pool of pages.  k, v [layers][pages][kv_heads][page_rows][head_dim] bfloat16, or
+    fp8 codes (float8_e4m3fn or uint8) with float32 scales k_scale, v_scale [layers][pages][kv_heads][page_rows]; all dense."""
+
+    def __init__(self, k, v, max_seqs: int, max_seq_pages: int, k_scale=None, v_scale=None, stream=None):
+        if k.dim() != 5 or v.shape != k.shape or v.dtype != k.dtype or not k.is_contiguous() or not v.is_contiguous():
+            raise ValueError("k and v must be dense [layers][pages][kv_heads][page_rows][head_dim] tensors of one dtype")
+        dtype = FP8_E4M3 if k.element_size() == 1 else _dtype_of(k)
+        if dtype == FP8_E4M3:
+            import torch
+
+            if k.dtype not in (torch.float8_e4m3fn, torch.uint8):
+                raise ValueError("pages of one byte an element must be float8_e4m3fn, or uint8 that holds its codes")
+        if (k_scale is not None or v_scale is not None) != (dtype == FP8_E4M3):
+            raise ValueError("fp8 pages, and no others, have scales")
+        for t in (k_scale, v_scale):
+            if dtype == FP8_E4M3 and (t is None or t.shape != k.shape[:4] or _dtype_of(t) != F32 or not t.is_contiguous()):
+                raise ValueError("scales must be dense float32 [layers][pages][kv_heads][page_rows]")
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale  # the handle reads and writes them
+        self.cfg = PagesCfg(dtype, k.shape[0], k.shape[2], k.shape[4], k.shape[3], k.shape[1], max_seqs, max_seq_pages, _ptr(k), _ptr(v),
+                            _ptr(k_scale), _ptr(v_scale))
+        self.handle = 0
+        out = ctypes.c_void_p(0)
+        _check(lib().fsx_pages_create(ctypes.byref(self.cfg), _stream_on(stream, k, v, k_scale, v_scale), ctypes.byref(out)))
+        self.handle = out.value
+
+    def extend(self, seqs, rows, stream=None):
+        """Room for rows[i] more rows of sequence seqs[i]."""
+        (s, ps), (r, pr) = _int32s(seqs, "seqs"), _int32s(rows, "rows")
+        if len(s) != len(r):
+            raise ValueError("as many row counts as sequences")
+        _check(lib().fsx_pages_extend(self.handle, len(s), ps, pr, _stream_on(stream, self.k)))
+
+    def fork(self, src, dst, rows=None, stream=None):
+        """Sequence dst[i] gets the first rows[i] (None: all) rows of src[i], in shared pages."""
+        (a, pa), (b, pb) = _int32s(src, "src"), _int32s(dst, "dst")
+        r, pr = _int32s(rows, "rows") if rows is not None else (a, None)
+        if not len(a) == len(b) == len(r):
+            raise ValueError("src, dst and rows must be of one length")
+        _check(lib().fsx_pages_fork(self.handle, len(a), pa, pb, pr, _stream_on(stream, self.k)))
+
+    def keep(self, seqs, ranges, stream=None):
+        """Sequence seqs[i] keeps its rows in ranges[i], a list of (first, count), ascending; ranges may be a RowRanges."""
+        s, ps = _int32s(seqs, "seqs")
+        r = ranges if isinstance(ranges, RowRanges) else RowRanges(ranges)
+        if r.n != len(s):
+            raise ValueError("ranges of every sequence")
+        _check(lib().fsx_pages_keep(self.handle, len(s), ps, r.c_counts, r.c_first, r.c_count, _stream_on(stream, self.k)))
+
+    def free(self, seqs, stream=None):
+        """The sequences have no rows any more."""
+        s, ps = _int32s(seqs, "seqs")
+        _check(lib().fsx_pages_free(self.handle, len(s), ps, _stream_on(stream, self.k)))
+
+    def tables(self):
+        """The lists of pages [max_seqs][max_seq_pages] (-1: none) and the lengths [max_seqs], as int32 arrays."""
+        table, length = np.empty((self.cfg.max_seqs, self.cfg.max_seq_pages), np.int32), np.empty(self.cfg.max_seqs, np.int32)
+        P = ctypes.POINTER(ctypes.c_int32)
+        _check(lib().fsx_pages_tables(self.handle, length.ctypes.data_as(P), table.ctypes.data_as(P), None))
+        return table, length
+
+    def free_pages(self) -> int:
+        n = ctypes.c_int64()
+        _check(lib().fsx_pages_tables(self.handle, None, None, ctypes.byref(n)))
+        return n.value
+
+    def write(self, layer: int, n_layers: int, k_rows, v_rows, seqs, rows: PackedRows, stream=None):
+        """Packed rows [n_layers][rows][kv_heads][head_dim] (bfloat16 or float32; any layer, row and head strides) become the last
+        rows.len[i] rows of sequence seqs[i]."""
+        s, ps = _int32s(seqs, "seqs")
+        if rows.n != len(s):
+            raise ValueError("packed rows of every sequence")
+        shape, tk, tv = k_rows.shape, k_rows.stride(), v_rows.stride()
+        if len(shape) != 4 or v_rows.shape != shape or v_rows.dtype != k_rows.dtype or shape[0] != n_layers or \
+                shape[2] != self.cfg.n_kv_heads or shape[3] != self.cfg.head_dim or tk[3] != 1 or tv[3] != 1:
+            raise ValueError("packed rows must be [n_layers][rows][kv_heads][head_dim] of one dtype, with a dense last dimension")
+        d = PagesRows(_dtype_of(k_rows), layer, n_layers, shape[1], tk[0], tk[1], tk[2], tv[0], tv[1], tv[2])
+        _check(lib().fsx_pages_write(self.handle, ctypes.byref(d), _ptr(k_rows), _ptr(v_rows), len(s), ps, rows.c_start, rows.c_len,
+                                     _stream_on(stream, k_rows, v_rows, self.k)))
+
+    def _attention_desc(self, q, out, scale: float) -> PromptDesc:
+        sq, tq, to = q.shape, q.stride(), out.stride()
+        if len(sq) != 3 or out.shape != sq or sq[2] != self.cfg.head_dim or tq[2] != 1 or to[2] != 1:
+            raise ValueError("q and out must be [sequences][heads][head_dim], with a dense last dimension")
+        return PromptDesc(sq[1], self.cfg.n_kv_heads, sq[2], _dtype_of(q), _dtype_of(out), scale, 0, sq[0], 0, tq[0], tq[1], 0, 0, 0, 0,
+                          to[0], to[1])
+
+    def attention(self, layer: int, q, out, seqs, scale: float = 0.0, lse=None, workspace=None, stream=None):
+        """fsx_pages_attention: row i of q [sequences][heads][head_dim] over all rows of sequence seqs[i]; lse
+        [sequences][heads] float32, dense, or None; workspace a dense device tensor of attention_workspace bytes, or None."""
+        s, ps = _int32s(seqs, "seqs")
+        if q.shape[0] != len(s):
+            raise ValueError("a row of q for every sequence")
+        if lse is not None and (_dtype_of(lse) != F32 or tuple(lse.shape) != tuple(q.shape[:2]) or not lse.is_contiguous()):
+            raise ValueError("lse must be a dense float32 [sequences][heads]")
+        if workspace is not None and not workspace.is_contiguous():
+            raise ValueError("workspace must be a dense tensor")
+        d = self._attention_desc(q, out, scale)
+        _check(lib().fsx_pages_attention(self.handle, ctypes.byref(d), layer, _ptr(q), _ptr(out), _ptr(lse), len(s), ps, _ptr(workspace),
+                                         workspace.numel() * workspace.element_size() if workspace is not None else 0,
+                                         _stream_on(stream, q, out, lse, workspace, self.k)))
+
+    def attention_workspace(self, q, seqs) -> int:
+        """fsx_pages_attention_workspace: bytes of the workspace that the call can use with the lengths of now (0: none)."""
+        s, ps = _int32s(seqs, "seqs")
+        d, need = self._attention_desc(q, q, 0.0), ctypes.c_int64()
+        _check(lib().fsx_pages_attention_workspace(self.handle, ctypes.byref(d), len(s), ps, ctypes.byref(need)))
+        return need.value
+
+    def close(self):
+        if self.handle:
+            lib().fsx_pages_destroy(ctypes.c_void_p(self.handle))
+            self.handle = 0
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
 
 
 class Loop:

@@ -1,0 +1,341 @@
+"""Attention of one new token over pages (fsx_pages_attention) against the formula in 64 bits (gpu_pages.attend derives the
+tolerances), and a decoder's step made of the operators together."""
+
+from __future__ import annotations
+
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from gpu_pages import BF16, F32, F64, U, Pool, attend, check_attention, near
+from paper_2607_15621_amd import fsx
+
+pytestmark = pytest.mark.gpu
+kinds = pytest.mark.parametrize("fp8,D", [(False, 128), (False, 64), (True, 128), (True, 64)], ids=["bf16-128", "bf16-64", "fp8-128", "fp8-64"])
+
+
+def run(p, layer, q, seqs, out_dtype=BF16, workspace=True, scale=0.0, stream=None):
+    out = torch.full(q.shape, 7.0, dtype=out_dtype, device="cuda")
+    lse = torch.full(q.shape[:2], 7.0, device="cuda")
+    need = p.pages.attention_workspace(q, seqs)
+    ws = torch.full((need,), 255, dtype=torch.uint8, device="cuda") if workspace and need else None
+    p.pages.attention(layer, q, out, seqs, scale, lse, ws, stream)
+    return out, lse
+
+
+def queries(p, n, heads, dtype=BF16, amp=1.0):
+    return (torch.randn(n, heads, p.D, generator=p.g) * amp).to(dtype).cuda()
+
+
+@kinds
+@pytest.mark.parametrize("P", [16, 32, 256])
+def test_lengths(fp8, D, P):
+    """None, one, around tiles, steps of a workgroup and pages, several parts; layers apart; entries out of order, one twice."""
+    lens = [0, 1, 2, 15, 16, 17, 31, 32, 33, 127, 128, 129, 257, 700, 1025]
+    p = Pool(seqs=len(lens), pages=sum(-(-n // P) for n in lens) + 2, most=-(-1025 // P), P=P, D=D, fp8=fp8, L=2, H=2)
+    p.extend(list(range(len(lens))), lens)
+    seqs = [14, 0, 3, 13, 1, 2, 12, 4, 5, 11, 10, 9, 3, 8, 7, 6]
+    q = queries(p, len(seqs), 8)
+    for layer in (0, 1):
+        out, lse = run(p, layer, q, seqs)
+        check_attention(p, layer, q, out, lse, seqs)
+    assert bool((out[1] == 0).all()) and bool((lse[1] == -math.inf).all())
+    out, lse = run(p, 1, q, seqs, F32, workspace=False)
+    check_attention(p, 1, q, out, lse, seqs)
+
+
+@kinds
+@pytest.mark.parametrize("G", [1, 2, 3, 5, 7, 8, 15, 16, 17, 20, 33])
+def test_groups(fp8, D, G):
+    """Query heads per key head: a tile of 16 not full, full, and more than one."""
+    p = Pool(seqs=3, pages=100, most=60, P=16, D=D, fp8=fp8, L=1, H=2)
+    p.extend([0, 1, 2], [5, 900, 130])
+    q = queries(p, 3, 2 * G)
+    out, lse = run(p, 0, q, [1, 0, 2])
+    check_attention(p, 0, q, out, lse, [1, 0, 2])
+
+
+@pytest.mark.parametrize("fp8", [False, True], ids=["bf16", "fp8"])
+def test_types_strides_and_scale(fp8):
+    p = Pool(seqs=4, pages=80, most=60, P=32, fp8=fp8, L=1, H=2)
+    p.extend([0, 1, 2], [300, 64, 1111])
+    for dtype in (BF16, F32):
+        wide = torch.randn(5, 6, 40, 128, generator=p.g).to(dtype).cuda()
+        q = wide[1:4, 2, 8:16]
+        for out_dtype in (BF16, F32):
+            big = torch.full((8, 3, 160), 7.0, dtype=out_dtype, device="cuda").transpose(0, 1)  # heads before rows, wider than a head
+            out, lse = big[:, :, 8:136], torch.empty(3, 8, device="cuda")
+            ws = torch.empty(p.pages.attention_workspace(q, [2, 0, 1]), dtype=torch.uint8, device="cuda")
+            p.pages.attention(0, q, out, [2, 0, 1], 0.31, lse, ws)
+            check_attention(p, 0, q, out, lse, [2, 0, 1], 0.31)
+            assert bool((big[:, :, :8] == 7).all()) and bool((big[:, :, 136:] == 7).all())
+
+
+@pytest.mark.parametrize("fp8", [False, True], ids=["bf16", "fp8"])
+@pytest.mark.parametrize("amp", [0.0, 0.05, 20.0, 300.0])
+def test_scores_of_every_size(fp8, amp):
+    """Flat weights, and weights that one row takes; the maximum late and early."""
+    p = Pool(seqs=2, pages=100, most=60, P=16, fp8=fp8, L=1, H=2)
+    p.extend([0], [777])
+    q = queries(p, 1, 4, amp=amp)
+    check_attention(p, 0, q, *run(p, 0, q, [0]), [0])
+    p.extend([1], [600])
+    for i in range(600):  # keys grow along the sequence
+        p.rows[1][i] = (p.rows[1][i][0], *p.rows[1][i][1:]) if fp8 else ((p.rows[1][i][0].to(F32) * (i / 200)).to(BF16), p.rows[1][i][1])
+    if not fp8:
+        table, _ = p.pages.tables()
+        for i in range(600):
+            p.k[:, table[1, i // 16], :, i % 16] = p.rows[1][i][0].cuda()
+    q = queries(p, 1, 4, amp=amp)
+    check_attention(p, 0, q, *run(p, 0, q, [1]), [1])
+
+
+def test_rows_behind_the_end_may_hold_anything():
+    """The pool is full of NaN, and then of infinities, but for the sequences' rows (every length in a page)."""
+    for fill in (math.nan, math.inf, -math.inf):
+        p = Pool(seqs=40, pages=120, most=3, P=16, L=1, H=1)
+        p.k.fill_(fill)
+        p.v.fill_(fill)
+        p.extend(list(range(40)), list(range(1, 41)))
+        q = queries(p, 40, 3)
+        out, lse = run(p, 0, q, list(range(40)))
+        assert bool(torch.isfinite(out).all()) and bool(torch.isfinite(lse).all())
+        check_attention(p, 0, q, out, lse, list(range(40)))
+
+
+def test_infinities_and_nan_that_are_seen():
+    """As the formula has it: a key of +infinity makes NaN, one of -infinity no weight, values that are not finite reach their channel."""
+    p = Pool(seqs=4, pages=20, most=8, P=16, L=1, H=1)
+    p.extend([0, 1, 2, 3], [50, 50, 50, 50])
+    q = torch.ones(4, 2, 128, dtype=BF16, device="cuda")
+    table, _ = p.pages.tables()
+
+    def put(t, s, i, c, x):
+        t[0, table[s, i // 16], 0, i % 16, c] = x
+    put(p.k, 0, 20, 3, math.inf)
+    put(p.k, 1, 20, 3, -math.inf)
+    put(p.v, 2, 49, 5, math.inf)
+    put(p.v, 3, 0, 7, math.nan)
+    out, lse = (t.cpu() for t in run(p, 0, q, [0, 1, 2, 3]))
+    assert bool(out[0].isnan().all())
+    k, v = p.decoded(1, 0)
+    k = k.clone()
+    k[20] = -1e30  # no weight
+    o, tol, z, ztol = attend(q[1].cpu(), torch.cat([k[:20], k[21:]]), torch.cat([v[:20], v[21:]]), 128 ** -0.5)
+    near(out[1].to(F64), o, tol + U * (o.abs() + tol), "without the row")
+    near(lse[1].to(F64), z, ztol, "without the row")
+    assert (out[2] == math.inf).nonzero().tolist() == [[0, 5], [1, 5]] and not bool(out[2].isnan().any())
+    assert out[3].isnan().nonzero().tolist() == [[0, 7], [1, 7]]
+
+
+def test_many_entries_and_less_workspace():
+    """More entries than a launch takes, long and short ones mixed; with less workspace the parts are fewer."""
+    p = Pool(seqs=5, pages=300, most=200, P=16, L=1, H=1)
+    p.extend([0, 1, 2, 3], [3000, 7, 260, 900])
+    seqs = [(i * 7) % 5 for i in range(600)]
+    q = queries(p, 600, 2)
+    out, lse = run(p, 0, q, seqs)
+    check_attention(p, 0, q[:10], out[:10], lse[:10], seqs[:10])
+    k = {s: p.decoded(s, 0) for s in range(5)}
+    for i in range(250, 600, 7):
+        o, tol, z, ztol = attend(q[i].cpu(), *k[seqs[i]], 128 ** -0.5)
+        near(out[i].cpu().to(F64), o, tol + U * (o.abs() + tol), i)
+        near(lse[i].cpu().to(F64), z, ztol, i)
+    need = p.pages.attention_workspace(q[:8], seqs[:8])
+    assert need > 0
+    for part in (need, need - 16, need // 2 // 16 * 16, need // 5 // 16 * 16, 16):
+        ws = torch.full((part + 64,), 255, dtype=torch.uint8, device="cuda")
+        out = torch.empty_like(q[:8])
+        p.pages.attention(0, q[:8], out, seqs[:8], workspace=ws[:part])
+        check_attention(p, 0, q[:8], out, None, seqs[:8])
+        assert bool((ws[part:] == 255).all())
+
+
+def test_the_same_bits_again_and_in_graphs():
+    """Two graphs with a workspace each, replayed in turn while the sequences grow, against eager calls."""
+    p = Pool(seqs=6, pages=200, most=80, P=16, L=2, H=2)
+    p.extend([0, 1, 2, 3], [1000, 40, 555, 0])
+    side = torch.cuda.Stream()
+    runs = []
+    for seqs in ([0, 1, 2, 3, 0], [2, 3]):
+        q = queries(p, len(seqs), 8)
+        out, lse = torch.zeros_like(q), torch.zeros(q.shape[:2], device="cuda")
+        ws = torch.empty(p.pages.attention_workspace(q, seqs), dtype=torch.uint8, device="cuda")
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            p.pages.attention(1, q, out, seqs, lse=lse, workspace=ws)
+        runs.append((seqs, q, out, lse, ws, graph))
+    for step in range(4):
+        for seqs, q, out, lse, ws, graph in runs:
+            q.copy_(queries(p, len(seqs), 8))
+            out.fill_(9)
+            graph.replay()
+            torch.cuda.synchronize()
+            check_attention(p, 1, q, out, lse, seqs)
+            first = out.clone()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(first, out)
+            a, b = run(p, 1, q, seqs), run(p, 1, q, seqs)
+            assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+            if step == 0:
+                assert torch.equal(a[0], out) and torch.equal(a[1], lse)
+        if step == 1:
+            p.free([0])          # a replay finds a sequence without rows
+        elif step == 2:
+            p.extend([0], [1200])
+        else:
+            p.extend([0, 1, 3], [17, 100, 1])
+
+
+def test_two_streams_at_once():
+    p = Pool(seqs=2, pages=200, most=100, P=16, L=1, H=2)
+    p.extend([0, 1], [1500, 1400])
+    q = [queries(p, 2, 8) for _ in "ab"]
+    want = [run(p, 0, x, [0, 1])[0] for x in q]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in q]
+    got = []
+    for _ in range(10):
+        got = []
+        for x, s in zip(q, streams):
+            with torch.cuda.stream(s):
+                got.append(run(p, 0, x, [0, 1])[0])
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_a_long_history():
+    """One token over 100,003 rows, the last pages of a pool of more than 2^32 elements."""
+    n, H, P, D = 70000, 8, 64, 128
+    k, v = (torch.empty(1, n, H, P, D, dtype=BF16, device="cuda") for _ in "kv")
+    rows = 100003
+    m = -(-rows // P)
+    pages = fsx.Pages(k, v, 2, n)
+    pages.extend([0, 1], [(n - m) * P, rows])
+    assert pages.tables()[0][1, m - 1] == n - 1
+    k[0, n - m:].normal_()
+    v[0, n - m:].normal_()
+    q = torch.randn(1, 16, D, device="cuda").to(BF16)
+    out, lse = torch.empty_like(q), torch.empty(1, 16, device="cuda")
+    ws = torch.empty(pages.attention_workspace(q, [1]), dtype=torch.uint8, device="cuda")
+    pages.attention(0, q, out, [1], lse=lse, workspace=ws)
+    host = [t[0, n - m:].transpose(1, 2).reshape(m * P, H, D)[:rows].to(F64).cpu() for t in (k, v)]
+    o, tol, z, ztol = attend(q[0].cpu(), *host, D ** -0.5)
+    near(out[0].cpu().to(F64), o, tol + U * (o.abs() + tol), "output")
+    near(lse[0].cpu().to(F64), z, ztol, "log sums")
+
+
+def test_refusals():
+    p = Pool(seqs=3, pages=20, most=6, L=1)
+    p.extend([0], [40])
+    q = queries(p, 2, 4)
+    out = torch.empty_like(q)
+    bad = torch.empty(2, 4, 132, dtype=BF16, device="cuda")[..., :128]
+    for call, word in ((lambda: p.pages.attention(1, q, out, [0, 1]), "layer"), (lambda: p.pages.attention(-1, q, out, [0, 1]), "layer"),
+                       (lambda: p.pages.attention(0, q, out, [0, 3]), "max_seqs"), (lambda: p.pages.attention(0, q, out, [0, -1]), "max_seqs"),
+                       (lambda: p.pages.attention(0, q, out, [0, 1], scale=-1.0), "scale"),
+                       (lambda: p.pages.attention(0, q, out, [0, 1], scale=math.nan), "scale"),
+                       (lambda: p.pages.attention(0, q[:, :3], out[:, :3], [0, 1]), "multiple"),
+                       (lambda: p.pages.attention(0, q[:0], out[:0], []), "n must"),
+                       (lambda: p.pages.attention(0, q, bad, [0, 1]), "multiples of 8"), (lambda: p.pages.attention(0, bad, out, [0, 1]), "multiples of 8"),
+                       (lambda: p.pages.attention(0, q, out[:, :1].expand(2, 4, 128), [0, 1]), "overlap"),
+                       (lambda: p.pages.attention(0, q, out, [0, 1], workspace=torch.empty(99, dtype=torch.uint8, device="cuda")[1:]), "workspace")):
+        with pytest.raises(fsx.FsxError, match=word):
+            call()
+    for call in (lambda: p.pages.attention(0, q, out, [0]), lambda: p.pages.attention(0, q, out[:1], [0, 1]),
+                 lambda: p.pages.attention(0, q.cpu(), out, [0, 1]), lambda: p.pages.attention(0, q.half(), out.half(), [0, 1]),
+                 lambda: p.pages.attention(0, q, out, [0, 1], lse=torch.empty(2, 5, device="cuda")),
+                 lambda: p.pages.attention(0, q, out, [0, 1], workspace=torch.empty(8, 8, dtype=torch.uint8, device="cuda").t()[:4])):
+        with pytest.raises(ValueError):
+            call()
+
+
+@pytest.mark.parametrize("fp8", [False, True], ids=["bf16", "fp8"])
+def test_a_decoder_step(fp8):
+    """The operators together: prompts of text and frames rotated by time, height and width, attended to and cached; one of them
+    forked; every sequence decoded a few tokens by captured steps; a frame dropped; decoded again.  Against the formulas in 64 bits
+    over the rows that should be cached."""
+    H, Hk, D, L = 8, 2, 128, 2
+    p = Pool(seqs=5, pages=120, most=20, P=16, D=D, H=Hk, L=L, fp8=fp8)
+    plan = fsx.RotaryPlan.sections((16, 24, 24))
+    lens = [150, 77]
+    rows = fsx.PackedRows(lens)
+    n = sum(lens)
+    pos = torch.stack([torch.arange(n) // 24, torch.arange(n) // 6 % 4, torch.arange(n) % 6]).to(torch.int32)
+    g = torch.Generator().manual_seed(11)
+
+    def turned(x, positions):
+        angle = positions.to(F64)[torch.from_numpy(plan.axis).long()].t() * torch.from_numpy(plan.freq)
+        c, s = angle.cos()[:, None], angle.sin()[:, None]
+        a, b = x[..., :64].to(F64), x[..., 64:].to(F64)
+        return torch.cat([a * c - b * s, b * c + a * s], 2)
+
+    # prompts, layer by layer
+    p.pages.extend([0, 1], lens)
+    stored = [[], []]
+    for layer in range(L):
+        x = torch.randn(n, H + 2 * Hk, D, generator=g).to(BF16).cuda()
+        host = x.cpu()
+        qk = x[:, :H + Hk]
+        fsx.rotary_rows(qk, qk, pos.cuda(), plan)
+        want = turned(host[:, :H + Hk], pos)
+        # (a product and sum in fp32, rounded once: half a step of the value, and 8 2^-24 of the pair)
+        pair = host[:, :H + Hk].to(F64).abs()
+        pair = pair[..., :64] + pair[..., 64:]
+        near(qk.cpu().to(F64), want, U * want.abs() + 16 * 2.0 ** -24 * torch.cat([pair, pair], 2), "rotation")
+        out = torch.empty(n, H, D, dtype=BF16, device="cuda")
+        fsx.prompt_attention(x[:, :H], x[:, H:H + Hk], x[:, H + Hk:], out, rows)
+        p.pages.write(layer, 1, x[None, :, H:H + Hk], x[None, :, H + Hk:], [0, 1], rows)
+        host = x.cpu()
+        a = 0
+        for s, m in enumerate(lens):  # the last token's own attention
+            o, tol, _, _ = attend(host[a + m - 1, :H], host[a:a + m, H:H + Hk].to(F64), host[a:a + m, H + Hk:].to(F64), D ** -0.5)
+            near(out[a + m - 1].cpu().to(F64), o, tol + U * (o.abs() + tol), "prompt")
+            a += m
+        stored[layer] = host
+    saved = Pool.stored(p, torch.stack([t[:, H:H + Hk] for t in stored]), torch.stack([t[:, H + Hk:] for t in stored]))
+    p.rows[0], p.rows[1] = saved[:lens[0]], saved[lens[0]:]
+    p.check()
+
+    seqs = [0, 1, 2, 3]
+    p.fork([0, 0], [2, 3])
+    x = torch.zeros(L, 4, H + 2 * Hk, D, dtype=BF16, device="cuda")
+    step_pos = torch.zeros(3, 4, dtype=torch.int32, device="cuda")
+    out = torch.zeros(L, 4, H, D, dtype=BF16, device="cuda")
+    one = fsx.PackedRows([1] * 4)
+    ws = torch.empty(p.pages.attention_workspace(out[0], seqs) + (1 << 16), dtype=torch.uint8, device="cuda")
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+
+    def step():
+        for layer in range(L):
+            qk = x[layer, :, :H + Hk]
+            fsx.rotary_rows(qk, qk, step_pos, plan)
+            p.pages.write(layer, 1, x[layer:layer + 1, :, H:H + Hk], x[layer:layer + 1, :, H + Hk:], seqs, one)
+            p.pages.attention(layer, x[layer, :, :H], out[layer], seqs, workspace=ws)
+
+    for t in range(6):
+        if t == 3:
+            p.keep([2, 0], [[(0, 24), (48, 105)], [(0, 24), (40, 113)]])  # a frame of one, part of one of the other
+        p.pages.extend(seqs, [1] * 4)
+        x.copy_(torch.randn(x.shape, generator=g))
+        step_pos.copy_(torch.tensor([[40 + t] * 4, [0, 1, 2, 3], [5, 4, 3, 2]]))
+        if t in (0, 3):  # (the graph's checks hold for the sequences as they are: captured again after a change of their lists)
+            torch.cuda.synchronize()
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=side):
+                step()
+        graph.replay()
+        torch.cuda.synchronize()
+        host = x.cpu()
+        new = Pool.stored(p, host[:, :, H:H + Hk], host[:, :, H + Hk:])
+        for s, row in zip(seqs, new):
+            p.rows[s].append(row)
+        p.check()
+        for layer in range(L):
+            check_attention(p, layer, host[layer, :, :H], out[layer], None, seqs, what=f"step {t} layer {layer}")
+    p.free(seqs)
+    assert p.pages.free_pages() == 120
