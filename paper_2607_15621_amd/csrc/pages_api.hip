@@ -161,10 +161,8 @@ extern "C" int fsx_rotary_rows(const fsx_rotary_desc* d, const void* x, void* y,
     a.f32 = d->dtype == FSX_F32; a.adjacent = d->layout == FSX_ROTARY_ADJACENT; a.inverse = d->inverse;
     a.copy_rest = x != y && 2 * d->n_pairs < d->head_dim;
     for (int j = 0; j < d->n_pairs; ++j) {
-      // the part of a turn, rounded to 2^-64 (a long double holds that many bits)
-      const long double t = (long double)d->freq[j] / 6.283185307179586476925286766559L, f = t - floorl(t);
-      const long double u = roundl(f * 0x1p64L);
-      a.turn[j] = u >= 0x1p64L ? 0 : (uint64_t)u;
+      // turns per step in units of 2^-64, modulo a turn (a long double holds 64 bits; the product is below 2^82)
+      a.turn[j] = (uint64_t)(__int128)(d->freq[j] * (0x1p64L / 6.283185307179586476925286766559L));
       a.axis[j] = (uint8_t)d->axis[j];
     }
     const hipError_t e = launch_rotary(a, (hipStream_t)stream);
