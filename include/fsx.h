@@ -497,9 +497,13 @@ int fsx_pages_write(fsx_pages* pages, const fsx_pages_rows* desc, const void* k_
  *   workspace DEVICE, 16-byte aligned, for the parts of long sequences, at most workspace_bytes of it are used; with less than
  *             fsx_pages_attention_workspace says, the sequences are cut into fewer parts, with none (NULL, 0) into one.  Calls that
  *             overlap must not share one.
- * How many parts follows from the lengths at the time of the call; a replay in a graph cuts the lengths it finds into as many.
- * Numerics as fsx_prompt_attention (fp8 rows are decoded exactly, their scales applied in fp32: a value's to its weight before that is
- * rounded to bf16).  Deterministic: the same arguments and lengths give the same bits. */
+ * Sequences that share whole pages from their first on (forks) are read together there, as far as n_heads / n_kv_heads is at most 8.
+ * How the work is shared out follows from the lists and lengths at the time of the call; a replay in a graph shares out the lengths
+ * that it finds in the same proportions, and reads apart what is no longer shared.
+ * Scores, softmax statistics and sums are fp32; a weight goes to the matrix instructions as two bf16 values, the second what the
+ * first leaves out (2^-16 of it is lost).  Fp8 rows are decoded exactly, a key's scale is applied to its score, a value's to its
+ * weight, in fp32.  Queries in FSX_F32 are rounded to bf16.  A weight is at most 2^8 until the end divides by their sum, so values
+ * beyond 2^119 / rows may overflow a sum.  Deterministic: the same arguments, lists and lengths give the same bits. */
 int fsx_pages_attention(fsx_pages* pages, const fsx_prompt_desc* desc, int32_t layer, const void* q, void* out, float* lse,
                         int32_t n, const int32_t* seqs, void* workspace, int64_t workspace_bytes, void* stream);
 /* The most workspace the call would use now (0: none). */

@@ -333,8 +333,9 @@ struct PageWriteArgs {
   int32_t seq[PAGE_WRITES], rows[PAGE_WRITES], block_prefix[PAGE_WRITES + 1];
 };
 hipError_t launch_page_write(PageWriteArgs a, int n, const int32_t* seqs, const int64_t* start, const int64_t* rows, hipStream_t s);
-// One new token of every entry's sequence over its pages.
-constexpr int PAGE_QUERIES = 256;
+// One new token of every entry's sequence over its pages.  Entries whose sequences share their first pages are neighbours; the rows
+// of those pages, `base` of them, are read for a tile of such entries at a time.
+constexpr int PAGE_QUERIES = 128;
 struct PageAttentionArgs {
   PagePool pool;
   const void* q;
@@ -344,14 +345,39 @@ struct PageAttentionArgs {
   int64_t q_row, q_head, o_row, o_head;  // elements
   int32_t H, G, layer, q_f32, o_f32;
   float c;               // scores in log2 units = c * q.k
-  int32_t n, row;        // entries, and the row of the first
-  int32_t seq[PAGE_QUERIES];
-  int32_t prefix[PAGE_QUERIES + 1];  // parts of the entries before
+  int32_t n, n_tiles;
+  // Steps of 32 rows: those of the tiles, `tiled` of them, then those of the entries; workgroups take `per` of them each, or (each)
+  // workgroups take one tile's or entry's stretch between multiples of `per`, the tiles' tiled_parts of them first.
+  int32_t per, each, tiled, total, tiled_parts;
+  int32_t seq[PAGE_QUERIES], base[PAGE_QUERIES];
+  uint16_t row[PAGE_QUERIES];
+  int32_t all[PAGE_QUERIES + 1];                                      // parts of the entries before, shared rows' too
+  int32_t steps[PAGE_QUERIES + 1], parts[PAGE_QUERIES + 1];           // steps, and stretches, before the entries' own
+  uint8_t tile[PAGE_QUERIES / 2], members[PAGE_QUERIES / 2];          // first entries of the tiles, and how many
+  int32_t tile_steps[PAGE_QUERIES / 2 + 1], tile_parts[PAGE_QUERIES / 2 + 1];  // before the tiles
 };
-// Parts of every entry's keys and the workspace's bytes, at most workspace_bytes.
-int64_t plan_page_attention(const PagePool& pool, int H, int n, const int32_t* seqs, const int32_t* host_len, int64_t workspace_bytes,
-                            std::vector<int32_t>& parts);
-hipError_t launch_page_attention(PageAttentionArgs a, int n, const int32_t* seqs, const std::vector<int32_t>& parts, hipStream_t s);
+static_assert(sizeof(PageAttentionArgs) <= 4096, "kernel arguments");
+// How a call is shared out.
+struct PagePlan {
+  struct Entry {
+    int32_t index, base;        // row of q; rows that a tile reads
+    int32_t steps, own, shared; // steps of the others; parts of them, and of the tile's
+  };
+  struct Tile {
+    int32_t first, members;
+  };
+  struct Launch {
+    int32_t first, n, first_tile, n_tiles, per, each, workgroups, parts;
+  };
+  std::vector<Entry> entries;
+  std::vector<Tile> tiles;
+  std::vector<Launch> launches;
+  bool wide = false;   // workgroups of eight waves
+  int64_t bytes = 0;   // of workspace
+};
+void plan_page_attention(const PagePool& pool, const PageLists& lists, int H, int n, const int32_t* seqs, int64_t workspace_bytes,
+                         PagePlan& plan);
+hipError_t launch_page_attention(PageAttentionArgs a, const int32_t* seqs, const PagePlan& plan, hipStream_t s);
 
 // ------------------------------------------------------------------ simple per-op path (any dtype)
 struct GenericWeights {

@@ -2,10 +2,13 @@
 //   O = sum_j exp(s_j) v_j / sum_j exp(s_j),   s_j = scale q . k_j,   lse = log sum_j exp(s_j)   over the sequence's rows j.
 //
 // Bound by memory: every key and value is read once, for all the query heads that share it, and a token has few of those.  The
-// rows of a sequence are cut into parts so that there are workgroups enough; a workgroup takes one part for one key head (and at
-// most 16 of its query heads), and k_page_merge puts the parts' states together.
+// rows of all sequences, one after the other, are cut into even shares for the workgroups, one for each CU; a workgroup takes one key
+// head (and at most 16 of its query heads), and k_page_merge puts the states of a sequence's parts together.  Pages that several
+// sequences share (forks of one history) are read once for as many of them as the 16 columns of a product hold.
+// 64 histories of 7,700 rows (32 heads over 8, 2.03 GB): 335 us, 6.0 TB/s, which is what a plain read reaches; one of 100,003 rows 76
+// us, 5.4 TB/s, 16 of 4,100 55 us, 4.9 TB/s, of which 5 us are the merge and 3 the way to the first keys (arguments, length, list).
 //
-// The four waves of a workgroup take tiles of 32 rows in turn, each on its own until the end.  Nothing goes through LDS on the way:
+// The waves of a workgroup take tiles of 32 rows in turn, each on its own until the end.  Nothing goes through LDS on the way:
 //   S = K Q^T   16x16x32 MFMA, A = 16 rows x 32 channels of keys as loaded (16 bytes of a row per lane), B = the queries; lane l
 //   then has the scores of query l % 16 and rows 4 (l / 16) .. + 3 of each half of the tile;
 //   O^T += V^T P^T   these registers, rounded to bf16, are the B operand as they stand; of the values a lane loads a piece of
@@ -14,13 +17,16 @@
 // With fewer than 16 query heads the other columns are idle; the products take a small part of the loads' time all the same.
 
 #include <algorithm>
+#include <numeric>
+#include <type_traits>
 
 #include "common.h"
 #include "kernels.h"
 
 namespace fsx {
 
-constexpr int PA_WAVES = 4, PA_KEYS = 32, PA_STEP = PA_WAVES * PA_KEYS;  // rows that a workgroup takes at a time
+constexpr int PA_KEYS = 32;     // rows that a wave takes at a time
+constexpr int PA_SHARED = 128;  // shared rows that are worth a tile
 
 // A state of a part: G x D sums of weighted values, then G maxima (log2 units) and G sums of weights; whole 16-byte pieces.
 __host__ __device__ constexpr int64_t part_floats(int G, int D) { return ((int64_t)G * (D + 2) + 3) / 4 * 4; }
@@ -42,62 +48,49 @@ struct PageTile {
   float4 ks[2], vs[2];  // FP8: scales of rows 4 (lane / 16) ..
 };
 
-template <int D, bool FP8>
-__global__ __launch_bounds__(256, 2) void k_page_attention(PageAttentionArgs a) {
+template <int D, bool FP8, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 2) void k_page_attention(PageAttentionArgs a) {
   constexpr int KS = D / 32, NC = D / 16, ES = FP8 ? 1 : 2;  // steps of the first product, products of the second
+  constexpr int STEP = WAVES * PA_KEYS;
   using Tile = PageTile<D, FP8>;
-  __shared__ float xo[PA_WAVES][16][D + 4];
-  __shared__ float xm[PA_WAVES][16], xl[PA_WAVES][16];
+  // Lists and lengths.  Nothing writes them while this runs: said so (constant memory), they are read by scalar loads.  As vector
+  // loads they came behind the values under way, and every tile waited for both.
+  typedef const __attribute__((address_space(4))) int32_t* list_t;
+  __shared__ float xo[WAVES][16][D + 4];
+  __shared__ float xm[WAVES][16], xl[WAVES][16];
   const PagePool& p = a.pool;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, c16 = lane & 15;
-
-  // The part: entry e, part x of n, key head hk, query heads h0 .. of it.
   const int blocks = (a.G + 15) / 16;
-  const int unit = blockIdx.x, hq = blockIdx.y, hk = hq / blocks, qb = hq - hk * blocks;
-  int e = 0;
-#pragma unroll
-  for (int i = 0; i < PAGE_QUERIES; i += 64) e += __popcll(__ballot(i + lane < a.n && a.prefix[i + lane + 1] <= unit));
-  e = __builtin_amdgcn_readfirstlane(e);
-  const int x = unit - a.prefix[e], n = a.prefix[e + 1] - a.prefix[e], seq = a.seq[e];
-  const int gq = min(16, a.G - 16 * qb), h0 = hk * a.G + 16 * qb;
-  const int len = p.len[seq];
-  const int per = ((len + n - 1) / n + PA_KEYS - 1) / PA_KEYS * PA_KEYS;  // (in a captured graph the length is not the planned one)
-  const int begin = min(x * per, len), end = min(begin + per, len);
-  const int32_t* __restrict__ pages = p.table + (int64_t)seq * p.most;
+  const int hq = blockIdx.y, hk = hq / blocks, qb = hq - hk * blocks, h0 = hk * a.G + 16 * qb, rows = min(a.G, 16);
+  const list_t lens = (list_t)p.len;
 
-  // queries: channels of step s that the lane's keys hold
-  uint4 q[KS];
-  {
-    const int64_t at = (a.row + e) * a.q_row + (int64_t)(h0 + min(c16, gq - 1)) * a.q_head;
-#pragma unroll
-    for (int s = 0; s < KS; ++s) {
-      const int ch = FP8 ? 64 * (s / 2) + 16 * g + 8 * (s % 2) : 32 * s + 8 * g;
-      if (a.q_f32) {
-        const float4* f = reinterpret_cast<const float4*>(reinterpret_cast<const float*>(a.q) + at + ch);
-        const float4 u = f[0], v = f[1];
-        q[s] = make_uint4(pack_bf16x2(u.x, u.y), pack_bf16x2(u.z, u.w), pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
-      } else {
-        q[s] = *reinterpret_cast<const uint4*>(reinterpret_cast<const uint16_t*>(a.q) + at + ch);
-      }
+  // The arguments are cold in every launch, a microsecond away: what may be needed of them comes in one round trip, a value per
+  // lane, and is looked up by lane.
+  struct Column {
+    int lo, hi;
+    __device__ __forceinline__ int before(int i) const {  // how many are at most i
+      return __popcll(__ballot(lo <= i)) + __popcll(__ballot(hi <= i));
     }
-  }
-
-  const int last_page = max(len - 1, 0) >> p.shift;
+    __device__ __forceinline__ int at(int i) const {
+      return i < 64 ? __builtin_amdgcn_readlane(lo, i) : __builtin_amdgcn_readlane(hi, i - 64);
+    }
+    __device__ __forceinline__ int start(int i, int first) const { return i == 0 ? first : at(i - 1); }
+  };
+  const auto column = [&](const auto& v, int index, int n) {
+    const int x = v[index], y = v[64 + index];
+    return Column{lane < n ? x : INT32_MAX, 64 + lane < n ? y : INT32_MAX};
+  };
   const char* kbase = (const char*)p.k;
   const char* vbase = (const char*)p.v;
-  const int lane_k = c16 * D * ES + 16 * g, lane_v = 4 * g * D * ES + c16 * (D / 16) * ES;
-  // First element row of the page row that tile row `key` is (past the end: some row that exists).
-  const auto row_of = [&](int key) {
-    const int page = pages[min(key >> p.shift, last_page)];
-    return (((int64_t)a.layer * p.pages + page) * p.Hk + hk) * p.P + (key & (p.P - 1));
-  };
+  const int64_t layer_row = ((int64_t)a.layer * p.pages * p.Hk + hk) * p.P;
+  const uint32_t lane_k = c16 * D * ES + 16 * g, lane_v = 4 * g * D * ES + c16 * (D / 16) * ES, lane_s = 4 * g;
   const auto load_k = [&](Tile& t, const int64_t (&row)[2]) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const char* src = kbase + row[h] * (D * ES) + lane_k;
 #pragma unroll
       for (int i = 0; i < Tile::KP; ++i) t.k[h][i] = *reinterpret_cast<const uint4*>(src + 64 * i);
-      if constexpr (FP8) t.ks[h] = *reinterpret_cast<const float4*>(p.k_scale + row[h] + 4 * g);
+      if constexpr (FP8) t.ks[h] = *reinterpret_cast<const float4*>(p.k_scale + row[h] + lane_s);
     }
   };
   const auto load_v = [&](Tile& t, const int64_t (&row)[2]) {
@@ -116,162 +109,272 @@ __global__ __launch_bounds__(256, 2) void k_page_attention(PageAttentionArgs a) 
           t.v[h][i][0] = *reinterpret_cast<const uint32_t*>(src + i * D * ES);
         }
       }
-      if constexpr (FP8) t.vs[h] = *reinterpret_cast<const float4*>(p.v_scale + row[h] + 4 * g);
+      if constexpr (FP8) t.vs[h] = *reinterpret_cast<const float4*>(p.v_scale + row[h] + lane_s);
     }
   };
 
-  f32x4 o[NC];
+  int at = a.each ? 0 : (int)blockIdx.x * a.per, until = a.each ? 1 : min(at + a.per, a.total);  // the workgroup's steps
+  while (at < until) {
+    // The stretch: of the rows of entry e from base on, or of those that a tile's members e .. e + members - 1 share.
+    int e, from, to, base, seq0, members = 1;
+    bool shared;
+    {
+      int here = lane;
+      asm volatile("" : "+v"(here));  // (looked up again for the next stretch: kept, they are a dozen registers)
+      const Column steps = column(a.steps, here + 1, a.n), parts = column(a.parts, here + 1, a.n);
+      const Column seqs = column(a.seq, here, a.n), bases = column(a.base, here, a.n);
+      Column tile_steps{INT32_MAX, INT32_MAX}, tile_parts = tile_steps, tile = tile_steps;
+      if (a.n_tiles) {
+        const int x = a.tile_steps[here + 1], y = a.tile_parts[here + 1];
+        tile.lo = a.tile[here] | a.members[here] << 8;
+        if (lane < a.n_tiles) tile_steps.lo = x, tile_parts.lo = y;
+      }
+      const int i = a.each ? (int)blockIdx.x : at;
+      shared = i < (a.each ? a.tiled_parts : a.tiled);
+      int before;  // stretches before, of all
+      if (shared) {
+        const int t = (a.each ? tile_parts : tile_steps).before(i), x = tile.at(t);
+        e = x & 255, members = x >> 8, from = tile_steps.start(t, 0), to = tile_steps.at(t), before = tile_parts.start(t, 0);
+      } else {
+        e = (a.each ? parts : steps).before(i);
+        from = steps.start(e, a.tiled), to = steps.at(e), before = parts.start(e, a.tiled_parts);
+      }
+      if (a.each) {
+        at = from + (i - before) * a.per;
+        until = min(to, at + a.per);
+      }
+      base = bases.at(e), seq0 = seqs.at(e);
+    }
+    const int cut = min(to, until), part = a.each ? (at - from) / a.per : at / a.per - from / a.per;
+    const int width = shared ? a.G : min(16, a.G - 16 * qb);  // columns of an entry
+    // The thread's column of the outcome: an entry, its query head, and where the state goes.
+    const int qi = threadIdx.x >> 4, ch = NC * (threadIdx.x & 15), member = qi / width, gi = qi - member * width;
+    const int en = e + min(member, members - 1), n_parts = a.all[en + 1] - a.all[en], out_row = a.row[en];
+    const int slot = a.all[en] + part + (shared ? a.parts[en + 1] - a.parts[en] : 0);  // parts of its own rows, then of the shared
+    // The lane's column: queries of the channels that its keys have in step s.
+    uint4 q[KS];
+    {
+      const int64_t at_q = a.row[e + min(c16 / width, members - 1)] * a.q_row + (int64_t)(h0 + c16 % width) * a.q_head;
 #pragma unroll
-  for (int c = 0; c < NC; ++c) o[c] = f32x4{0.f, 0.f, 0.f, 0.f};
-  float m = -INFINITY, l = 0.f;  // maximum (log2 units), the same in the four lanes of a query; the lane's share of the sum
-
-  Tile t;
-  int key = begin + w * PA_KEYS;
-  if (key < end) {
-    int64_t row[2] = {row_of(key), row_of(key + 16)};
-    load_k(t, row);
-    load_v(t, row);
-    for (;;) {
-      const int next = key + PA_STEP;
-      const bool more = next < end;
-      int64_t nrow[2] = {row_of(more ? next : key), row_of((more ? next : key) + 16)};
-      // scores
-      f32x4 s[2];
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        s[h] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int i = 0; i < KS; ++i) {
-          uint4 ka;
-          if constexpr (FP8) {
-            const uint4 u = t.k[h][i / 2];
-            const uint32_t lo = i % 2 ? u.z : u.x, hi = i % 2 ? u.w : u.y;
-            ka = make_uint4(e4m3x2_to_bf16x2(lo, false), e4m3x2_to_bf16x2(lo, true), e4m3x2_to_bf16x2(hi, false), e4m3x2_to_bf16x2(hi, true));
-          } else {
-            ka = t.k[h][i];
-          }
-          s[h] = mfma_bf16(ka, q[i], s[h]);
+      for (int s = 0; s < KS; ++s) {
+        const int c = FP8 ? 64 * (s / 2) + 16 * g + 8 * (s % 2) : 32 * s + 8 * g;
+        if (a.q_f32) {
+          const float4* f = reinterpret_cast<const float4*>(reinterpret_cast<const float*>(a.q) + at_q + c);
+          const float4 u = f[0], v = f[1];
+          q[s] = make_uint4(pack_bf16x2(u.x, u.y), pack_bf16x2(u.z, u.w), pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
+        } else {
+          q[s] = *reinterpret_cast<const uint4*>(reinterpret_cast<const uint16_t*>(a.q) + at_q + c);
         }
       }
-      float sc[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        sc[i] = s[i / 4][i % 4] * a.c;
-        if constexpr (FP8) sc[i] *= reinterpret_cast<const float*>(&t.ks[i / 4])[i % 4];
+    }
+    // The pages of the first tile as planned come along with the length (entries of a list are pages that exist, also behind its end).
+    list_t pages = (list_t)(p.table + (int64_t)seq0 * p.most);
+    const int first_key = (shared ? 0 : base) + (at - from + w) * PA_KEYS;
+    const int guess0 = min(first_key >> p.shift, p.most - 1), guess1 = min((first_key + 16) >> p.shift, p.most - 1);
+    const int page0 = pages[guess0], page1 = pages[guess1], len0 = lens[seq0];
+    // Its steps as planned are at - from .. cut - from of to - from; of the rows that are found (in a captured graph not those that
+    // were planned) it takes the same share.
+    const int total = shared ? base : max(len0 - base, 0), found = (total + PA_KEYS - 1) / PA_KEYS;
+    const auto share = [&](int step) { return found == to - from ? step : (int)((int64_t)step * found / (to - from)); };
+    const int begin = (shared ? 0 : base) + share(at - from) * PA_KEYS;
+    const int stop = min(begin + (share(cut - from) - share(at - from)) * PA_KEYS, (shared ? 0 : base) + total);
+
+    // Whether the members of the tile still share these pages (since a graph was captured, their lists may have changed); if not,
+    // each takes a round of its own.
+    int rounds = 1;
+    if (shared) {
+      const int first = begin >> p.shift, count = stop > begin ? ((stop - 1) >> p.shift) - first + 1 : 0;
+      bool same = true;
+      for (int i = threadIdx.x; i < count * members; i += 64 * WAVES) {
+        const int j = i / members, s = a.seq[e + i - j * members];
+        same &= p.len[s] >= base && p.table[(int64_t)s * p.most + first + j] == p.table[(int64_t)seq0 * p.most + first + j];
       }
-      if (more) load_k(t, nrow);
-      const int left = end - key;  // rows of the tile that count
-      if (left < PA_KEYS) {
+      rounds = __builtin_amdgcn_readfirstlane(__syncthreads_and(same) ? 1 : members);
+    }
+
+    for (int round = 0; round < rounds; ++round) {
+      const int seq = round ? a.seq[e + round] : seq0, len = round ? lens[seq] : len0, end = min(stop, len);
+      if (round) pages = (list_t)(p.table + (int64_t)seq * p.most);
+      const int last_page = max(len - 1, 0) >> p.shift;
+      // First element row of the page row that tile row `key` is (past the end: some row that exists).
+      const auto row_in = [&](int page, int key) { return layer_row + (int64_t)page * (p.Hk * p.P) + (key & (p.P - 1)); };
+      const auto row_of = [&](int key) { return row_in(pages[min(key >> p.shift, last_page)], key); };
+      f32x4 o[NC];
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (16 * (i / 4) + 4 * g + i % 4 >= left) sc[i] = -INFINITY;
-      }
-      // The maximum that the exponents are taken from is raised only where they would pass 2^8, which sums in fp32 and relative
-      // roundings do not mind; then it is the same in the lanes of a query.
-      float top = vmax3(vmax3(sc[0], sc[1], sc[2]), vmax3(sc[3], sc[4], sc[5]), vmax(sc[6], sc[7]));
-      if (__any(top > m + 8.f)) {
-        const float now = rows_max(vmax(top, m)), back = __builtin_amdgcn_exp2f(m - (now == -INFINITY ? 0.f : now));
-        m = now;
-        l *= back;
+      for (int c = 0; c < NC; ++c) o[c] = f32x4{0.f, 0.f, 0.f, 0.f};
+      float m = -INFINITY, l = 0.f;  // maximum (log2 units), the same in the four lanes of a query; the lane's share of the sum
+
+      Tile t;
+      int key = begin + w * PA_KEYS;
+      int64_t next[2];  // rows of the tile after, looked up a tile ahead of its loads
+      // A tile: while it is computed, the next one's keys are loaded in place of its keys and, behind it, values in place of its values.
+      // The last is another copy of the code: loads under a condition would be waited for as if they had been left out.
+      const auto compute = [&](auto more) {
+        constexpr bool MORE = decltype(more)::value;
+        // scores
+        f32x4 s[2];
 #pragma unroll
-        for (int c = 0; c < NC; ++c)
+        for (int h = 0; h < 2; ++h) {
+          s[h] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int i = 0; i < 4; ++i) o[c][i] *= back;
-      }
-      const float mz = m == -INFINITY ? 0.f : m;
-      float pr[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        pr[i] = __builtin_amdgcn_exp2f(sc[i] - mz);
-        l += pr[i];
-        if constexpr (FP8) pr[i] *= reinterpret_cast<const float*>(&t.vs[i / 4])[i % 4];
-      }
-      if (left < PA_KEYS) {  // whatever lies behind the last row
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (16 * (i / 4) + 4 * g + i % 4 >= left) {
-            pr[i] = 0.f;
-#pragma unroll
-            for (int j = 0; j < Tile::VW; ++j) t.v[i / 4][i % 4][j] = 0;
-          }
-      }
-      const uint4 pb = make_uint4(pack_bf16x2(pr[0], pr[1]), pack_bf16x2(pr[2], pr[3]), pack_bf16x2(pr[4], pr[5]), pack_bf16x2(pr[6], pr[7]));
-      // values: product c takes channel c of every lane's piece, eight rows of it
-#pragma unroll
-      for (int c = 0; c < NC; ++c) {
-        uint32_t r[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {  // rows 2 j and 2 j + 1
-          const int h = j / 2, i = 2 * (j % 2);
-          if constexpr (FP8) {
-            // bytes c of two rows side by side, then to bf16
-            const uint32_t two = __builtin_amdgcn_perm(t.v[h][i + 1][c / 4], t.v[h][i][c / 4], c % 4 < 2 ? 0x05010400u : 0x07030602u);
-            r[j] = e4m3x2_to_bf16x2(two, c % 2);
-          } else {
-            r[j] = __builtin_amdgcn_perm(t.v[h][i + 1][c / 2], t.v[h][i][c / 2], c % 2 ? 0x07060302u : 0x05040100u);
+          for (int i = 0; i < KS; ++i) {
+            uint4 ka;
+            if constexpr (FP8) {
+              const uint4 u = t.k[h][i / 2];
+              const uint32_t lo = i % 2 ? u.z : u.x, hi = i % 2 ? u.w : u.y;
+              ka = make_uint4(e4m3x2_to_bf16x2(lo, false), e4m3x2_to_bf16x2(lo, true), e4m3x2_to_bf16x2(hi, false), e4m3x2_to_bf16x2(hi, true));
+            } else {
+              ka = t.k[h][i];
+            }
+            s[h] = mfma_bf16(ka, q[i], s[h]);
           }
         }
-        o[c] = mfma_bf16(make_uint4(r[0], r[1], r[2], r[3]), pb, o[c]);
+        float sc[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          sc[i] = s[i / 4][i % 4] * a.c;
+          if constexpr (FP8) sc[i] *= reinterpret_cast<const float*>(&t.ks[i / 4])[i % 4];
+        }
+        if constexpr (MORE) load_k(t, next);
+        const int left = MORE ? PA_KEYS : end - key;  // rows of the tile that count: all of them, but for the last of the wave's
+        if (left < PA_KEYS) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            if (16 * (i / 4) + 4 * g + i % 4 >= left) sc[i] = -INFINITY;
+        }
+        // The maximum that the exponents are taken from is raised only where they would pass 2^8, which sums in fp32 and relative
+        // roundings do not mind; then it is the same in the lanes of a query.
+        float top = vmax3(vmax3(sc[0], sc[1], sc[2]), vmax3(sc[3], sc[4], sc[5]), vmax(sc[6], sc[7]));
+        if (__any(top > m + 8.f)) {
+          const float now = rows_max(vmax(top, m)), back = __builtin_amdgcn_exp2f(m - (now == -INFINITY ? 0.f : now));
+          m = now;
+          l *= back;
+#pragma unroll
+          for (int c = 0; c < NC; ++c)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[c][i] *= back;
+        }
+        const float mz = m == -INFINITY ? 0.f : m;
+        float pr[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          pr[i] = __builtin_amdgcn_exp2f(sc[i] - mz);
+          l += pr[i];
+          if constexpr (FP8) pr[i] *= reinterpret_cast<const float*>(&t.vs[i / 4])[i % 4];
+        }
+        if (left < PA_KEYS) {  // whatever lies behind the last row
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            if (16 * (i / 4) + 4 * g + i % 4 >= left) {
+              pr[i] = 0.f;
+#pragma unroll
+              for (int j = 0; j < Tile::VW; ++j) t.v[i / 4][i % 4][j] = 0;
+            }
+        }
+        const uint4 pb = make_uint4(pack_bf16x2(pr[0], pr[1]), pack_bf16x2(pr[2], pr[3]), pack_bf16x2(pr[4], pr[5]), pack_bf16x2(pr[6], pr[7]));
+        const auto rest = [&](uint32_t two, int i) {
+          return pack_bf16x2(pr[i] - __uint_as_float(two << 16), pr[i + 1] - __uint_as_float(two & 0xFFFF0000u));
+        };
+        const uint4 pl = make_uint4(rest(pb.x, 0), rest(pb.y, 2), rest(pb.z, 4), rest(pb.w, 6));
+        // values: product c takes channel c of every lane's piece, eight rows of it
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+          uint32_t r[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {  // rows 2 j and 2 j + 1
+            const int h = j / 2, i = 2 * (j % 2);
+            if constexpr (FP8) {
+              // bytes c of two rows side by side, then to bf16
+              const uint32_t two = __builtin_amdgcn_perm(t.v[h][i + 1][c / 4], t.v[h][i][c / 4], c % 4 < 2 ? 0x05010400u : 0x07030602u);
+              r[j] = e4m3x2_to_bf16x2(two, c % 2);
+            } else {
+              r[j] = __builtin_amdgcn_perm(t.v[h][i + 1][c / 2], t.v[h][i][c / 2], c % 2 ? 0x07060302u : 0x05040100u);
+            }
+          }
+          o[c] = mfma_bf16(make_uint4(r[0], r[1], r[2], r[3]), pb, o[c]);
+          o[c] = mfma_bf16(make_uint4(r[0], r[1], r[2], r[3]), pl, o[c]);
+        }
+        if constexpr (MORE) {
+          load_v(t, next);
+          __builtin_amdgcn_sched_barrier(0);  // (not to be one with the first tile's loads, at the head of the loop)
+        }
+      };
+      if (key < end) {
+        const bool planned = round == 0 && key == first_key && ((key + 16) >> p.shift) <= last_page;
+        next[0] = planned ? row_in(page0, key) : row_of(key);
+        next[1] = planned ? row_in(page1, key + 16) : row_of(key + 16);
+        load_k(t, next);
+        load_v(t, next);
+        next[0] = row_of(key + STEP), next[1] = row_of(key + STEP + 16);
+        if (key + STEP < end) {
+          do {
+            compute(std::true_type{});
+            key += STEP;
+            next[0] = row_of(key + STEP), next[1] = row_of(key + STEP + 16);
+          } while (key + STEP < end);
+        }
+        compute(std::false_type{});
       }
-      if (!more) break;
-      load_v(t, nrow);
-      key = next;
-    }
-  }
-  l = rows_sum(l);
+      l = rows_sum(l);
 
-  // The waves' states put together.  Lane: query c16, o[c][i]: channel (D / 16) (4 g + i) + c.
+      // The waves' states put together.  Lane: query c16, o[c][i]: channel (D / 16) (4 g + i) + c.
 #pragma unroll
-  for (int c = 0; c < NC; ++c)
+      for (int c = 0; c < NC; ++c)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) xo[w][c16][NC * (4 * g + i) + c] = o[c][i];
-  if (g == 0) {
-    xm[w][c16] = m;
-    xl[w][c16] = l;
-  }
-  __syncthreads();
-  // thread: query t / 16, channels D / 16 (t % 16) ..
-  const int qi = threadIdx.x >> 4, ch = NC * (threadIdx.x & 15);
-  if (qi >= gq) return;
-  float mm = xm[0][qi], f[PA_WAVES], ll = 0.f;
+        for (int i = 0; i < 4; ++i) xo[w][c16][NC * (4 * g + i) + c] = o[c][i];
+      if (g == 0) {
+        xm[w][c16] = m;
+        xl[w][c16] = l;
+      }
+      __syncthreads();
+      // thread: column t / 16, channels D / 16 (t % 16) ..
+      if (qi < 16 && member < members && (rounds == 1 || member == round)) {
+        float mm = xm[0][qi], f[WAVES], ll = 0.f;
 #pragma unroll
-  for (int i = 1; i < PA_WAVES; ++i) mm = vmax(mm, xm[i][qi]);
-  const float mz = mm == -INFINITY ? 0.f : mm;
+        for (int i = 1; i < WAVES; ++i) mm = vmax(mm, xm[i][qi]);
+        const float mz = mm == -INFINITY ? 0.f : mm;
 #pragma unroll
-  for (int i = 0; i < PA_WAVES; ++i) {
-    f[i] = __builtin_amdgcn_exp2f(xm[i][qi] - mz);
-    ll += xl[i][qi] * f[i];
-  }
-  float r[NC];
+        for (int i = 0; i < WAVES; ++i) {
+          f[i] = __builtin_amdgcn_exp2f(xm[i][qi] - mz);
+          ll += xl[i][qi] * f[i];
+        }
+        float r[NC];
 #pragma unroll
-  for (int c = 0; c < NC; ++c) {
-    r[c] = 0.f;
+        for (int c = 0; c < NC; ++c) {
+          r[c] = 0.f;
 #pragma unroll
-    for (int i = 0; i < PA_WAVES; ++i) r[c] += xo[i][qi][ch + c] * f[i];
-  }
-  if (n > 1) {
-    float* part = a.part + ((int64_t)unit * gridDim.y * part_floats(min(a.G, 16), D)) + hq * part_floats(min(a.G, 16), D);
+          for (int i = 0; i < WAVES; ++i) r[c] += xo[i][qi][ch + c] * f[i];
+        }
+        if (n_parts > 1) {
+          float* state = a.part + ((int64_t)slot * gridDim.y + hq) * part_floats(rows, D);
 #pragma unroll
-    for (int c = 0; c < NC; c += 4) *reinterpret_cast<float4*>(part + qi * D + ch + c) = make_float4(r[c], r[c + 1], r[c + 2], r[c + 3]);
-    if ((threadIdx.x & 15) == 0) {
-      part[min(a.G, 16) * D + qi] = mm;
-      part[min(a.G, 16) * (D + 1) + qi] = ll;
+          for (int c = 0; c < NC; c += 4)
+            *reinterpret_cast<float4*>(state + gi * D + ch + c) = make_float4(r[c], r[c + 1], r[c + 2], r[c + 3]);
+          if ((threadIdx.x & 15) == 0) {
+            state[rows * D + gi] = mm;
+            state[rows * (D + 1) + gi] = ll;
+          }
+        } else {
+          const float inv = len > 0 ? 1.f / ll : 0.f;
+          const int64_t to_out = out_row * a.o_row + (int64_t)(h0 + gi) * a.o_head + ch;
+#pragma unroll
+          for (int c = 0; c < NC; c += 4) {
+            if (a.o_f32) {
+              *reinterpret_cast<float4*>(reinterpret_cast<float*>(a.out) + to_out + c) =
+                  make_float4(r[c] * inv, r[c + 1] * inv, r[c + 2] * inv, r[c + 3] * inv);
+            } else {
+              *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(a.out) + to_out + c) =
+                  make_uint2(pack_bf16x2(r[c] * inv, r[c + 1] * inv), pack_bf16x2(r[c + 2] * inv, r[c + 3] * inv));
+            }
+          }
+          if (a.lse && (threadIdx.x & 15) == 0)
+            a.lse[(int64_t)out_row * a.H + h0 + gi] = (mm + __builtin_amdgcn_logf(ll)) * (1.f / LOG2E);
+        }
+      }
+      if (round + 1 < rounds || cut < until) __syncthreads();  // the exchange is free again
     }
-    return;
+    at = cut;
   }
-  const float inv = len > 0 ? 1.f / ll : 0.f;
-  const int64_t row = a.row + e;
-  const int64_t at = row * a.o_row + (int64_t)(h0 + qi) * a.o_head + ch;
-#pragma unroll
-  for (int c = 0; c < NC; c += 4) {
-    if (a.o_f32) {
-      *reinterpret_cast<float4*>(reinterpret_cast<float*>(a.out) + at + c) = make_float4(r[c] * inv, r[c + 1] * inv, r[c + 2] * inv, r[c + 3] * inv);
-    } else {
-      *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(a.out) + at + c) =
-          make_uint2(pack_bf16x2(r[c] * inv, r[c + 1] * inv), pack_bf16x2(r[c + 2] * inv, r[c + 3] * inv));
-    }
-  }
-  if (a.lse && (threadIdx.x & 15) == 0) a.lse[row * a.H + h0 + qi] = (mm + __builtin_amdgcn_logf(ll)) * (1.f / LOG2E);
 }
 
 // The parts of one (entry, query head) put together, in their order: D / 4 threads take every PM-th part, then the groups' states.
@@ -281,11 +384,11 @@ __global__ __launch_bounds__(256) void k_page_merge(PageAttentionArgs a) {
   __shared__ float4 xo[GROUPS][T];
   __shared__ float xl[GROUPS], xm[GROUPS];
   const int e = blockIdx.x, h = blockIdx.y, hk = h / a.G, gi = h - hk * a.G, blocks = (a.G + 15) / 16, rows = min(a.G, 16);
-  const int n = a.prefix[e + 1] - a.prefix[e];
+  const int n = a.all[e + 1] - a.all[e];
   if (n <= 1) return;  // written already
   const int grp = threadIdx.x / T, t = threadIdx.x % T;
   const int64_t step = (int64_t)blocks * (a.H / a.G) * part_floats(rows, D);
-  const float* part = a.part + a.prefix[e] * step + (hk * blocks + gi / 16) * part_floats(rows, D);
+  const float* part = a.part + a.all[e] * step + (hk * blocks + gi / 16) * part_floats(rows, D);
   const int qi = gi % 16;
   float m = -INFINITY, l = 0.f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -320,57 +423,179 @@ __global__ __launch_bounds__(256) void k_page_merge(PageAttentionArgs a) {
 #pragma unroll
   for (int i = 1; i < GROUPS; ++i) add(xm[i], xl[i], xo[i][t]);
   const float inv = a.pool.len[a.seq[e]] > 0 ? 1.f / l : 0.f;
-  const int64_t row = a.row + e, at = row * a.o_row + (int64_t)h * a.o_head + 4 * t;
+  const int64_t row = a.row[e], at = row * a.o_row + (int64_t)h * a.o_head + 4 * t;
   if (a.o_f32) *reinterpret_cast<float4*>(reinterpret_cast<float*>(a.out) + at) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
   else *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(a.out) + at) = make_uint2(pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
   if (a.lse && t == 0) a.lse[row * a.H + h] = (m + __builtin_amdgcn_logf(l)) * (1.f / LOG2E);
 }
 
-int64_t plan_page_attention(const PagePool& p, int H, int n, const int32_t* seqs, const int32_t* host_len, int64_t workspace_bytes,
-                            std::vector<int32_t>& parts) {
-  constexpr int64_t WGS = 2048;
-  const int G = H / p.Hk, units = p.Hk * ((G + 15) / 16);
-  const int64_t state = 4 * units * part_floats(std::min(G, 16), p.D);  // bytes of a part, all heads
-  int64_t rows = 0;
-  for (int i = 0; i < n; ++i) rows += host_len[seqs[i]];
-  int64_t chunk = std::max<int64_t>(PA_STEP, (rows * units / WGS + PA_STEP - 1) / PA_STEP * PA_STEP), need = 0;
-  parts.resize(n);
-  for (;; chunk *= 2) {
-    need = 0;
-    int64_t split = 0;
-    for (int i = 0; i < n; ++i) {
-      parts[i] = (int32_t)std::max<int64_t>(1, (host_len[seqs[i]] + chunk - 1) / chunk);
-      need += parts[i];
-      split += parts[i] > 1;
+// Sequences that share whole pages from their first on, as groups of neighbours, where several of them fit a tile's columns.
+static void share_pages(const PageLists& lists, const int32_t* seqs, int per_tile, PagePlan& plan) {
+  std::vector<PagePlan::Entry>& es = plan.entries;
+  const auto list = [&](const PagePlan::Entry& x) { return &lists.table[(size_t)seqs[x.index] * lists.most]; };
+  const auto whole = [&](const PagePlan::Entry& x) { return lists.len[seqs[x.index]] / lists.P; };
+  // (a sequence named twice shares with itself)
+  const auto key = [&](const PagePlan::Entry& x) { return whole(x) > 0 ? list(x)[0] : -1; };
+  std::stable_sort(es.begin(), es.end(), [&](const auto& x, const auto& y) { return key(x) < key(y); });
+  for (size_t i = 0, e; i < es.size(); i = e) {
+    for (e = i + 1; e < es.size() && key(es[e]) == key(es[i]);) ++e;
+    if (key(es[i]) < 0) continue;
+    while (e - i > 1) {
+      // pages that each has in common with the first; the group, the most in common first, that saves the most reading
+      for (size_t j = i; j < e; ++j) {
+        const int most = std::min(whole(es[i]), whole(es[j]));
+        const int32_t *u = list(es[i]), *v = list(es[j]);
+        int n = 0;
+        while (n < most && u[n] == v[n]) ++n;
+        es[j].base = n;
+      }
+      std::stable_sort(es.begin() + i, es.begin() + e, [](const auto& x, const auto& y) { return x.base > y.base; });
+      size_t k = 2;
+      for (size_t j = 3; j <= e - i; ++j)
+        if ((int64_t)es[i + j - 1].base * (j - 1) > (int64_t)es[i + k - 1].base * (k - 1)) k = j;
+      const int rows = es[i + k - 1].base * lists.P;
+      const size_t in = rows < PA_SHARED ? 0 : (k % per_tile == 1 ? k - 1 : k);  // (a tile of one saves nothing)
+      for (size_t j = 0; j < k; ++j) es[i + j].base = j < in ? rows : 0;
+      for (size_t j = 0; j < in; j += per_tile) plan.tiles.push_back({(int32_t)(i + j), (int32_t)std::min<size_t>(per_tile, in - j)});
+      i += k;
     }
-    need = split ? need * state : 0;
-    if (need <= workspace_bytes) return need;
+    for (; i < e; ++i) es[i].base = 0;
   }
 }
 
-hipError_t launch_page_attention(PageAttentionArgs a, int n, const int32_t* seqs, const std::vector<int32_t>& parts, hipStream_t s) {
+void plan_page_attention(const PagePool& p, const PageLists& lists, int H, int n, const int32_t* seqs, int64_t workspace_bytes,
+                         PagePlan& plan) {
+  constexpr int64_t CUS = 256;
+  const int G = H / p.Hk, units = p.Hk * ((G + 15) / 16);
+  const int64_t state = 4 * units * part_floats(std::min(G, 16), p.D);  // bytes of a part, all heads
+  plan.entries.resize(n);
+  bool shared = false;
+  int longest = 0;
+  for (int i = 0; i < n; ++i) {
+    const int32_t s = seqs[i], len = lists.len[s];
+    plan.entries[i] = {i, 0, 0, 1, 0};
+    shared |= len >= lists.P && lists.ref[lists.table[(size_t)s * lists.most]] > 1;
+    longest = std::max(longest, len);
+  }
+  if (shared && G <= 8 && n > 1) share_pages(lists, seqs, 16 / G, plan);
+  // Short sequences that do not fill the chip: no parts, in workgroups of eight waves, and one launch.  us with and without, 32 heads
+  // over 8: one sequence of 300 rows 8.6 and 11.1, of 1,000 14.2 and 10.7, 16 of 500 10.7 and 13.2, of 1,000 15.5 and 17.9; 64 of
+  // 1,000 51 and 50, 200 of 600 108 and 103.
+  const int64_t all = (int64_t)n * units;
+  plan.wide = plan.tiles.empty() && all < 2 * CUS && longest <= (4 * all >= CUS ? 1024 : 512);
+  const auto steps = [](int64_t rows) { return (int)((rows + PA_KEYS - 1) / PA_KEYS); };
+  for (auto& x : plan.entries) x.steps = std::max(1, steps(lists.len[seqs[x.index]] - x.base));
+  // The launches, the members of a tile together.
+  for (int i = 0, tile = 0; i < n;) {
+    int m = std::min(PAGE_QUERIES, n - i), end = tile;
+    const int tiles = (int)plan.tiles.size();
+    while (end < tiles && plan.tiles[end].first + plan.tiles[end].members <= i + m) ++end;
+    if (end < tiles && plan.tiles[end].first < i + m) m = plan.tiles[end].first - i;
+    plan.launches.push_back({i, m, tile, end - tile, 1, 1, m, 0});
+    i += m;
+    tile = end;
+  }
+  const auto whole = [&] {  // a workgroup for each entry and key head
+    plan.bytes = 0;
+    for (auto& x : plan.entries) x.own = 1, x.shared = 0;
+    for (auto& l : plan.launches) l.per = 1 << 30, l.each = 1, l.workgroups = l.n, l.parts = 0;
+  };
+  if (plan.wide) return whole();
+  // As many steps for every workgroup, at least four (one for each wave), so that all of them run at once and end together; a
+  // workgroup's steps may begin in one sequence and end in another.  Where those stretches are many and short, their starts and ends
+  // weigh more than an even share: then each is a workgroup of its own (as where a workgroup's steps are few).  us, the one and the other: 64 uneven histories of 7,700
+  // rows (32 heads over 8) 336 and 445, 16 of 4,100 55 and 65; 64 of 740 fp8 rows (32 over 32) behind shared ones 144 and 107, one
+  // of 60,000 and 63 of 10 (32 over 32) 350 and 238.  More workgroups than CUs: 16 of 4,100 56 instead of 55, one of 100,003 77
+  // instead of 75.
+  const auto cut = [&](int64_t workgroups) {
+    int64_t most = 0;
+    for (auto& l : plan.launches) {
+      int64_t total = 0, stretches = l.n_tiles + l.n;
+      for (int t = 0; t < l.n_tiles; ++t) total += steps(plan.entries[plan.tiles[l.first_tile + t].first].base);
+      for (int j = 0; j < l.n; ++j) total += plan.entries[l.first + j].steps;
+      l.per = (int)std::max<int64_t>(4, (total + workgroups - 1) / workgroups);
+      l.workgroups = (int)((total + l.per - 1) / l.per);
+      l.each = l.per < 16 || (stretches > 3 * l.workgroups && total < (p.fp8 ? 128 : 64) * stretches);
+      const auto parts = [&](int64_t at, int64_t count) {
+        return (int)(l.each ? (count + l.per - 1) / l.per : (at + count - 1) / l.per - at / l.per + 1);
+      };
+      int64_t at = 0, split = 0;
+      stretches = l.parts = 0;
+      for (int t = 0; t < l.n_tiles; ++t) {
+        const auto& x = plan.tiles[l.first_tile + t];
+        const int count = steps(plan.entries[x.first].base), m = parts(at, count);
+        for (int j = 0; j < x.members; ++j) plan.entries[x.first + j].shared = m;
+        stretches += m;
+        at += count;
+      }
+      for (int j = 0; j < l.n; ++j) {
+        auto& x = plan.entries[l.first + j];
+        x.own = parts(at, x.steps);
+        stretches += x.own;
+        l.parts += x.own + x.shared;
+        split += x.own + x.shared > 1;
+        at += x.steps;
+      }
+      if (l.each) l.workgroups = (int)stretches;
+      if (!split) l.parts = 0;
+      most += l.parts;
+    }
+    plan.bytes = most * state;
+  };
+  int64_t w = std::max<int64_t>(1, CUS / units);
+  for (cut(w); plan.bytes > workspace_bytes && w > 1;) cut(w /= 2);
+  if (plan.bytes > workspace_bytes) {
+    plan.tiles.clear();
+    for (auto& x : plan.entries) x.base = 0;
+    for (auto& l : plan.launches) l.first_tile = l.n_tiles = 0;
+    for (auto& x : plan.entries) x.steps = std::max(1, steps(lists.len[seqs[x.index]]));
+    whole();
+  }
+}
+
+hipError_t launch_page_attention(PageAttentionArgs a, const int32_t* seqs, const PagePlan& plan, hipStream_t s) {
   const PagePool& p = a.pool;
   const int blocks = (a.G + 15) / 16, rows = std::min(a.G, 16);
-  for (int i = 0; i < n;) {
-    a.n = std::min(PAGE_QUERIES, n - i);
-    a.row = i;
-    a.prefix[0] = 0;
-    bool split = false;
-    for (int j = 0; j < a.n; ++j) {
-      a.seq[j] = seqs[i + j];
-      a.prefix[j + 1] = a.prefix[j] + parts[i + j];
-      split |= parts[i + j] > 1;
+  for (const auto& l : plan.launches) {
+    a.n = l.n;
+    a.n_tiles = l.n_tiles;
+    a.per = l.per;
+    a.each = l.each;
+    a.all[0] = a.tile_steps[0] = a.tile_parts[0] = 0;
+    for (int t = 0; t < l.n_tiles; ++t) {
+      const PagePlan::Tile& x = plan.tiles[l.first_tile + t];
+      a.tile[t] = (uint8_t)(x.first - l.first);
+      a.members[t] = (uint8_t)x.members;
+      a.tile_steps[t + 1] = a.tile_steps[t] + (plan.entries[x.first].base + PA_KEYS - 1) / PA_KEYS;
+      a.tile_parts[t + 1] = a.tile_parts[t] + plan.entries[x.first].shared;
     }
-    const dim3 grid(a.prefix[a.n], p.Hk * blocks), merge(a.n, a.H);
-    const auto fn = p.D == 64 ? (p.fp8 ? k_page_attention<64, true> : k_page_attention<64, false>)
-                              : (p.fp8 ? k_page_attention<128, true> : k_page_attention<128, false>);
-    hipLaunchKernelGGL(fn, grid, dim3(256), 0, s, a);
-    if (split) {
+    a.steps[0] = a.tiled = a.tile_steps[l.n_tiles];
+    a.parts[0] = a.tiled_parts = a.tile_parts[l.n_tiles];
+    for (int j = 0; j < l.n; ++j) {
+      const PagePlan::Entry& x = plan.entries[l.first + j];
+      a.seq[j] = seqs[x.index];
+      a.row[j] = (uint16_t)x.index;
+      a.base[j] = x.base;
+      a.steps[j + 1] = a.steps[j] + x.steps;
+      a.parts[j + 1] = a.parts[j] + x.own;
+      a.all[j + 1] = a.all[j] + x.own + x.shared;
+    }
+    a.total = a.steps[l.n];
+    const dim3 grid(l.workgroups, p.Hk * blocks), merge(l.n, a.H);
+    if (plan.wide) {
+      const auto fn = p.D == 64 ? (p.fp8 ? k_page_attention<64, true, 8> : k_page_attention<64, false, 8>)
+                                : (p.fp8 ? k_page_attention<128, true, 8> : k_page_attention<128, false, 8>);
+      hipLaunchKernelGGL(fn, grid, dim3(512), 0, s, a);
+    } else {
+      const auto fn = p.D == 64 ? (p.fp8 ? k_page_attention<64, true, 4> : k_page_attention<64, false, 4>)
+                                : (p.fp8 ? k_page_attention<128, true, 4> : k_page_attention<128, false, 4>);
+      hipLaunchKernelGGL(fn, grid, dim3(256), 0, s, a);
+    }
+    if (l.parts) {
       if (p.D == 64) hipLaunchKernelGGL(k_page_merge<64>, merge, dim3(256), 0, s, a);
       else hipLaunchKernelGGL(k_page_merge<128>, merge, dim3(256), 0, s, a);
     }
-    a.part += (int64_t)a.prefix[a.n] * p.Hk * blocks * part_floats(rows, p.D);
-    i += a.n;
+    a.part += (int64_t)l.parts * p.Hk * blocks * part_floats(rows, p.D);
   }
   return hipGetLastError();
 }

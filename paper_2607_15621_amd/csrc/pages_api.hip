@@ -312,8 +312,9 @@ extern "C" int fsx_pages_attention_workspace(const fsx_pages* h, const fsx_promp
   return guarded([&]() -> int {
     if (!h) return bad("pages is NULL");
     if (const int rc = check_attention(h, d, n, seqs)) return rc;
-    std::vector<int32_t> parts;
-    *bytes = plan_page_attention(h->pool(), d->n_heads, n, seqs, h->lists.len.data(), INT64_MAX, parts);
+    PagePlan plan;
+    plan_page_attention(h->pool(), h->lists, d->n_heads, n, seqs, INT64_MAX, plan);
+    *bytes = plan.bytes;
     return done();
   });
 }
@@ -338,9 +339,9 @@ extern "C" int fsx_pages_attention(fsx_pages* h, const fsx_prompt_desc* d, int32
     a.H = d->n_heads; a.G = d->n_heads / h->cfg.n_kv_heads; a.layer = layer;
     a.q_f32 = d->q_dtype == FSX_F32; a.o_f32 = d->out_dtype == FSX_F32;
     a.c = (d->scale > 0.f ? d->scale : 1.0f / sqrtf((float)d->head_dim)) * 1.4426950408889634f;
-    std::vector<int32_t> parts;
-    plan_page_attention(a.pool, a.H, n, seqs, h->lists.len.data(), workspace_bytes, parts);
-    const hipError_t e = launch_page_attention(a, n, seqs, parts, (hipStream_t)stream);
+    PagePlan plan;
+    plan_page_attention(a.pool, h->lists, a.H, n, seqs, workspace_bytes, plan);
+    const hipError_t e = launch_page_attention(a, seqs, plan, (hipStream_t)stream);
     return e == hipSuccess ? done() : hip_error("the attention's kernels", e);
   });
 }

@@ -102,12 +102,12 @@ class Pool:
         return parts[0].to(F64), parts[1].to(F64)
 
 
-def attend(q, k, v, scale):
+def attend(q, k, v, scale, weight=2.0 ** -16):
     """One token's attention in 64 bits: q [heads][channels], k, v [rows][key heads][channels]; output, its tolerance without the
     output's rounding, log sums and theirs.
 
-    With A = sum_j P_j |v_j| and half a bf16 step u = 2^-8: the weights' rounding moves an output by at most u A.  A score is a sum of
-    D products in fp32, scaled (an fp8 row's scale among it) by two roundings more: off by at most
+    With A = sum_j P_j |v_j|: a weight is two bf16 values, each rounded by at most half a step, 2^-8 of it, the second of what the
+    first left, so an output moves by at most 2^-16 A (fsx_prompt_attention rounds them once: `weight` is U there).  A score is a sum of D products in fp32, scaled (an fp8 row's scale among it) by two roundings more: off by at most
     ds = (D + 6) 2^-24 scale sum_c |q_c k_c|, which changes every weight by a factor within exp(+-2 ds); the exponentials are off by
     2^-22, and the statistics, sums and the merges of parts add (rows + 64) roundings of 2^-24."""
     q = q.to(BF16).to(F64)
@@ -122,7 +122,7 @@ def attend(q, k, v, scale):
         z = torch.logsumexp(s, 0)
         p = torch.exp(s - z)
         ds = (D + 6) * 2.0 ** -24 * big + (n + 64) * 2.0 ** -24 + 2.0 ** -22
-        out[h], tol[h] = p @ vh, (p @ vh.abs()) * (U + 4 * ds) + 1e-30
+        out[h], tol[h] = p @ vh, (p @ vh.abs()) * (weight + 4 * ds) + 1e-30
         lse[h], ltol[h] = z, 2 * ds + 2.0 ** -22 * z.abs() + 1e-7
     return out, tol, lse, ltol
 

@@ -191,6 +191,55 @@ def test_the_same_bits_again_and_in_graphs():
             p.extend([0, 1, 3], [17, 100, 1])
 
 
+@kinds
+@pytest.mark.parametrize("G", [1, 2, 3, 5, 8, 9])
+def test_shared_pages(fp8, D, G):
+    """Forks of forks that share from nothing to everything, one of them twice, an empty one, sequences that share nothing."""
+    p = Pool(seqs=16, pages=400, most=60, P=16, D=D, fp8=fp8, L=1, H=2)
+    p.extend([0, 14], [700, 333])
+    p.fork([0] * 8, [1, 2, 3, 4, 5, 6, 7, 8], [700, 700, 650, 640, 641, 400, 20, 0])
+    p.extend([1, 3, 4, 8, 15], [1, 30, 200, 70, 5])
+    p.fork([4, 4, 14], [9, 10, 11])
+    p.extend([9, 0, 11], [100, 3, 16])
+    for seqs in ([5, 0, 9, 1, 14, 2, 3, 3, 12, 11, 4, 15, 10, 8, 7, 6], [0, 2], [14, 11, 0, 1, 2], list(range(16)) * 9):
+        q = queries(p, len(seqs), 2 * G)
+        out, lse = run(p, 0, q, seqs)
+        check_attention(p, 0, q[:16], out[:16], lse[:16], seqs[:16])
+        if len(seqs) > 100:
+            check_attention(p, 0, q[120:], out[120:], lse[120:], seqs[120:])
+        again = run(p, 0, q, seqs)
+        assert torch.equal(again[0], out) and torch.equal(again[1], lse)
+        for ws in (torch.empty(0, dtype=torch.uint8, device="cuda"), torch.empty(20000, dtype=torch.uint8, device="cuda")):
+            less = torch.empty_like(out)
+            p.pages.attention(0, q, less, seqs, workspace=ws)
+            check_attention(p, 0, q[:16], less[:16], None, seqs[:16])
+
+
+@pytest.mark.parametrize("fp8", [False, True], ids=["bf16", "fp8"])
+def test_pages_that_are_no_longer_shared_in_a_replay(fp8):
+    """A graph that read shared pages once: members that grow, are pruned, are freed, and forked from elsewhere."""
+    p = Pool(seqs=8, pages=300, most=60, P=16, fp8=fp8, L=1, H=2)
+    p.extend([0, 7], [600, 500])
+    p.fork([0] * 4, [1, 2, 3, 4])
+    p.extend([0, 1, 2, 3, 4], [5, 1, 40, 100, 17])
+    seqs, side = [2, 0, 4, 1, 3], torch.cuda.Stream()
+    q = queries(p, 5, 4)
+    out, lse = torch.zeros_like(q), torch.zeros(q.shape[:2], device="cuda")
+    ws = torch.empty(p.pages.attention_workspace(q, seqs), dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        p.pages.attention(0, q, out, seqs, lse=lse, workspace=ws)
+    for change in (lambda: None, lambda: p.extend([1, 3], [20, 1]), lambda: p.keep([4], [[(0, 64), (96, 521)]]),
+                   lambda: p.keep([0, 2], [[(0, 300)], [(1, 639)]]), lambda: p.free([0]), lambda: (p.free([1]), p.fork([7], [1])),
+                   lambda: p.extend([0, 1], [33, 1]), lambda: p.free([2, 3, 4, 0, 1])):
+        change()
+        q.copy_(queries(p, 5, 4))
+        graph.replay()
+        torch.cuda.synchronize()
+        check_attention(p, 0, q, out, lse, seqs)
+
+
 def test_two_streams_at_once():
     p = Pool(seqs=2, pages=200, most=100, P=16, L=1, H=2)
     p.extend([0, 1], [1500, 1400])
@@ -293,7 +342,7 @@ def test_a_decoder_step(fp8):
         host = x.cpu()
         a = 0
         for s, m in enumerate(lens):  # the last token's own attention
-            o, tol, _, _ = attend(host[a + m - 1, :H], host[a:a + m, H:H + Hk].to(F64), host[a:a + m, H + Hk:].to(F64), D ** -0.5)
+            o, tol, _, _ = attend(host[a + m - 1, :H], host[a:a + m, H:H + Hk].to(F64), host[a:a + m, H + Hk:].to(F64), D ** -0.5, U)
             near(out[a + m - 1].cpu().to(F64), o, tol + U * (o.abs() + tol), "prompt")
             a += m
         stored[layer] = host
