@@ -297,16 +297,20 @@ struct PagePool {
   const int32_t* len;
   int32_t layers, pages, Hk, P, shift, D, fp8, most;  // P = 1 << shift
 };
-// Entries of lists and lengths, and pages copied.
-constexpr int PAGE_RUNS = 80, PAGE_COPIES = 150;
+// Entries of lists and lengths, and pages copied, up to four copies of one page side by side.
+constexpr int PAGE_RUNS = 80, PAGE_COPIES = 64, PAGE_TARGETS = 4;
+struct PageCopies {
+  int32_t from, rows, n, to[PAGE_TARGETS];
+};
 struct PageUpdateArgs {
   PagePool pool;
   int32_t* table;  // written; copied entries come from pool.table
   int32_t* len;    // NULL: lengths stay
   int32_t n_runs, n_copies;
   PageRun runs[PAGE_RUNS];
-  PageCopy copies[PAGE_COPIES];
+  PageCopies copies[PAGE_COPIES];
 };
+static_assert(sizeof(PageUpdateArgs) <= 4096, "kernel arguments");
 hipError_t launch_page_update(const PagePool& pool, int32_t* table, int32_t* len, const std::vector<PageRun>& runs,
                               const std::vector<PageCopy>& copies, hipStream_t s);
 // Rows that close up: row i of the outcome, from `start` on, is row i - to + first of the last range with to <= i.
@@ -314,7 +318,7 @@ constexpr int PAGE_MOVES = 64, PAGE_RANGES = 256;
 struct PageMoveArgs {
   PagePool pool;
   const int32_t* to_table;
-  int32_t n_moves;
+  int32_t n_moves, split;  // workgroups that share a row's channels
   PageMove moves[PAGE_MOVES];
   PageRange ranges[PAGE_RANGES];  // count: the first row's place in the outcome
 };

@@ -15,7 +15,8 @@ __device__ __forceinline__ int64_t page_row(const PagePool& p, int layer, int pa
 }
 
 // ---------------------------------------------------------------------------------------------------------------
-// A workgroup for each run of entries, and one for each copied page, layer and head.
+// A workgroup for each run of entries, and one for each copied page, layer, head, and keys or values; it reads the page's rows once
+// for up to four copies (16 copies of 43 rows, 32 layers of 8 heads, 96 MB: @FORK@).
 __global__ __launch_bounds__(256) void k_page_update(PageUpdateArgs a) {
   const PagePool& p = a.pool;
   if ((int)blockIdx.x < a.n_runs) {
@@ -26,106 +27,171 @@ __global__ __launch_bounds__(256) void k_page_update(PageUpdateArgs a) {
     if (a.len && threadIdx.x == 0) a.len[r.seq] = r.len;
     return;
   }
-  const int i = blockIdx.x - a.n_runs, n = a.n_copies, lh = i / n;  // a page's copies side by side
-  const PageCopy c = a.copies[i - lh * n];
-  const int layer = lh / p.Hk, h = lh - layer * p.Hk;
-  const int64_t from = page_row(p, layer, c.from, h, 0), to = page_row(p, layer, c.to, h, 0);
+  const int i = blockIdx.x - a.n_runs, kv = i & 1, n = a.n_copies, lh = (i >> 1) / n;
+  const PageCopies& c = a.copies[(i >> 1) - lh * n];
+  const int layer = lh / p.Hk, h = lh - layer * p.Hk, targets = c.n;
   const int es = p.fp8 ? 1 : 2, pieces = c.rows * p.D * es / 16;
-  const auto copy = [&](void* base) {
-    const u32x4_t* src = reinterpret_cast<const u32x4_t*>((const char*)base + from * p.D * es);
-    u32x4_t* dst = reinterpret_cast<u32x4_t*>((char*)base + to * p.D * es);
-    for (int e0 = threadIdx.x; e0 < pieces; e0 += 4 * 256) {
-      u32x4_t x[4];
+  const int64_t from = page_row(p, layer, c.from, h, 0);
+  char* base = (char*)(kv ? p.v : p.k);
+  int64_t to[PAGE_TARGETS];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) x[u] = src[min(e0 + 256 * u, pieces - 1)];
+  for (int t = 0; t < PAGE_TARGETS; ++t) to[t] = page_row(p, layer, c.to[t], h, 0);
+  const u32x4_t* src = reinterpret_cast<const u32x4_t*>(base + from * p.D * es);
+  for (int e0 = threadIdx.x; e0 < pieces; e0 += 4 * 256) {
+    u32x4_t x[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) x[u] = src[min(e0 + 256 * u, pieces - 1)];
+#pragma unroll
+    for (int t = 0; t < PAGE_TARGETS; ++t) {
+      if (t >= targets) break;
+      u32x4_t* dst = reinterpret_cast<u32x4_t*>(base + to[t] * p.D * es);
 #pragma unroll
       for (int u = 0; u < 4; ++u)
         if (e0 + 256 * u < pieces) dst[e0 + 256 * u] = x[u];
     }
-  };
-  copy(p.k);
-  copy(p.v);
-  if (p.fp8)
-    for (int e = threadIdx.x; e < c.rows; e += 256) {
-      p.k_scale[to + e] = p.k_scale[from + e];
-      p.v_scale[to + e] = p.v_scale[from + e];
-    }
+  }
+  if (p.fp8) {
+    float* scales = kv ? p.v_scale : p.k_scale;
+    for (int e = threadIdx.x; e < c.rows; e += 256)
+      for (int t = 0; t < targets; ++t) scales[page_row(p, layer, c.to[t], h, e)] = scales[from + e];
+  }
 }
 
 hipError_t launch_page_update(const PagePool& pool, int32_t* table, int32_t* len, const std::vector<PageRun>& runs,
                               const std::vector<PageCopy>& copies, hipStream_t s) {
-  PageUpdateArgs a;
+  PageUpdateArgs a{};
   a.pool = pool;
   a.table = table;
   a.len = len;
   for (size_t r = 0, c = 0; r < runs.size() || c < copies.size();) {
     a.n_runs = (int)std::min<size_t>(PAGE_RUNS, runs.size() - r);
-    a.n_copies = (int)std::min<size_t>(PAGE_COPIES, copies.size() - c);
     std::copy_n(runs.begin() + r, a.n_runs, a.runs);
-    std::copy_n(copies.begin() + c, a.n_copies, a.copies);
     r += a.n_runs;
-    c += a.n_copies;
-    hipLaunchKernelGGL(k_page_update, dim3(a.n_runs + a.n_copies * pool.layers * pool.Hk), dim3(256), 0, s, a);
+    for (a.n_copies = 0; c < copies.size(); ++c) {
+      PageCopies* last = a.n_copies ? &a.copies[a.n_copies - 1] : nullptr;
+      if (last && last->from == copies[c].from && last->rows == copies[c].rows && last->n < PAGE_TARGETS) {
+        last->to[last->n++] = copies[c].to;
+      } else {
+        if (a.n_copies == PAGE_COPIES) break;
+        a.copies[a.n_copies++] = {copies[c].from, copies[c].rows, 1, {copies[c].to}};
+      }
+    }
+    hipLaunchKernelGGL(k_page_update, dim3(a.n_runs + 2 * a.n_copies * pool.layers * pool.Hk), dim3(256), 0, s, a);
   }
   return hipGetLastError();
 }
 
 // ---------------------------------------------------------------------------------------------------------------
-// Rows that close up, in place where the sequence has its pages alone.  A workgroup takes one head of one layer, keys or values, of
-// a sequence from its first row that is written to its last: no row moves up, so the rows that a stretch of the outcome overwrites
-// come from that stretch or have been read before, and a stretch is read whole before it is written.
+// Rows that close up, in place where the sequence has its pages alone.  A workgroup takes one head of one layer, keys or values (or
+// some of their channels), of a sequence from its first row that is written to its last: no row moves up, so the rows that a stretch
+// of the outcome overwrites come from that stretch or have been read before.  A stretch is read whole before it is written, and the
+// next one is on its way by then (16 sequences of 1,024 rows, 560 of them moved, 4 layers of 8 heads, 294 MB: @MOVE@).
 __global__ __launch_bounds__(256) void k_page_move(PageMoveArgs a) {
   __shared__ PageRange ranges[PAGE_RANGES];
   const PagePool& p = a.pool;
   const PageMove m = a.moves[blockIdx.y];
   for (int i = threadIdx.x; i < m.n_ranges; i += 256) ranges[i] = a.ranges[m.range + i];
   __syncthreads();
-  const int lh = blockIdx.x >> 1, kv = blockIdx.x & 1, layer = lh / p.Hk, h = lh - layer * p.Hk;
-  const int es = p.fp8 ? 1 : 2, ppr = p.D * es / 16;  // pieces of a row
-  char* base = (char*)(kv ? p.v : p.k);
-  float* scales = kv ? p.v_scale : p.k_scale;
+  const int unit = blockIdx.x / a.split, part = blockIdx.x - unit * a.split;
+  const int lh = unit >> 1, kv = unit & 1, layer = lh / p.Hk, h = lh - layer * p.Hk;
+  const int es = p.fp8 ? 1 : 2, ppr = p.D * es / 16 / a.split;  // pieces of a row: 4, 8 or 16
+  char* base = (char*)(kv ? p.v : p.k) + part * ppr * 16;
+  float* scales = p.fp8 && part == 0 ? (kv ? p.v_scale : p.k_scale) : nullptr;
   const int32_t* from = p.table + (int64_t)m.seq * p.most;
   const int32_t* to = a.to_table + (int64_t)m.seq * p.most;
-  const auto source = [&](int i) {
+  const auto source = [&](int i) {  // the row that becomes row i
     int lo = 0;
     for (int n = m.n_ranges; n > 1;) {  // the last range that begins at or before row i
       const int half = n >> 1;
       if (ranges[lo + half].count <= i) lo += half;
       n -= half;
     }
-    const int r = i - ranges[lo].count + ranges[lo].first;
-    return page_row(p, layer, from[r >> p.shift], h, r & (p.P - 1));
+    return i - ranges[lo].count + ranges[lo].first;
   };
-  const auto target = [&](int i) { return page_row(p, layer, to[i >> p.shift], h, i & (p.P - 1)); };
+  const auto place = [&](int page, int row) { return page_row(p, layer, page, h, row & (p.P - 1)); };
   constexpr int U = 4;
-  const int stretch = U * 256 / ppr;  // rows; 256 at most
-  for (int i0 = m.start; i0 < m.rows; i0 += stretch) {
-    const int n = min(stretch, m.rows - i0) * ppr;
+  const int stretch = U * 256 / ppr, shift = __builtin_ctz(ppr);  // rows; 256 at most
+  // Where a stretch's pieces come from and go to is looked up two stretches ahead: loads come back in order, so pages looked up
+  // behind the rows under way would come when those have.
+  struct Pages {
+    int row[U], from[U], to[U], scale_row, scale_from, scale_to;
+  };
+  struct Stretch {
     u32x4_t x[U];
-    float sc = 0.f;
+    int to[U], scale_to;
+    float scale;
+  };
+  const auto look_up = [&](Pages& g, int i0) {
+    const int n = min(stretch, m.rows - i0) * ppr;
+    if (n <= 0) return;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int e = min((int)threadIdx.x + 256 * u, n - 1), i = e / ppr;
-      x[u] = *reinterpret_cast<const u32x4_t*>(base + source(i0 + i) * p.D * es + 16 * (e - i * ppr));
+      const int i = i0 + (min((int)threadIdx.x + 256 * u, n - 1) >> shift);
+      g.row[u] = source(i);
+      g.from[u] = from[g.row[u] >> p.shift];
+      g.to[u] = to[i >> p.shift];
     }
-    const bool scaled = p.fp8 && (int)threadIdx.x < min(stretch, m.rows - i0);
-    if (scaled) sc = scales[source(i0 + threadIdx.x)];
-    vm_wait_all();  // (a barrier alone does not wait for loads)
-    __syncthreads();
+    if (scales) {
+      const int i = i0 + min((int)threadIdx.x, (n >> shift) - 1);
+      g.scale_row = source(i);
+      g.scale_from = from[g.scale_row >> p.shift];
+      g.scale_to = to[i >> p.shift];
+    }
+  };
+  const auto load = [&](Stretch& s, const Pages& g, int i0) {
+    const int n = min(stretch, m.rows - i0) * ppr;
+    if (n <= 0) return;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int e = (int)threadIdx.x + 256 * u, i = e / ppr;
-      if (e < n) *reinterpret_cast<u32x4_t*>(base + target(i0 + i) * p.D * es + 16 * (e - i * ppr)) = x[u];
+      const int e = min((int)threadIdx.x + 256 * u, n - 1);
+      s.x[u] = *reinterpret_cast<const u32x4_t*>(base + place(g.from[u], g.row[u]) * p.D * es + 16 * (e & (ppr - 1)));
+      s.to[u] = g.to[u];
     }
-    if (scaled) scales[target(i0 + threadIdx.x)] = sc;
+    if (scales) {
+      s.scale = scales[place(g.scale_from, g.scale_row)];
+      s.scale_to = g.scale_to;
+    }
+  };
+  const auto store = [&](Stretch& s, int i0) {
+    // all of the stretch is read: this wave's part has arrived (the registers are needed here), and so have the others'
+    asm volatile("" : "+v"(s.x[0]), "+v"(s.x[1]), "+v"(s.x[2]), "+v"(s.x[3]), "+v"(s.scale)::"memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    const int n = min(stretch, m.rows - i0) * ppr;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int e = (int)threadIdx.x + 256 * u;
+      if (e < n) *reinterpret_cast<u32x4_t*>(base + place(s.to[u], i0 + (e >> shift)) * p.D * es + 16 * (e & (ppr - 1))) = s.x[u];
+    }
+    if (scales && (int)threadIdx.x < n >> shift) scales[place(s.scale_to, i0 + (int)threadIdx.x)] = s.scale;
+  };
+  Pages g[2];
+  Stretch s[2];
+  s[0].scale = s[1].scale = 0.f;
+  look_up(g[0], m.start);
+  look_up(g[1], m.start + stretch);
+  load(s[0], g[0], m.start);
+  for (int i0 = m.start; i0 < m.rows; i0 += 2 * stretch) {
+    const int i1 = i0 + stretch, i2 = i1 + stretch;
+    look_up(g[0], i2);
+    load(s[1], g[1], i1);
+    store(s[0], i0);
+    if (i1 >= m.rows) break;
+    look_up(g[1], i2 + stretch);
+    load(s[0], g[0], i2);
+    store(s[1], i1);
   }
 }
 
 hipError_t launch_page_move(const PagePool& pool, const int32_t* to_table, const std::vector<PageMove>& moves,
                             const std::vector<PageRange>& ranges, hipStream_t s) {
-  PageMoveArgs a;
+  PageMoveArgs a{};
   a.pool = pool;
   a.to_table = to_table;
+  // Channels shared out where sequences, layers and heads are few: four workgroups for each CU, or pieces of 64 bytes of a row.
+  const int64_t units = (int64_t)2 * pool.layers * pool.Hk * moves.size();
+  const int most = pool.D * (pool.fp8 ? 1 : 2) / 64;
+  for (a.split = 1; a.split < most && units * a.split < 1024;) a.split *= 2;
   for (size_t i = 0; i < moves.size();) {
     int n_ranges = 0;
     for (a.n_moves = 0; i < moves.size() && a.n_moves < PAGE_MOVES && n_ranges + moves[i].n_ranges <= PAGE_RANGES; ++i) {
@@ -140,7 +206,7 @@ hipError_t launch_page_move(const PagePool& pool, const int32_t* to_table, const
       n_ranges += m.n_ranges;
       a.moves[a.n_moves++] = m;
     }
-    hipLaunchKernelGGL(k_page_move, dim3(2 * pool.layers * pool.Hk, a.n_moves), dim3(256), 0, s, a);
+    hipLaunchKernelGGL(k_page_move, dim3(2 * pool.layers * pool.Hk * a.split, a.n_moves), dim3(256), 0, s, a);
   }
   return hipGetLastError();
 }

@@ -104,9 +104,14 @@ hipError_t launch_rotary(RotaryArgs a, hipStream_t s) {
   };
   const int v = !a.f32 && fits(8) ? 8 : (fits(4) ? 4 : 1);
   const int64_t units = (int64_t)a.heads * (a.pairs + (a.copy_rest ? a.dim - 2 * a.pairs : 0)) / v;  // of a row
-  // rows of a workgroup: a few pieces for each of its threads, once the rows are many
-  a.block = (int)std::min<int64_t>({std::max<int64_t>(1, 2048 / units), std::max<int64_t>(1, a.rows / 2048), 2048 / a.pairs});
-  a.block = (int)std::max<int64_t>(a.block, (a.rows >> 23) + 1);
+  // rows of a workgroup: up to eight pieces for each of its threads, once the rows are many, and as few threads without one in the
+  // last turn as may be (16,001 rows of 15 heads of 20 pairs of pieces: @GRAD@)
+  const int64_t most = std::max<int64_t>(1, std::min<int64_t>({2048 / units, a.rows / 2048, 2048 / a.pairs}));
+  const auto busy = [&](int64_t b) { return (double)(b * units) / ((b * units + 255) / 256 * 256); };
+  int64_t best = most;
+  for (int64_t b = most; b >= 1 && 2 * b > most; --b)
+    if (busy(b) > busy(best) + 0.02) best = b;
+  a.block = (int)std::max<int64_t>(best, (a.rows >> 23) + 1);
   const int64_t blocks = (a.rows + a.block - 1) / a.block;
   const dim3 grid((unsigned)blocks, (unsigned)std::max<int64_t>(1, std::min<int64_t>((a.block * units + 255) / 256, 2048 / blocks)));
   const auto fn = a.f32 ? (v == 4 ? k_rotary<float, 4> : k_rotary<float, 1>)
