@@ -2,6 +2,7 @@
 // sequence keeps some of them, and packed rows written into pages.  All of it is memory traffic.
 
 #include <algorithm>
+#include <type_traits>
 
 #include "codes_device.h"
 #include "common.h"
@@ -213,8 +214,29 @@ hipError_t launch_page_move(const PagePool& pool, const int32_t* to_table, const
 
 // ---------------------------------------------------------------------------------------------------------------
 // Packed rows into the last rows of their sequences.  A workgroup takes a.block rows of one sequence in one layer, keys or values,
-// and all heads; a thread 16 elements of a head's row at a time, so that the threads of a row (4 or 8) find its scale by exchange
-// and each element is read once.
+// and all heads; a thread 16 bytes of a cached row at a time.  The threads of an fp8 row (4 or 8) find its scale by exchange, so each
+// element is read once.  @WRITE@
+template <int PDT>
+struct Raw8 {
+  uint4 p[PDT == FSX_F32 ? 2 : 1];
+};
+template <int PDT, int E>
+using RawRows = std::conditional_t<E == 16, Raw16<PDT>, Raw8<PDT>>;
+template <int PDT, int E>
+__device__ __forceinline__ RawRows<PDT, E> load_rows(const void* base, int64_t at) {
+  RawRows<PDT, E> r;
+  const uint4* src = reinterpret_cast<const uint4*>((const char*)base + at * (PDT == FSX_F32 ? 4 : 2));
+#pragma unroll
+  for (int i = 0; i < (int)(sizeof(r) / 16); ++i) r.p[i] = src[i];
+  return r;
+}
+__device__ __forceinline__ uint4 to_bf16(const Raw8<FSX_BF16>& r) { return r.p[0]; }
+__device__ __forceinline__ uint4 to_bf16(const Raw8<FSX_F32>& r) {
+  const uint4 a = r.p[0], b = r.p[1];
+  return make_uint4(pack_bf16x2(__uint_as_float(a.x), __uint_as_float(a.y)), pack_bf16x2(__uint_as_float(a.z), __uint_as_float(a.w)),
+                    pack_bf16x2(__uint_as_float(b.x), __uint_as_float(b.y)), pack_bf16x2(__uint_as_float(b.z), __uint_as_float(b.w)));
+}
+
 template <int PDT, int CDT>
 __global__ __launch_bounds__(256) void k_page_write(PageWriteArgs a) {
   const PagePool& p = a.pool;
@@ -230,23 +252,26 @@ __global__ __launch_bounds__(256) void k_page_write(PageWriteArgs a) {
   const int64_t packed = l * (kv ? a.v_layer : a.k_layer) + (a.start[s] + r0) * row_step;
   char* cache = (char*)(kv ? p.v : p.k);
   float* scales = kv ? p.v_scale : p.k_scale;
-  const int cpr = p.D / 16, total = nr * p.Hk * cpr;
+  constexpr int E = CDT == FSX_BF16 ? 8 : 16;  // elements of 16 bytes
+  const int cpr = p.D / E, total = nr * p.Hk * cpr;
   for (int e0 = threadIdx.x; e0 < total; e0 += 4 * 256) {
-    Raw16<PDT> in[4];
+    RawRows<PDT, E> in[4];
     int64_t at[4];
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       // (past the end: the last row again, by whole rows)
       const int e = e0 + 256 * u < total ? e0 + 256 * u : total - cpr + e0 % cpr;
       const int c = e % cpr, i = e / cpr, r = i / p.Hk, h = i - r * p.Hk, row = max(first + r, 0);
-      in[u] = load_raw<PDT>(rows, packed + r * row_step + h * head_step + 16 * c);
+      in[u] = load_rows<PDT, E>(rows, packed + r * row_step + h * head_step + E * c);
       at[u] = page_row(p, a.layer + l, pages[row >> p.shift], h, row & (p.P - 1));
     }
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       const int e = e0 + 256 * u, c = e % cpr;
-      float scale = 1.f;
-      if constexpr (CDT == FSX_FP8_E4M3) {
+      const bool valid = e < total && first + (e / cpr) / p.Hk >= 0;
+      if constexpr (CDT == FSX_BF16) {
+        if (valid) *reinterpret_cast<uint4*>((uint16_t*)cache + at[u] * p.D + E * c) = to_bf16(in[u]);
+      } else {
         uint32_t t = 0;
 #pragma unroll
         for (int i = 0; i < Raw16<PDT>::N; ++i) t = fold_top<PDT>(t, in[u].p[i], false);
@@ -264,12 +289,12 @@ __global__ __launch_bounds__(256) void k_page_write(PageWriteArgs a) {
         top = fmaxf(top, other(top, std::integral_constant<int, 0xB1>{}));
         top = fmaxf(top, other(top, std::integral_constant<int, 0x4E>{}));
         if (cpr == 8) top = fmaxf(top, other(top, std::integral_constant<int, 0x141>{}));
-        scale = scale_of(top, 1.f);
-      }
-      const auto out = convert<PDT, CDT>(in[u], scale);
-      if (e < total && first + (e / cpr) / p.Hk >= 0) {
-        store_raw<CDT>(cache, at[u] * p.D + 16 * c, out);
-        if (CDT == FSX_FP8_E4M3 && c == 0) scales[at[u]] = scale;
+        const float scale = scale_of(top, 1.f);
+        const auto out = convert<PDT, CDT>(in[u], scale);
+        if (valid) {
+          store_raw<CDT>(cache, at[u] * p.D + 16 * c, out);
+          if (c == 0) scales[at[u]] = scale;
+        }
       }
     }
   }
@@ -280,7 +305,7 @@ hipError_t launch_page_write(PageWriteArgs a, int n, const int32_t* seqs, const 
   int64_t total = 0;
   for (int i = 0; i < n; ++i) total += rows[i];
   // rows of a workgroup: four pieces for every thread, once there are workgroups enough
-  const int64_t full = std::max<int64_t>(1, 4 * 256 / (p.Hk * (p.D / 16)));
+  const int64_t full = std::max<int64_t>(1, 4 * 256 / (p.Hk * (p.D / (p.fp8 ? 16 : 8))));
   a.block = (int)std::max<int64_t>({1, std::min<int64_t>(full, total * a.n_layers * 2 / 2048), (total >> 23) + 1});
   for (int i = 0; i < n;) {
     a.n = 0;
