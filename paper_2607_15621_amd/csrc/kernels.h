@@ -318,11 +318,12 @@ constexpr int PAGE_MOVES = 64, PAGE_RANGES = 256;
 struct PageMoveArgs {
   PagePool pool;
   const int32_t* to_table;
+  int32_t* len;            // lengths of the sequences that move, or NULL
   int32_t n_moves, split;  // workgroups that share a row's channels
   PageMove moves[PAGE_MOVES];
   PageRange ranges[PAGE_RANGES];  // count: the first row's place in the outcome
 };
-hipError_t launch_page_move(const PagePool& pool, const int32_t* to_table, const std::vector<PageMove>& moves,
+hipError_t launch_page_move(const PagePool& pool, const int32_t* to_table, int32_t* len, const std::vector<PageMove>& moves,
                             const std::vector<PageRange>& ranges, hipStream_t s);
 // Packed rows into the last rows of sequences.
 constexpr int PAGE_WRITES = 128;

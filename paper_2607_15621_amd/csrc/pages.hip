@@ -91,6 +91,7 @@ __global__ __launch_bounds__(256) void k_page_move(PageMoveArgs a) {
   __shared__ PageRange ranges[PAGE_RANGES];
   const PagePool& p = a.pool;
   const PageMove m = a.moves[blockIdx.y];
+  if (a.len && blockIdx.x == 0 && threadIdx.x == 0) a.len[m.seq] = m.rows;  // (not read here)
   for (int i = threadIdx.x; i < m.n_ranges; i += 256) ranges[i] = a.ranges[m.range + i];
   __syncthreads();
   const int unit = blockIdx.x / a.split, part = blockIdx.x - unit * a.split;
@@ -184,11 +185,12 @@ __global__ __launch_bounds__(256) void k_page_move(PageMoveArgs a) {
   }
 }
 
-hipError_t launch_page_move(const PagePool& pool, const int32_t* to_table, const std::vector<PageMove>& moves,
+hipError_t launch_page_move(const PagePool& pool, const int32_t* to_table, int32_t* len, const std::vector<PageMove>& moves,
                             const std::vector<PageRange>& ranges, hipStream_t s) {
   PageMoveArgs a{};
   a.pool = pool;
   a.to_table = to_table;
+  a.len = len;
   // Channels shared out where sequences, layers and heads are few: four workgroups for each CU, or pieces of 64 bytes of a row.
   const int64_t units = (int64_t)2 * pool.layers * pool.Hk * moves.size();
   const int most = pool.D * (pool.fp8 ? 1 : 2) / 64;

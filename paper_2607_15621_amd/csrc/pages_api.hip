@@ -241,9 +241,19 @@ extern "C" int fsx_pages_keep(fsx_pages* h, int32_t n, const int32_t* seqs, cons
     if (const int rc = l.keep(n, seqs, n_ranges, first, count)) return set_error(rc, l.error);
     const hipStream_t s = (hipStream_t)stream;
     const PagePool pool = h->pool();
-    // where pages are replaced, the rows move by both lists before the new one becomes the sequence's
-    hipError_t e = l.before.empty() ? hipSuccess : launch_page_update(pool, h->next, nullptr, l.before, {}, s);
-    if (e == hipSuccess) e = launch_page_move(pool, l.before.empty() ? h->table : h->next, l.moves, l.ranges, s);
+    // Where pages are replaced, the rows move by both lists before the new one becomes the sequence's; elsewhere the lists stay, and
+    // the lengths are set with the rows.
+    const bool in_place = l.before.empty();
+    hipError_t e = in_place ? hipSuccess : launch_page_update(pool, h->next, nullptr, l.before, {}, s);
+    if (e == hipSuccess) e = launch_page_move(pool, in_place ? h->table : h->next, in_place ? h->len : nullptr, l.moves, l.ranges, s);
+    if (in_place) {
+      size_t m = 0, left = 0;
+      for (const PageRun& r : l.runs) {
+        if (m < l.moves.size() && l.moves[m].seq == r.seq) ++m;
+        else l.runs[left++] = r;
+      }
+      l.runs.resize(left);
+    }
     if (e == hipSuccess) e = launch_page_update(pool, h->table, h->len, l.runs, {}, s);
     return enqueued(h, e);
   });
