@@ -507,19 +507,22 @@ void plan_page_attention(const PagePool& p, const PageLists& lists, int H, int n
   if (plan.wide) return whole();
   // As many steps for every workgroup, at least four (one for each wave), so that all of them run at once and end together; a
   // workgroup's steps may begin in one sequence and end in another.  Where those stretches are many and short, their starts and ends
-  // weigh more than an even share: then each is a workgroup of its own (as where a workgroup's steps are few).  us, the one and the other: 64 uneven histories of 7,700
+  // weigh more than an even share: then each is a workgroup of its own.  us, the one and the other: 64 uneven histories of 7,700
   // rows (32 heads over 8) 336 and 445, 16 of 4,100 55 and 65; 64 of 740 fp8 rows (32 over 32) behind shared ones 144 and 107, one
-  // of 60,000 and 63 of 10 (32 over 32) 350 and 238.  More workgroups than CUs: 16 of 4,100 56 instead of 55, one of 100,003 77
-  // instead of 75.
+  // of 60,000 and 63 of 10 (32 over 32) 350 and 238.  So too where a share is short, with two workgroups for each CU if there are
+  // several sequences: 16 of 301 to 1,051 15.3 instead of 17.4, 16 of 1,500 fp8 rows 16.8 instead of 19.3, five of 300 to 5,000 15.2
+  // instead of 17.4.  Otherwise more workgroups than CUs cost: 16 of 4,100 56 instead of 55, one of 100,003 77 instead of 75.
   const auto cut = [&](int64_t workgroups) {
     int64_t most = 0;
     for (auto& l : plan.launches) {
       int64_t total = 0, stretches = l.n_tiles + l.n;
       for (int t = 0; t < l.n_tiles; ++t) total += steps(plan.entries[plan.tiles[l.first_tile + t].first].base);
       for (int j = 0; j < l.n; ++j) total += plan.entries[l.first + j].steps;
-      l.per = (int)std::max<int64_t>(4, (total + workgroups - 1) / workgroups);
+      const bool few = total < 48 * workgroups;
+      const int64_t share = few && l.n > 1 ? 2 * workgroups : workgroups;
+      l.per = (int)std::max<int64_t>(4, (total + share - 1) / share);
       l.workgroups = (int)((total + l.per - 1) / l.per);
-      l.each = l.per < 16 || (stretches > 3 * l.workgroups && total < (p.fp8 ? 128 : 64) * stretches);
+      l.each = few || (stretches > 3 * l.workgroups && total < (p.fp8 ? 128 : 64) * stretches);
       const auto parts = [&](int64_t at, int64_t count) {
         return (int)(l.each ? (count + l.per - 1) / l.per : (at + count - 1) / l.per - at / l.per + 1);
       };
