@@ -439,7 +439,7 @@ typedef struct fsx_pages fsx_pages;
 typedef struct {
   int32_t dtype;          /* FSX_BF16, or FSX_FP8_E4M3 with a scale for every row of a head (stored value = code * scale) */
   int32_t n_layers;       /* 1..1024 */
-  int32_t n_kv_heads;     /* 1..1024 */
+  int32_t n_kv_heads;     /* 1..1024; n_layers * n_kv_heads at most 2^16 (FSX_E_UNSUPPORTED beyond) */
   int32_t head_dim;       /* 64 or 128 (FSX_E_UNSUPPORTED otherwise) */
   int32_t page_rows;      /* 16, 32, 64, 128 or 256 */
   int32_t n_pages;        /* pages of the pool, at least 1; the tensors' rows may pass 2^31 elements */
@@ -476,10 +476,12 @@ int fsx_pages_free(fsx_pages* pages, int32_t n, const int32_t* seqs, void* strea
 int fsx_pages_tables(const fsx_pages* pages, int32_t* len, int32_t* table, int64_t* free_pages);
 /* Packed rows of sequences as in fsx_prompt_attention (row_start, row_len HOST [n]): the row_len[i] rows become the last rows of
  * seqs[i] (none twice), in layers layer .. layer + n_layers - 1.  Element (layer l, row r, head h, channel c) of k_rows is
- * k_rows[l * k_layer + r * k_row + h * k_head + c], 16-byte aligned, strides multiples of 8.
+ * k_rows[l * k_layer + r * k_row + h * k_head + c], 16-byte aligned, strides multiples of 8, not in the pool itself.
  * BF16 pages: a copy, or one rounding (rows_dtype FSX_F32).  FP8 pages: per row and head scale = max(amax / 448, 2^-126) in fp32,
  * amax the row's largest finite magnitude (1 where that is 0), and the codes of fsx_cache_append_rows_quantize with it.
- * FSX_E_INVALID: a sequence has fewer rows, or some of the rows lie in a page that another sequence has too (extend first). */
+ * FSX_E_INVALID: a sequence has fewer rows, or some of the rows lie in a page that another sequence has too (extend first).  Lengths
+ * and sharing are checked in the call, not in the replays of a graph that it is captured in: there the rows become the last ones that
+ * the sequence then has, for which fsx_pages_extend must have made room since its last fork. */
 typedef struct {
   int32_t rows_dtype;  /* FSX_BF16 or FSX_F32 */
   int32_t layer, n_layers;
@@ -493,6 +495,7 @@ int fsx_pages_write(fsx_pages* pages, const fsx_pages_rows* desc, const void* k_
  * key head h / (n_heads / n_kv_heads)) belongs to seqs[i].  A sequence without rows gives 0, and a lse of -infinity.
  *   desc      as in fsx_prompt_attention: n_heads, n_kv_heads and head_dim (equal to the pool's), q_dtype, out_dtype, scale, q_rows
  *             (at least n), q_row, q_head, out_row, out_head; the other fields are not read
+ *   out       DEVICE, rows and heads as q's, n rows; must not overlap q
  *   lse       DEVICE [n][n_heads] fp32, to merge with another part by, or NULL
  *   workspace DEVICE, 16-byte aligned, for the parts of long sequences, at most workspace_bytes of it are used; with less than
  *             fsx_pages_attention_workspace says, the sequences are cut into fewer parts, with none (NULL, 0) into one.  Calls that
@@ -501,7 +504,7 @@ int fsx_pages_write(fsx_pages* pages, const fsx_pages_rows* desc, const void* k_
  * How the work is shared out follows from the lists and lengths at the time of the call; a replay in a graph shares out the lengths
  * that it finds in the same proportions, and reads apart what is no longer shared.
  * Scores, softmax statistics and sums are fp32; a weight goes to the matrix instructions as two bf16 values, the second what the
- * first leaves out (2^-16 of it is lost).  Fp8 rows are decoded exactly, a key's scale is applied to its score, a value's to its
+ * first leaves out (2^-15 of it is lost).  Fp8 rows are decoded exactly, a key's scale is applied to its score, a value's to its
  * weight, in fp32.  Queries in FSX_F32 are rounded to bf16.  A weight is at most 2^8 until the end divides by their sum, so values
  * beyond 2^119 / rows may overflow a sum.  Deterministic: the same arguments, lists and lengths give the same bits. */
 int fsx_pages_attention(fsx_pages* pages, const fsx_prompt_desc* desc, int32_t layer, const void* q, void* out, float* lse,

@@ -273,11 +273,15 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_page_attention(PageAttentionA
               for (int j = 0; j < Tile::VW; ++j) t.v[i / 4][i % 4][j] = 0;
             }
         }
-        const uint4 pb = make_uint4(pack_bf16x2(pr[0], pr[1]), pack_bf16x2(pr[2], pr[3]), pack_bf16x2(pr[4], pr[5]), pack_bf16x2(pr[6], pr[7]));
-        const auto rest = [&](uint32_t two, int i) {
-          return pack_bf16x2(pr[i] - __uint_as_float(two << 16), pr[i + 1] - __uint_as_float(two & 0xFFFF0000u));
+        // The weights as two bf16 values: their upper halves, and what those leave out, rounded (2^-15 of a weight is lost; a second
+        // product costs nothing next to the loads).  The second one is kept above zero where the weight is, by 2^-24 of it: an infinite
+        // value times zero, or a negative rest, would be NaN.
+        const auto upper = [&](int i) { return __builtin_amdgcn_perm(__float_as_uint(pr[i + 1]), __float_as_uint(pr[i]), 0x07060302u); };
+        const auto rest = [&](int i) {
+          const auto left_out = [](float w) { return fmaf(w, 0x1p-24f, w - __uint_as_float(__float_as_uint(w) & 0xFFFF0000u)); };
+          return pack_bf16x2(left_out(pr[i]), left_out(pr[i + 1]));
         };
-        const uint4 pl = make_uint4(rest(pb.x, 0), rest(pb.y, 2), rest(pb.z, 4), rest(pb.w, 6));
+        const uint4 pb = make_uint4(upper(0), upper(2), upper(4), upper(6)), pl = make_uint4(rest(0), rest(2), rest(4), rest(6));
         // values: product c takes channel c of every lane's piece, eight rows of it
 #pragma unroll
         for (int c = 0; c < NC; ++c) {

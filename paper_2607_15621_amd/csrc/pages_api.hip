@@ -20,7 +20,13 @@ struct fsx_pages {
   int32_t* len = nullptr;    // device [max_seqs]
   bool failed = false;       // the device's lists may not be the host's
   explicit fsx_pages(const fsx_pages_cfg& c) : cfg(c), lists(c.n_pages, c.max_seqs, c.max_seq_pages, c.page_rows) {}
-  ~fsx_pages() { (void)hipFree(table); }
+  ~fsx_pages() {
+    // (a handle may be given back while some stream is captured; the free itself is no part of that)
+    hipStreamCaptureMode mode = hipStreamCaptureModeRelaxed;
+    const bool swapped = hipThreadExchangeStreamCaptureMode(&mode) == hipSuccess;
+    (void)hipFree(table);
+    if (swapped) (void)hipThreadExchangeStreamCaptureMode(&mode);
+  }
   PagePool pool() const {
     int shift = 0;
     while (1 << shift < cfg.page_rows) ++shift;
@@ -178,6 +184,7 @@ extern "C" int fsx_pages_create(const fsx_pages_cfg* c, void* stream, fsx_pages*
     if (c->dtype != FSX_BF16 && c->dtype != FSX_FP8_E4M3) return set_error(FSX_E_UNSUPPORTED, "pages must be BF16 or FP8_E4M3");
     if (c->n_layers < 1 || c->n_layers > 1024) return bad("n_layers must be in 1..1024");
     if (c->n_kv_heads < 1 || c->n_kv_heads > 1024) return bad("n_kv_heads must be in 1..1024");
+    if (c->n_layers * c->n_kv_heads > 1 << 16) return set_error(FSX_E_UNSUPPORTED, "n_layers * n_kv_heads beyond 2^16");
     if (c->head_dim != 64 && c->head_dim != 128) return set_error(FSX_E_UNSUPPORTED, "head_dim must be 64 or 128");
     if (c->page_rows < 16 || c->page_rows > 256 || (c->page_rows & (c->page_rows - 1)))
       return bad("page_rows must be 16, 32, 64, 128 or 256");
@@ -189,9 +196,13 @@ extern "C" int fsx_pages_create(const fsx_pages_cfg* c, void* stream, fsx_pages*
     if (!c->k || !c->v || !aligned16(c->k) || !aligned16(c->v)) return bad("k and v must be non-NULL and 16-byte aligned");
     if (c->dtype == FSX_FP8_E4M3 && (!c->k_scale || !c->v_scale || !aligned16(c->k_scale) || !aligned16(c->v_scale)))
       return bad("fp8 pages need k_scale and v_scale, 16-byte aligned");
+    hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
+    hipError_t e = hipStreamIsCapturing((hipStream_t)stream, &status);
+    if (e != hipSuccess) return hip_error("hipStreamIsCapturing", e);
+    if (status != hipStreamCaptureStatusNone) return set_error(FSX_E_UNSUPPORTED, "pages cannot be created inside a captured graph");
     auto* h = new fsx_pages(*c);
     const size_t entries = ((size_t)c->max_seqs * c->max_seq_pages + 63) / 64 * 64, bytes = 4 * (2 * entries + ((size_t)c->max_seqs + 63) / 64 * 64);
-    hipError_t e = hipGetDevice(&h->device);
+    e = hipGetDevice(&h->device);
     if (e == hipSuccess) e = hipMalloc((void**)&h->table, bytes);
     if (e == hipErrorOutOfMemory) {
       (void)hipGetLastError();
@@ -304,6 +315,18 @@ extern "C" int fsx_pages_write(fsx_pages* h, const fsx_pages_rows* d, const void
     if (total == 0) return done();
     if (total > (int64_t)1 << 31) return set_error(FSX_E_UNSUPPORTED, "more than 2^31 rows");
     if (!k_rows || !v_rows || !aligned16(k_rows) || !aligned16(v_rows)) return bad("k_rows and v_rows must be non-NULL and 16-byte aligned");
+    // rows that lie in the pool themselves would be read and written at once
+    const int64_t es = d->rows_dtype == FSX_F32 ? 4 : 2;
+    const int64_t pool = (int64_t)c.n_layers * c.n_pages * c.n_kv_heads * c.page_rows * c.head_dim * (c.dtype == FSX_BF16 ? 2 : 1);
+    const auto meets = [&](const void* rows, int64_t layer, int64_t row, int64_t head) {
+      const __int128 n = (__int128)(d->n_layers - 1) * layer + (__int128)(d->total_rows - 1) * row + (__int128)(c.n_kv_heads - 1) * head + c.head_dim;
+      const __int128 from = (__int128)(uintptr_t)rows, to = from + n * es;
+      for (const void* x : {c.k, c.v})
+        if (from < (__int128)(uintptr_t)x + pool && (__int128)(uintptr_t)x < to) return true;
+      return false;
+    };
+    if (meets(k_rows, d->k_layer, d->k_row, d->k_head) || meets(v_rows, d->v_layer, d->v_row, d->v_head))
+      return bad("k_rows and v_rows must not lie in the pool");
     PageWriteArgs a{};
     a.pool = h->pool();
     a.k = k_rows; a.v = v_rows;

@@ -102,12 +102,12 @@ class Pool:
         return parts[0].to(F64), parts[1].to(F64)
 
 
-def attend(q, k, v, scale, weight=2.0 ** -16):
+def attend(q, k, v, scale, weight=2.0 ** -15):
     """One token's attention in 64 bits: q [heads][channels], k, v [rows][key heads][channels]; output, its tolerance without the
     output's rounding, log sums and theirs.
 
-    With A = sum_j P_j |v_j|: a weight is two bf16 values, each rounded by at most half a step, 2^-8 of it, the second of what the
-    first left, so an output moves by at most 2^-16 A (fsx_prompt_attention rounds them once: `weight` is U there).  A score is a sum of D products in fp32, scaled (an fp8 row's scale among it) by two roundings more: off by at most
+    With A = sum_j P_j |v_j|: a weight is two bf16 values, the first cut off (at most a step, 2^-7, is left), the second what is left
+    rounded by at most half a step, 2^-8 of that, so an output moves by at most 2^-15 A (fsx_prompt_attention rounds them once: `weight` is U there).  A score is a sum of D products in fp32, scaled (an fp8 row's scale among it) by two roundings more: off by at most
     ds = (D + 6) 2^-24 scale sum_c |q_c k_c|, which changes every weight by a factor within exp(+-2 ds); the exponentials are off by
     2^-22, and the statistics, sums and the merges of parts add (rows + 64) roundings of 2^-24."""
     q = q.to(BF16).to(F64)

@@ -130,6 +130,26 @@ def test_infinities_and_nan_that_are_seen():
     assert out[3].isnan().nonzero().tolist() == [[0, 7], [1, 7]]
 
 
+@pytest.mark.parametrize("G", [1, 4, 16])
+@pytest.mark.parametrize("flat", [True, False], ids=["flat", "uneven"])
+def test_infinite_values_reach_their_channel_whatever_their_weight(G, flat):
+    """One value of infinity in each of 48 sequences of 48 rows, at another row and channel, of either sign: that channel is infinite
+    and every other finite (flat: every weight is 1, which bf16 holds without a rest)."""
+    p = Pool(seqs=48, pages=150, most=3, P=16, L=1, H=2)
+    p.extend(list(range(48)), [48] * 48)
+    table, _ = p.pages.tables()
+    for s in range(48):
+        p.v[0, table[s, s // 16], :, s % 16, (5 * s) % 128] = math.inf if s % 2 else -math.inf
+    q = queries(p, 48, 2 * G, amp=0.0 if flat else 1.0)
+    for split in (list(range(48)), [7]):
+        out = run(p, 0, q[:len(split)], split)[0].cpu()
+        for i, s in enumerate(split):
+            want = torch.zeros(128)
+            want[(5 * s) % 128] = math.inf if s % 2 else -math.inf
+            assert not bool(out[i].isnan().any()), s
+            assert torch.equal(torch.where(torch.isinf(out[i].float()), out[i].float(), torch.zeros(())), want.expand(2 * G, 128)), s
+
+
 def test_many_entries_and_less_workspace():
     """More entries than a launch takes, long and short ones mixed; with less workspace the parts are fewer."""
     p = Pool(seqs=5, pages=300, most=200, P=16, L=1, H=1)

@@ -217,6 +217,26 @@ def test_the_device_s_length_counts_in_a_replay():
         p.check()
 
 
+def test_handles_made_and_given_back_while_a_graph_is_captured():
+    p, gone = Pool(seqs=3, pages=20, most=8, L=1), Pool(seqs=3, pages=20, most=8, L=1)
+    p.extend([0], [5])
+    k, v = (t.cuda() for t in p.new(1))
+    p.pages.extend([0], [1])
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        p.pages.write(0, 1, k, v, [0], fsx.PackedRows([1]))
+        with pytest.raises(fsx.FsxError, match="captured"):
+            fsx.Pages(p.k, p.v, 3, 8)
+        gone.pages.close()
+    for _ in range(2):
+        graph.replay()
+    torch.cuda.synchronize()
+    p.rows[0] += p.stored(k.cpu(), v.cpu())
+    p.check()
+
+
 def test_on_another_stream():
     p = Pool(seqs=3, pages=20, most=8)
     side = torch.cuda.Stream()
@@ -292,6 +312,11 @@ def test_refusals():
                 lambda: fsx.Pages(p.k.to(torch.int8), p.v.to(torch.int8), 1, 1), lambda: fsx.Pages(p.k.cpu(), p.v.cpu(), 1, 1)):
         with pytest.raises((ValueError, fsx.FsxError)):
             bad()
+    within = p.k.view(2, -1, 2, 128)[:, 5:25]  # rows of the pool itself
+    with pytest.raises(fsx.FsxError, match="pool"):
+        p.pages.extend([2], [4])
+        write([2], [4], k=within, v=v)
+    p.free([2])
     odd = torch.randn(2, 20, 2, 132).to(BF16).cuda()[..., :128]
     with pytest.raises(fsx.FsxError, match="multiples of 8"):
         write([0], [0], k=odd, v=odd)

@@ -70,8 +70,8 @@ def create(**kw):
 @pytest.mark.parametrize("kw,code,word", [
     (dict(dtype=fsx.F32), UNSUPPORTED, "BF16"), (dict(n_layers=0), INVALID, "n_layers"), (dict(n_layers=1025), INVALID, "n_layers"),
     (dict(n_kv_heads=0), INVALID, "n_kv_heads"), (dict(n_kv_heads=1025), INVALID, "n_kv_heads"), (dict(head_dim=96), UNSUPPORTED, "head_dim"),
-    (dict(page_rows=8), INVALID, "page_rows"), (dict(page_rows=48), INVALID, "page_rows"), (dict(page_rows=512), INVALID, "page_rows"),
-    (dict(n_pages=0), INVALID, "n_pages"), (dict(n_pages=2 ** 31 - 1, n_layers=1024, n_kv_heads=1024), INVALID, "2^48"),
+    (dict(n_layers=1024, n_kv_heads=65), UNSUPPORTED, "2^16"), (dict(page_rows=8), INVALID, "page_rows"), (dict(page_rows=48), INVALID, "page_rows"), (dict(page_rows=512), INVALID, "page_rows"),
+    (dict(n_pages=0), INVALID, "n_pages"), (dict(n_pages=2 ** 31 - 1, n_layers=1024, n_kv_heads=64, page_rows=256), INVALID, "2^48"),
     (dict(max_seqs=0), INVALID, "max_seqs"), (dict(max_seqs=65537), INVALID, "max_seqs"),
     (dict(max_seq_pages=0), INVALID, "max_seq_pages"), (dict(max_seq_pages=(1 << 24) + 1), INVALID, "max_seq_pages"),
     (dict(max_seq_pages=1 << 24, max_seqs=17), INVALID, "max_seq_pages"), (dict(k=0), INVALID, "k and v"), (dict(v=PTR + 8), INVALID, "k and v"),
