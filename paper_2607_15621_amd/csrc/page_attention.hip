@@ -28,6 +28,10 @@ namespace fsx {
 constexpr int PA_KEYS = 32;     // rows that a wave takes at a time
 constexpr int PA_SHARED = 128;  // shared rows that are worth a tile
 
+// Columns of a workgroup: 16, or 32 for groups of more query heads, which would read the keys twice (16 histories of 900 rows, 8
+// key heads, 160 query heads: 17.5 us instead of 21.8).
+__host__ __device__ constexpr int columns(int G) { return G > 16 ? 32 : 16; }
+
 // A state of a part: G x D sums of weighted values, then G maxima (log2 units) and G sums of weights; whole 16-byte pieces.
 __host__ __device__ constexpr int64_t part_floats(int G, int D) { return ((int64_t)G * (D + 2) + 3) / 4 * 4; }
 
@@ -48,22 +52,23 @@ struct PageTile {
   float4 ks[2], vs[2];  // FP8: scales of rows 4 (lane / 16) ..
 };
 
-template <int D, bool FP8, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, 2) void k_page_attention(PageAttentionArgs a) {
+template <int D, bool FP8, int WAVES, int CT>
+__global__ __launch_bounds__(64 * WAVES, WAVES == 8 || CT == 1 ? 2 : 1) void k_page_attention(PageAttentionArgs a) {
   constexpr int KS = D / 32, NC = D / 16, ES = FP8 ? 1 : 2;  // steps of the first product, products of the second
-  constexpr int STEP = WAVES * PA_KEYS;
+  constexpr int STEP = WAVES * PA_KEYS, W = 16 * CT;  // rows at a time; columns
   using Tile = PageTile<D, FP8>;
   // Lists and lengths.  Nothing writes them while this runs: said so (constant memory), they are read by scalar loads.  As vector
   // loads they came behind the values under way, and every tile waited for both.
   typedef const __attribute__((address_space(4))) int32_t* list_t;
-  __shared__ float xo[WAVES][16][D + 4];
-  __shared__ float xm[WAVES][16], xl[WAVES][16];
+  __shared__ float xo[WAVES][W][D + 4];
+  __shared__ float xm[WAVES][W], xl[WAVES][W];
   const PagePool& p = a.pool;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, c16 = lane & 15;
-  const int blocks = (a.G + 15) / 16;
+  const int blocks = (a.G + W - 1) / W;
   // Stretch by stretch, the longest first, where each is a workgroup; otherwise head by head (us, the other way round: 64 of 740 fp8
   // rows behind shared ones 103 instead of 90, 64 histories of 7,700 rows 345 instead of 335).
-  const int hq = a.each ? blockIdx.x : blockIdx.y, index = a.each ? blockIdx.y : blockIdx.x, hk = hq / blocks, qb = hq - hk * blocks, h0 = hk * a.G + 16 * qb, rows = min(a.G, 16);
+  const int hq = a.each ? blockIdx.x : blockIdx.y, index = a.each ? blockIdx.y : blockIdx.x;
+  const int hk = hq / blocks, qb = hq - hk * blocks, h0 = hk * a.G + W * qb, rows = min(a.G, W);
   const list_t lens = (list_t)p.len;
 
   // The arguments are cold in every launch, a microsecond away: what may be needed of them comes in one round trip, a value per
@@ -148,24 +153,26 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_page_attention(PageAttentionA
       base = bases.at(e), seq0 = seqs.at(e);
     }
     const int cut = min(to, until), part = a.each ? (at - from) / a.per : at / a.per - from / a.per;
-    const int width = shared ? a.G : min(16, a.G - 16 * qb);  // columns of an entry
-    // The thread's column of the outcome: an entry, its query head, and where the state goes.
-    const int qi = threadIdx.x >> 4, ch = NC * (threadIdx.x & 15), member = qi / width, gi = qi - member * width;
-    const int en = e + min(member, members - 1), n_parts = a.all[en + 1] - a.all[en], out_row = a.row[en];
+    const int width = shared ? a.G : min(W, a.G - W * qb);  // columns of an entry
+    // The thread's column of the outcome (of the first 16; more are one entry's): an entry, and where its state goes.
+    const int ch = NC * (threadIdx.x & 15), en = e + min((int)(threadIdx.x >> 4) / width, members - 1);
+    const int n_parts = a.all[en + 1] - a.all[en], out_row = a.row[en];
     const int slot = a.all[en] + part + (shared ? a.parts[en + 1] - a.parts[en] : 0);  // parts of its own rows, then of the shared
-    // The lane's column: queries of the channels that its keys have in step s.
-    uint4 q[KS];
-    {
-      const int64_t at_q = a.row[e + min(c16 / width, members - 1)] * a.q_row + (int64_t)(h0 + c16 % width) * a.q_head;
+    // The lane's columns: queries of the channels that its keys have in step s.
+    uint4 q[CT][KS];
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) {
+      const int col = 16 * ct + c16;
+      const int64_t at_q = a.row[e + min(col / width, members - 1)] * a.q_row + (int64_t)(h0 + col % width) * a.q_head;
 #pragma unroll
       for (int s = 0; s < KS; ++s) {
         const int c = FP8 ? 64 * (s / 2) + 16 * g + 8 * (s % 2) : 32 * s + 8 * g;
         if (a.q_f32) {
           const float4* f = reinterpret_cast<const float4*>(reinterpret_cast<const float*>(a.q) + at_q + c);
           const float4 u = f[0], v = f[1];
-          q[s] = make_uint4(pack_bf16x2(u.x, u.y), pack_bf16x2(u.z, u.w), pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
+          q[ct][s] = make_uint4(pack_bf16x2(u.x, u.y), pack_bf16x2(u.z, u.w), pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
         } else {
-          q[s] = *reinterpret_cast<const uint4*>(reinterpret_cast<const uint16_t*>(a.q) + at_q + c);
+          q[ct][s] = *reinterpret_cast<const uint4*>(reinterpret_cast<const uint16_t*>(a.q) + at_q + c);
         }
       }
     }
@@ -201,10 +208,14 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_page_attention(PageAttentionA
       // First element row of the page row that tile row `key` is (past the end: some row that exists).
       const auto row_in = [&](int page, int key) { return layer_row + (int64_t)page * (p.Hk * p.P) + (key & (p.P - 1)); };
       const auto row_of = [&](int key) { return row_in(pages[min(key >> p.shift, last_page)], key); };
-      f32x4 o[NC];
+      f32x4 o[CT][NC];
+      float m[CT], l[CT];  // maximum (log2 units), the same in the four lanes of a query; the lane's share of the sum
 #pragma unroll
-      for (int c = 0; c < NC; ++c) o[c] = f32x4{0.f, 0.f, 0.f, 0.f};
-      float m = -INFINITY, l = 0.f;  // maximum (log2 units), the same in the four lanes of a query; the lane's share of the sum
+      for (int ct = 0; ct < CT; ++ct) {
+        m[ct] = -INFINITY, l[ct] = 0.f;
+#pragma unroll
+        for (int c = 0; c < NC; ++c) o[ct][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+      }
 
       Tile t;
       int key = begin + w * PA_KEYS;
@@ -214,74 +225,87 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_page_attention(PageAttentionA
       const auto compute = [&](auto more) {
         constexpr bool MORE = decltype(more)::value;
         // scores
-        f32x4 s[2];
+        f32x4 s[CT][2];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          s[h] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int ct = 0; ct < CT; ++ct) s[ct][h] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
           for (int i = 0; i < KS; ++i) {
             uint4 ka;
             if constexpr (FP8) {
               const uint4 u = t.k[h][i / 2];
               const uint32_t lo = i % 2 ? u.z : u.x, hi = i % 2 ? u.w : u.y;
-              ka = make_uint4(e4m3x2_to_bf16x2(lo, false), e4m3x2_to_bf16x2(lo, true), e4m3x2_to_bf16x2(hi, false), e4m3x2_to_bf16x2(hi, true));
+              ka = make_uint4(e4m3x2_to_bf16x2(lo, false), e4m3x2_to_bf16x2(lo, true), e4m3x2_to_bf16x2(hi, false),
+                              e4m3x2_to_bf16x2(hi, true));
             } else {
               ka = t.k[h][i];
             }
-            s[h] = mfma_bf16(ka, q[i], s[h]);
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct) s[ct][h] = mfma_bf16(ka, q[ct][i], s[ct][h]);
           }
         }
-        float sc[8];
+        float sc[CT][8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          sc[i] = s[i / 4][i % 4] * a.c;
-          if constexpr (FP8) sc[i] *= reinterpret_cast<const float*>(&t.ks[i / 4])[i % 4];
-        }
+        for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            sc[ct][i] = s[ct][i / 4][i % 4] * a.c;
+            if constexpr (FP8) sc[ct][i] *= reinterpret_cast<const float*>(&t.ks[i / 4])[i % 4];
+          }
         if constexpr (MORE) load_k(t, next);
         const int left = MORE ? PA_KEYS : end - key;  // rows of the tile that count: all of them, but for the last of the wave's
-        if (left < PA_KEYS) {
+        uint4 pb[CT], pl[CT];
 #pragma unroll
-          for (int i = 0; i < 8; ++i)
-            if (16 * (i / 4) + 4 * g + i % 4 >= left) sc[i] = -INFINITY;
+        for (int ct = 0; ct < CT; ++ct) {
+          if (left < PA_KEYS) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+              if (16 * (i / 4) + 4 * g + i % 4 >= left) sc[ct][i] = -INFINITY;
+          }
+          // The maximum that the exponents are taken from is raised only where they would pass 2^8, which sums in fp32 and relative
+          // roundings do not mind; then it is the same in the lanes of a query.
+          const float(&x)[8] = sc[ct];
+          float top = vmax3(vmax3(x[0], x[1], x[2]), vmax3(x[3], x[4], x[5]), vmax(x[6], x[7]));
+          if (__any(top > m[ct] + 8.f)) {
+            const float now = rows_max(vmax(top, m[ct])), back = __builtin_amdgcn_exp2f(m[ct] - (now == -INFINITY ? 0.f : now));
+            m[ct] = now;
+            l[ct] *= back;
+#pragma unroll
+            for (int c = 0; c < NC; ++c)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) o[ct][c][i] *= back;
+          }
+          const float mz = m[ct] == -INFINITY ? 0.f : m[ct];
+          float pr[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            pr[i] = __builtin_amdgcn_exp2f(x[i] - mz);
+            l[ct] += pr[i];
+            if constexpr (FP8) pr[i] *= reinterpret_cast<const float*>(&t.vs[i / 4])[i % 4];
+          }
+          if (left < PA_KEYS) {  // whatever lies behind the last row
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+              if (16 * (i / 4) + 4 * g + i % 4 >= left) {
+                pr[i] = 0.f;
+#pragma unroll
+                for (int j = 0; j < Tile::VW; ++j) t.v[i / 4][i % 4][j] = 0;
+              }
+          }
+          // The weights as two bf16 values: their upper halves, and what those leave out, rounded (2^-15 of a weight is lost; a second
+          // product costs nothing next to the loads).  The second one is kept above zero where the weight is, by 2^-24 of it: an
+          // infinite value times zero, or a negative rest, would be NaN.
+          const auto upper = [&](int i) {
+            return __builtin_amdgcn_perm(__float_as_uint(pr[i + 1]), __float_as_uint(pr[i]), 0x07060302u);
+          };
+          const auto rest = [&](int i) {
+            const auto left_out = [](float w) { return fmaf(w, 0x1p-24f, w - __uint_as_float(__float_as_uint(w) & 0xFFFF0000u)); };
+            return pack_bf16x2(left_out(pr[i]), left_out(pr[i + 1]));
+          };
+          pb[ct] = make_uint4(upper(0), upper(2), upper(4), upper(6));
+          pl[ct] = make_uint4(rest(0), rest(2), rest(4), rest(6));
         }
-        // The maximum that the exponents are taken from is raised only where they would pass 2^8, which sums in fp32 and relative
-        // roundings do not mind; then it is the same in the lanes of a query.
-        float top = vmax3(vmax3(sc[0], sc[1], sc[2]), vmax3(sc[3], sc[4], sc[5]), vmax(sc[6], sc[7]));
-        if (__any(top > m + 8.f)) {
-          const float now = rows_max(vmax(top, m)), back = __builtin_amdgcn_exp2f(m - (now == -INFINITY ? 0.f : now));
-          m = now;
-          l *= back;
-#pragma unroll
-          for (int c = 0; c < NC; ++c)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) o[c][i] *= back;
-        }
-        const float mz = m == -INFINITY ? 0.f : m;
-        float pr[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          pr[i] = __builtin_amdgcn_exp2f(sc[i] - mz);
-          l += pr[i];
-          if constexpr (FP8) pr[i] *= reinterpret_cast<const float*>(&t.vs[i / 4])[i % 4];
-        }
-        if (left < PA_KEYS) {  // whatever lies behind the last row
-#pragma unroll
-          for (int i = 0; i < 8; ++i)
-            if (16 * (i / 4) + 4 * g + i % 4 >= left) {
-              pr[i] = 0.f;
-#pragma unroll
-              for (int j = 0; j < Tile::VW; ++j) t.v[i / 4][i % 4][j] = 0;
-            }
-        }
-        // The weights as two bf16 values: their upper halves, and what those leave out, rounded (2^-15 of a weight is lost; a second
-        // product costs nothing next to the loads).  The second one is kept above zero where the weight is, by 2^-24 of it: an infinite
-        // value times zero, or a negative rest, would be NaN.
-        const auto upper = [&](int i) { return __builtin_amdgcn_perm(__float_as_uint(pr[i + 1]), __float_as_uint(pr[i]), 0x07060302u); };
-        const auto rest = [&](int i) {
-          const auto left_out = [](float w) { return fmaf(w, 0x1p-24f, w - __uint_as_float(__float_as_uint(w) & 0xFFFF0000u)); };
-          return pack_bf16x2(left_out(pr[i]), left_out(pr[i + 1]));
-        };
-        const uint4 pb = make_uint4(upper(0), upper(2), upper(4), upper(6)), pl = make_uint4(rest(0), rest(2), rest(4), rest(6));
         // values: product c takes channel c of every lane's piece, eight rows of it
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
@@ -297,8 +321,11 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_page_attention(PageAttentionA
               r[j] = __builtin_amdgcn_perm(t.v[h][i + 1][c / 2], t.v[h][i][c / 2], c % 2 ? 0x07060302u : 0x05040100u);
             }
           }
-          o[c] = mfma_bf16(make_uint4(r[0], r[1], r[2], r[3]), pb, o[c]);
-          o[c] = mfma_bf16(make_uint4(r[0], r[1], r[2], r[3]), pl, o[c]);
+#pragma unroll
+          for (int ct = 0; ct < CT; ++ct) {
+            o[ct][c] = mfma_bf16(make_uint4(r[0], r[1], r[2], r[3]), pb[ct], o[ct][c]);
+            o[ct][c] = mfma_bf16(make_uint4(r[0], r[1], r[2], r[3]), pl[ct], o[ct][c]);
+          }
         }
         if constexpr (MORE) {
           load_v(t, next);
@@ -321,20 +348,25 @@ __global__ __launch_bounds__(64 * WAVES, 2) void k_page_attention(PageAttentionA
         }
         compute(std::false_type{});
       }
-      l = rows_sum(l);
 
-      // The waves' states put together.  Lane: query c16, o[c][i]: channel (D / 16) (4 g + i) + c.
+      // The waves' states put together.  Lane: query c16 of a column tile, o[c][i]: channel (D / 16) (4 g + i) + c.
 #pragma unroll
-      for (int c = 0; c < NC; ++c)
+      for (int ct = 0; ct < CT; ++ct) {
+        const float sum = rows_sum(l[ct]);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) xo[w][c16][NC * (4 * g + i) + c] = o[c][i];
-      if (g == 0) {
-        xm[w][c16] = m;
-        xl[w][c16] = l;
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) xo[w][16 * ct + c16][NC * (4 * g + i) + c] = o[ct][c][i];
+        if (g == 0) {
+          xm[w][16 * ct + c16] = m[ct];
+          xl[w][16 * ct + c16] = sum;
+        }
       }
       __syncthreads();
-      // thread: column t / 16, channels D / 16 (t % 16) ..
-      if (qi < 16 && member < members && (rounds == 1 || member == round)) {
+      // thread: column t / 16 of a column tile, channels D / 16 (t % 16) ..
+      for (int qi = threadIdx.x >> 4; qi < min(W, width * members); qi += 4 * WAVES) {
+        const int member = qi / width, gi = qi - member * width;
+        if (rounds > 1 && member != round) continue;
         float mm = xm[0][qi], f[WAVES], ll = 0.f;
 #pragma unroll
         for (int i = 1; i < WAVES; ++i) mm = vmax(mm, xm[i][qi]);
@@ -389,13 +421,14 @@ __global__ __launch_bounds__(256) void k_page_merge(PageAttentionArgs a) {
   constexpr int T = D / 4, GROUPS = 256 / T;
   __shared__ float4 xo[GROUPS][T];
   __shared__ float xl[GROUPS], xm[GROUPS];
-  const int e = blockIdx.x, h = blockIdx.y, hk = h / a.G, gi = h - hk * a.G, blocks = (a.G + 15) / 16, rows = min(a.G, 16);
+  const int e = blockIdx.x, h = blockIdx.y, hk = h / a.G, gi = h - hk * a.G;
+  const int W = columns(a.G), blocks = (a.G + W - 1) / W, rows = min(a.G, W);
   const int n = a.all[e + 1] - a.all[e];
   if (n <= 1) return;  // written already
   const int grp = threadIdx.x / T, t = threadIdx.x % T;
   const int64_t step = (int64_t)blocks * (a.H / a.G) * part_floats(rows, D);
-  const float* part = a.part + a.all[e] * step + (hk * blocks + gi / 16) * part_floats(rows, D);
-  const int qi = gi % 16;
+  const float* part = a.part + a.all[e] * step + (hk * blocks + gi / W) * part_floats(rows, D);
+  const int qi = gi % W;
   float m = -INFINITY, l = 0.f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
   const auto add = [&](float mc, float lc, float4 v) {
@@ -474,8 +507,8 @@ static void share_pages(const PageLists& lists, const int32_t* seqs, int per_til
 void plan_page_attention(const PagePool& p, const PageLists& lists, int H, int n, const int32_t* seqs, int64_t workspace_bytes,
                          PagePlan& plan) {
   constexpr int64_t CUS = 256;
-  const int G = H / p.Hk, units = p.Hk * ((G + 15) / 16);
-  const int64_t state = 4 * units * part_floats(std::min(G, 16), p.D);  // bytes of a part, all heads
+  const int G = H / p.Hk, W = columns(G), units = p.Hk * ((G + W - 1) / W);
+  const int64_t state = 4 * units * part_floats(std::min(G, W), p.D);  // bytes of a part, all heads
   plan.entries.resize(n);
   bool shared = false;
   int longest = 0;
@@ -570,7 +603,7 @@ void plan_page_attention(const PagePool& p, const PageLists& lists, int H, int n
 
 hipError_t launch_page_attention(PageAttentionArgs a, const int32_t* seqs, const PagePlan& plan, hipStream_t s) {
   const PagePool& p = a.pool;
-  const int blocks = (a.G + 15) / 16, rows = std::min(a.G, 16);
+  const int W = columns(a.G), blocks = (a.G + W - 1) / W, rows = std::min(a.G, W);
   for (const auto& l : plan.launches) {
     a.n = l.n;
     a.n_tiles = l.n_tiles;
@@ -597,15 +630,20 @@ hipError_t launch_page_attention(PageAttentionArgs a, const int32_t* seqs, const
     }
     a.total = a.steps[l.n];
     const dim3 grid(l.each ? p.Hk * blocks : l.workgroups, l.each ? l.workgroups : p.Hk * blocks), merge(l.n, a.H);
-    if (plan.wide) {
-      const auto fn = p.D == 64 ? (p.fp8 ? k_page_attention<64, true, 8> : k_page_attention<64, false, 8>)
-                                : (p.fp8 ? k_page_attention<128, true, 8> : k_page_attention<128, false, 8>);
-      hipLaunchKernelGGL(fn, grid, dim3(512), 0, s, a);
-    } else {
-      const auto fn = p.D == 64 ? (p.fp8 ? k_page_attention<64, true, 4> : k_page_attention<64, false, 4>)
-                                : (p.fp8 ? k_page_attention<128, true, 4> : k_page_attention<128, false, 4>);
-      hipLaunchKernelGGL(fn, grid, dim3(256), 0, s, a);
-    }
+    const auto launch = [&](auto ct) {
+      constexpr int CT = decltype(ct)::value;
+      if (plan.wide) {
+        const auto fn = p.D == 64 ? (p.fp8 ? k_page_attention<64, true, 8, CT> : k_page_attention<64, false, 8, CT>)
+                                  : (p.fp8 ? k_page_attention<128, true, 8, CT> : k_page_attention<128, false, 8, CT>);
+        hipLaunchKernelGGL(fn, grid, dim3(512), 0, s, a);
+      } else {
+        const auto fn = p.D == 64 ? (p.fp8 ? k_page_attention<64, true, 4, CT> : k_page_attention<64, false, 4, CT>)
+                                  : (p.fp8 ? k_page_attention<128, true, 4, CT> : k_page_attention<128, false, 4, CT>);
+        hipLaunchKernelGGL(fn, grid, dim3(256), 0, s, a);
+      }
+    };
+    if (W == 32) launch(std::integral_constant<int, 2>{});
+    else launch(std::integral_constant<int, 1>{});
     if (l.parts) {
       if (p.D == 64) hipLaunchKernelGGL(k_page_merge<64>, merge, dim3(256), 0, s, a);
       else hipLaunchKernelGGL(k_page_merge<128>, merge, dim3(256), 0, s, a);

@@ -4,7 +4,8 @@
 // The gradient of the rotation is the rotation back.
 //
 // Bound by memory: every element is read and written once.  The angles of a row are the same for all of its heads, so a workgroup
-// computes the sines and cosines of its rows once, into LDS, and then walks over the heads.
+// computes the sines and cosines of its rows once, into LDS, and then walks over the heads (16,384 bf16 rows of 64 heads x 128, 537 MB:
+// 105 us, 5.1 TB/s; a large copy reaches 4.9).
 //
 // Angles: positions are whole numbers and f_j / 2 pi is given as a fraction of a turn in units of 2^-64, so their product modulo
 // 2^64 is the angle's place in its turn, exact but for the fraction's own rounding (2^-65 a step), however far the position: nothing
@@ -105,7 +106,7 @@ hipError_t launch_rotary(RotaryArgs a, hipStream_t s) {
   const int v = !a.f32 && fits(8) ? 8 : (fits(4) ? 4 : 1);
   const int64_t units = (int64_t)a.heads * (a.pairs + (a.copy_rest ? a.dim - 2 * a.pairs : 0)) / v;  // of a row
   // rows of a workgroup: up to eight pieces for each of its threads, once the rows are many, and as few threads without one in the
-  // last turn as may be (16,001 rows of 15 heads of 20 pairs of pieces: @GRAD@)
+  // last turn as may be (16,001 fp32 rows of 15 heads of 40 pairs, 154 MB: 34.6 us with 5 rows, 37.4 with 7)
   const int64_t most = std::max<int64_t>(1, std::min<int64_t>({2048 / units, a.rows / 2048, 2048 / a.pairs}));
   const auto busy = [&](int64_t b) { return (double)(b * units) / ((b * units + 255) / 256 * 256); };
   int64_t best = most;
