@@ -549,7 +549,7 @@ void plan_page_attention(const PagePool& p, const PageLists& lists, int H, int n
   // of 60,000 and 63 of 10 (32 over 32) 350 and 238.  So too where a share is short, with two workgroups for each CU if there are
   // several sequences: 16 of 301 to 1,051 15.3 instead of 17.4, 16 of 1,500 fp8 rows 16.8 instead of 19.3, five of 300 to 5,000 15.2
   // instead of 17.4.  Otherwise more workgroups than CUs cost: 16 of 4,100 56 instead of 55, one of 100,003 77 instead of 75.
-  const auto cut = [&](int64_t workgroups) {
+  const auto cut = [&](int64_t workgroups, bool apart) {
     int64_t most = 0;
     for (auto& l : plan.launches) {
       int64_t total = 0, stretches = l.n_tiles + l.n;
@@ -559,7 +559,7 @@ void plan_page_attention(const PagePool& p, const PageLists& lists, int H, int n
       const int64_t share = few && l.n > 1 ? 2 * workgroups : workgroups;
       l.per = (int)std::max<int64_t>(4, (total + share - 1) / share);
       l.workgroups = (int)((total + l.per - 1) / l.per);
-      l.each = few || (stretches > 3 * l.workgroups && total < (p.fp8 ? 128 : 64) * stretches);
+      l.each = apart || few || (stretches > 3 * l.workgroups && total < (p.fp8 ? 128 : 64) * stretches);
       const auto parts = [&](int64_t at, int64_t count) {
         return (int)(l.each ? (count + l.per - 1) / l.per : (at + count - 1) / l.per - at / l.per + 1);
       };
@@ -587,7 +587,8 @@ void plan_page_attention(const PagePool& p, const PageLists& lists, int H, int n
     plan.bytes = most * state;
   };
   int64_t w = std::max<int64_t>(1, CUS / units);
-  for (cut(w); plan.bytes > workspace_bytes && w > 1;) cut(w /= 2);
+  // With less workspace, longer parts, but none of several sequences: at the least a workgroup for each.
+  for (cut(w, false); plan.bytes > workspace_bytes && w > 1;) cut(w /= 2, true);
   if (plan.bytes > workspace_bytes) {
     plan.tiles.clear();
     for (auto& x : plan.entries) x.base = 0;

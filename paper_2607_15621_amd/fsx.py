@@ -496,7 +496,8 @@ def rotary_rows(x, out, positions, plan: RotaryPlan, inverse: bool = False, stre
     sx, tx, ty = x.shape, x.stride(), out.stride()
     if len(sx) != 3 or out.shape != sx or out.dtype != x.dtype or tx[2] != 1 or ty[2] != 1:
         raise ValueError("x and out must be [rows][heads][channels] of one dtype, with a dense last dimension")
-    if positions.dim() != 2 or positions.shape[1] != sx[0] or positions.element_size() != 4 or positions.is_floating_point():
+    if positions.dim() != 2 or positions.shape[1] != sx[0] or positions.element_size() != 4 or \
+            positions.is_floating_point() or not positions.dtype.is_signed:
         raise ValueError("positions must be int32 [axes][rows]")
     tp = positions.stride()
     d = RotaryDesc(_dtype_of(x), sx[1], sx[2], len(plan.axis), plan.layout, positions.shape[0], int(inverse), plan.c_axis, plan.c_freq,
