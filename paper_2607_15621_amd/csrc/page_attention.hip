@@ -17,6 +17,7 @@
 // With fewer than 16 query heads the other columns are idle; the products take a small part of the loads' time all the same.
 
 #include <algorithm>
+#include <cstring>
 #include <numeric>
 #include <type_traits>
 
@@ -485,7 +486,8 @@ static void share_pages(const PageLists& lists, const int32_t* seqs, int per_til
       for (size_t j = i; j < e; ++j) {
         const int most = std::min(whole(es[i]), whole(es[j]));
         const int32_t *u = list(es[i]), *v = list(es[j]);
-        int n = 0;
+        int n = u == v ? most : 0;
+        while (n + 64 <= most && !memcmp(u + n, v + n, 64 * sizeof(int32_t))) n += 64;
         while (n < most && u[n] == v[n]) ++n;
         es[j].base = n;
       }

@@ -57,6 +57,23 @@ def test_groups(fp8, D, G):
     check_attention(p, 0, q, out, lse, [1, 0, 2])
 
 
+@kinds
+@pytest.mark.parametrize("G", [1, 4, 16, 17, 33])
+def test_short_sequences(fp8, D, G):
+    """All of at most 512 rows: one launch, without parts or a workspace."""
+    lens = [0, 1, 31, 255, 256, 257, 300, 511, 512]
+    p = Pool(seqs=9, pages=160, most=32, P=16, D=D, fp8=fp8, L=1, H=2)
+    p.extend(list(range(9)), lens)
+    seqs = [8, 3, 0, 5, 1, 7, 2, 6, 4, 8]
+    q = queries(p, 10, 2 * G)
+    assert p.pages.attention_workspace(q, seqs) == 0
+    out, lse = run(p, 0, q, seqs)
+    check_attention(p, 0, q, out, lse, seqs)
+    p.fork([8], [0])  # (forks of which little is shared, and those that share nothing, alike)
+    out, lse = run(p, 0, q, seqs)
+    check_attention(p, 0, q, out, lse, seqs)
+
+
 @pytest.mark.parametrize("fp8", [False, True], ids=["bf16", "fp8"])
 def test_types_strides_and_scale(fp8):
     p = Pool(seqs=4, pages=80, most=60, P=32, fp8=fp8, L=1, H=2)
