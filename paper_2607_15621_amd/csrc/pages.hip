@@ -245,42 +245,54 @@ template <int PDT, int CDT>
 __global__ __launch_bounds__(256) void k_page_write(PageWriteArgs a) {
   const PagePool& p = a.pool;
   const int lane = threadIdx.x & 63, l = blockIdx.y, kv = blockIdx.z, blk = blockIdx.x;
-  int s = 0;
-#pragma unroll
-  for (int i = 0; i < PAGE_WRITES; i += 64) s += __popcll(__ballot(i + lane < a.n && a.block_prefix[i + lane + 1] <= blk));
-  const int r0 = (blk - a.block_prefix[s]) * a.block, nr = min(a.block, a.rows[s] - r0), seq = a.seq[s];
-  const int first = p.len[seq] - a.rows[s] + r0;  // row of the sequence
+  // the entry, its arguments in one round trip, a value per lane
+  static_assert(PAGE_WRITES == 128, "two entries for each lane");
+  const int prefix[2] = {a.block_prefix[lane + 1], a.block_prefix[64 + lane + 1]}, seqs[2] = {a.seq[lane], a.seq[64 + lane]};
+  const int counts[2] = {a.rows[lane], a.rows[64 + lane]};
+  const int64_t starts[2] = {a.start[lane], a.start[64 + lane]};
+  const int s = __popcll(__ballot(lane < a.n && prefix[0] <= blk)) + __popcll(__ballot(64 + lane < a.n && prefix[1] <= blk));
+  const auto of = [&](const int (&v)[2], int i) {
+    return i < 64 ? __builtin_amdgcn_readlane(v[0], i) : __builtin_amdgcn_readlane(v[1], i - 64);
+  };
+  const int low[2] = {(int)starts[0], (int)starts[1]}, high[2] = {(int)(starts[0] >> 32), (int)(starts[1] >> 32)};
+  const int64_t start = (int64_t)of(high, s) << 32 | (uint32_t)of(low, s);
+  const int seq = of(seqs, s), count = of(counts, s), r0 = (blk - (s ? of(prefix, s - 1) : 0)) * a.block, nr = min(a.block, count - r0);
+  const int first = p.len[seq] - count + r0;  // row of the sequence
   const int32_t* pages = p.table + (int64_t)seq * p.most;
   const char* rows = (const char*)(kv ? a.v : a.k);
   const int64_t row_step = kv ? a.v_row : a.k_row, head_step = kv ? a.v_head : a.k_head;
-  const int64_t packed = l * (kv ? a.v_layer : a.k_layer) + (a.start[s] + r0) * row_step;
+  const int64_t packed = l * (kv ? a.v_layer : a.k_layer) + (start + r0) * row_step;
+  const int64_t layer_row = (int64_t)(a.layer + l) * p.pages * p.Hk * p.P;
   char* cache = (char*)(kv ? p.v : p.k);
   float* scales = kv ? p.v_scale : p.k_scale;
-  constexpr int E = CDT == FSX_BF16 ? 8 : 16;  // elements of 16 bytes
-  const int cpr = p.D / E, total = nr * p.Hk * cpr;
-  for (int e0 = threadIdx.x; e0 < total; e0 += 4 * 256) {
-    RawRows<PDT, E> in[4];
-    int64_t at[4];
+  constexpr int E = CDT == FSX_BF16 ? 8 : 16, U = 4;  // elements of 16 bytes; pieces under way
+  // The thread's piece of a head's row, and its (row, head), which moves on by `heads` of them at a time.
+  const int cpr = p.D / E, c = threadIdx.x & (cpr - 1), heads = 256 / cpr, dr = heads / p.Hk, dh = heads - dr * p.Hk;
+  int r = (int)threadIdx.x / cpr / p.Hk, h = (int)threadIdx.x / cpr - r * p.Hk;
+  while (r < nr) {
+    RawRows<PDT, E> in[U];
+    int64_t at[U];
+    bool valid[U];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      // (past the end: the last row again, by whole rows)
-      const int e = e0 + 256 * u < total ? e0 + 256 * u : total - cpr + e0 % cpr;
-      const int c = e % cpr, i = e / cpr, r = i / p.Hk, h = i - r * p.Hk, row = max(first + r, 0);
-      in[u] = load_rows<PDT, E>(rows, packed + r * row_step + h * head_step + E * c);
-      at[u] = page_row(p, a.layer + l, pages[row >> p.shift], h, row & (p.P - 1));
+    for (int u = 0; u < U; ++u) {
+      const int i = min(r, nr - 1), row = max(first + i, 0);
+      in[u] = load_rows<PDT, E>(rows, packed + i * row_step + h * head_step + E * c);
+      at[u] = layer_row + (int64_t)pages[row >> p.shift] * (p.Hk * p.P) + h * p.P + (row & (p.P - 1));
+      valid[u] = r < nr && first + i >= 0;
+      r += dr, h += dh;
+      if (h >= p.Hk) h -= p.Hk, ++r;
     }
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const int e = e0 + 256 * u, c = e % cpr;
-      const bool valid = e < total && first + (e / cpr) / p.Hk >= 0;
+    for (int u = 0; u < U; ++u) {
       if constexpr (CDT == FSX_BF16) {
-        if (valid) *reinterpret_cast<uint4*>((uint16_t*)cache + at[u] * p.D + E * c) = to_bf16(in[u]);
+        if (valid[u]) *reinterpret_cast<uint4*>((uint16_t*)cache + at[u] * p.D + E * c) = to_bf16(in[u]);
       } else {
         uint32_t t = 0;
 #pragma unroll
         for (int i = 0; i < Raw16<PDT>::N; ++i) t = fold_top<PDT>(t, in[u].p[i], false);
         float top = top_value<PDT>(t);
-        if (!(top < INFINITY)) {
+        const bool finite = top < INFINITY;
+        if (!finite) {
           t = 0;
 #pragma unroll
           for (int i = 0; i < Raw16<PDT>::N; ++i) t = fold_top<PDT>(t, in[u].p[i], true);
@@ -293,11 +305,13 @@ __global__ __launch_bounds__(256) void k_page_write(PageWriteArgs a) {
         top = fmaxf(top, other(top, std::integral_constant<int, 0xB1>{}));
         top = fmaxf(top, other(top, std::integral_constant<int, 0x4E>{}));
         if (cpr == 8) top = fmaxf(top, other(top, std::integral_constant<int, 0x141>{}));
-        const float scale = scale_of(top, 1.f);
-        const auto out = convert<PDT, CDT>(in[u], scale);
-        if (valid) {
+        const Scale scale(scale_of(top, 1.f));
+        float x[16];
+        to_floats<PDT>(in[u], x);
+        const auto out = __all(finite && !scale.tiny) ? from_floats<CDT, true>(x, scale) : from_floats<CDT>(x, scale);
+        if (valid[u]) {
           store_raw<CDT>(cache, at[u] * p.D + 16 * c, out);
-          if (c == 0) scales[at[u]] = scale;
+          if (c == 0) scales[at[u]] = scale.s;
         }
       }
     }
@@ -308,9 +322,10 @@ hipError_t launch_page_write(PageWriteArgs a, int n, const int32_t* seqs, const 
   const PagePool& p = a.pool;
   int64_t total = 0;
   for (int i = 0; i < n; ++i) total += rows[i];
-  // rows of a workgroup: four pieces for every thread, once there are workgroups enough
+  // rows of a workgroup: four pieces for every thread, once there are two workgroups for each CU (15,000 uneven rows of 4 heads x 64
+  // into fp8 pages: 10 us, with eight for each 15)
   const int64_t full = std::max<int64_t>(1, 4 * 256 / (p.Hk * (p.D / (p.fp8 ? 16 : 8))));
-  a.block = (int)std::max<int64_t>({1, std::min<int64_t>(full, total * a.n_layers * 2 / 2048), (total >> 23) + 1});
+  a.block = (int)std::max<int64_t>({1, std::min<int64_t>(full, total * a.n_layers * 2 / 512), (total >> 23) + 1});
   for (int i = 0; i < n;) {
     a.n = 0;
     a.block_prefix[0] = 0;
