@@ -351,8 +351,8 @@ struct PageAttentionArgs {
   int32_t H, G, layer, q_f32, o_f32;
   float c;               // scores in log2 units = c * q.k
   int32_t n, n_tiles;
-  // Steps of 32 rows: those of the tiles, `tiled` of them, then those of the entries; workgroups take `per` of them each, or (each)
-  // workgroups take one tile's or entry's stretch between multiples of `per`, the tiles' tiled_parts of them first.
+  // Steps of 32 rows, and some for each stretch's start: those of the tiles, `tiled` of them, then those of the entries.  A workgroup
+  // takes `per` of them, whatever they belong to, or (each) at most `per` of one tile or entry, the tiles' tiled_parts stretches first.
   int32_t per, each, tiled, total, tiled_parts;
   int32_t seq[PAGE_QUERIES], base[PAGE_QUERIES];
   uint16_t row[PAGE_QUERIES];
@@ -372,7 +372,7 @@ struct PagePlan {
     int32_t first, members;
   };
   struct Launch {
-    int32_t first, n, first_tile, n_tiles, per, each, workgroups, parts;
+    int32_t first, n, first_tile, n_tiles, per, each, extra, workgroups, parts;  // extra: steps added to every stretch
   };
   std::vector<Entry> entries;
   std::vector<Tile> tiles;

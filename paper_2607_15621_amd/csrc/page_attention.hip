@@ -27,6 +27,9 @@
 namespace fsx {
 
 constexpr int PA_KEYS = 32;     // rows that a wave takes at a time
+// Steps that a stretch's start and end are worth, where a workgroup takes one after the other: as part of its length, in even shares (64
+// sequences of 1 to 7,300 rows, 24 heads over 8, 66.6 us without and 52 with it; 2 and 4: 63 and 58, 10: 52).
+constexpr int PA_START = 8;
 constexpr int PA_SHARED = 128;  // shared rows that are worth a tile
 
 // Columns of a workgroup: 16, or 32 for groups of more query heads, which would read the keys twice (16 histories of 900 rows, 8
@@ -182,10 +185,12 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 || CT == 1 ? 2 : 1) void k_p
     const int first_key = (shared ? 0 : base) + (at - from + w) * PA_KEYS;
     const int guess0 = min(first_key >> p.shift, p.most - 1), guess1 = min((first_key + 16) >> p.shift, p.most - 1);
     const int page0 = pages[guess0], page1 = pages[guess1], len0 = lens[seq0];
-    // Its steps as planned are at - from .. cut - from of to - from; of the rows that are found (in a captured graph not those that
-    // were planned) it takes the same share.
+    // Its steps as planned, its start among them, are at - from .. cut - from of to - from; of the rows that are found (in a captured
+    // graph not those that were planned) it takes the same share.
     const int total = shared ? base : max(len0 - base, 0), found = (total + PA_KEYS - 1) / PA_KEYS;
-    const auto share = [&](int step) { return found == to - from ? step : (int)((int64_t)step * found / (to - from)); };
+    const auto share = [&](int step) {
+      return step == 0 || found == to - from ? step : (step == to - from ? found : (int)((int64_t)step * found / (to - from)));
+    };
     const int begin = (shared ? 0 : base) + share(at - from) * PA_KEYS;
     const int stop = min(begin + (share(cut - from) - share(at - from)) * PA_KEYS, (shared ? 0 : base) + total);
 
@@ -550,14 +555,14 @@ void plan_page_attention(const PagePool& p, const PageLists& lists, int H, int n
     const int tiles = (int)plan.tiles.size();
     while (end < tiles && plan.tiles[end].first + plan.tiles[end].members <= i + m) ++end;
     if (end < tiles && plan.tiles[end].first < i + m) m = plan.tiles[end].first - i;
-    plan.launches.push_back({i, m, tile, end - tile, 1, 1, m, 0});
+    plan.launches.push_back({i, m, tile, end - tile, 1, 1, 0, m, 0});
     i += m;
     tile = end;
   }
   const auto whole = [&] {  // a workgroup for each entry and key head
     plan.bytes = 0;
     for (auto& x : plan.entries) x.own = 1, x.shared = 0;
-    for (auto& l : plan.launches) l.per = 1 << 30, l.each = 1, l.workgroups = l.n, l.parts = 0;
+    for (auto& l : plan.launches) l.per = 1 << 30, l.each = 1, l.extra = 0, l.workgroups = l.n, l.parts = 0;
   };
   if (plan.wide) return whole();
   // As many steps for every workgroup, at least four (one for each wave), so that all of them run at once and end together; a
@@ -574,10 +579,12 @@ void plan_page_attention(const PagePool& p, const PageLists& lists, int H, int n
       for (int t = 0; t < l.n_tiles; ++t) total += steps(plan.entries[plan.tiles[l.first_tile + t].first].base);
       for (int j = 0; j < l.n; ++j) total += plan.entries[l.first + j].steps;
       const bool few = total < 48 * workgroups;
+      l.each = apart || few || (stretches > 3 * workgroups && total < (p.fp8 ? 128 : 64) * stretches);
+      l.extra = l.each ? 0 : PA_START;
+      total += stretches * l.extra;
       const int64_t share = few && l.n > 1 ? 2 * workgroups : workgroups;
       l.per = (int)std::max<int64_t>(4, (total + share - 1) / share);
       l.workgroups = (int)((total + l.per - 1) / l.per);
-      l.each = apart || few || (stretches > 3 * l.workgroups && total < (p.fp8 ? 128 : 64) * stretches);
       const auto parts = [&](int64_t at, int64_t count) {
         return (int)(l.each ? (count + l.per - 1) / l.per : (at + count - 1) / l.per - at / l.per + 1);
       };
@@ -585,18 +592,18 @@ void plan_page_attention(const PagePool& p, const PageLists& lists, int H, int n
       stretches = l.parts = 0;
       for (int t = 0; t < l.n_tiles; ++t) {
         const auto& x = plan.tiles[l.first_tile + t];
-        const int count = steps(plan.entries[x.first].base), m = parts(at, count);
+        const int count = steps(plan.entries[x.first].base) + l.extra, m = parts(at, count);
         for (int j = 0; j < x.members; ++j) plan.entries[x.first + j].shared = m;
         stretches += m;
         at += count;
       }
       for (int j = 0; j < l.n; ++j) {
         auto& x = plan.entries[l.first + j];
-        x.own = parts(at, x.steps);
+        x.own = parts(at, x.steps + l.extra);
         stretches += x.own;
         l.parts += x.own + x.shared;
         split += x.own + x.shared > 1;
-        at += x.steps;
+        at += x.steps + l.extra;
       }
       if (l.each) l.workgroups = (int)stretches;
       if (!split) l.parts = 0;
@@ -633,7 +640,7 @@ hipError_t launch_page_attention(PageAttentionArgs a, const int32_t* seqs, const
       const PagePlan::Tile& x = plan.tiles[l.first_tile + t];
       a.tile[t] = (uint8_t)(x.first - l.first);
       a.members[t] = (uint8_t)x.members;
-      a.tile_steps[t + 1] = a.tile_steps[t] + (plan.entries[x.first].base + PA_KEYS - 1) / PA_KEYS;
+      a.tile_steps[t + 1] = a.tile_steps[t] + (plan.entries[x.first].base + PA_KEYS - 1) / PA_KEYS + l.extra;
       a.tile_parts[t + 1] = a.tile_parts[t] + plan.entries[x.first].shared;
     }
     a.steps[0] = a.tiled = a.tile_steps[l.n_tiles];
@@ -644,7 +651,7 @@ hipError_t launch_page_attention(PageAttentionArgs a, const int32_t* seqs, const
       a.seq[j] = seqs[x.index];
       a.row[j] = (uint16_t)x.index;
       a.base[j] = x.base;
-      a.steps[j + 1] = a.steps[j] + x.steps;
+      a.steps[j + 1] = a.steps[j] + x.steps + l.extra;
       a.parts[j + 1] = a.parts[j] + x.own;
       a.all[j + 1] = a.all[j] + x.own + x.shared;
       most = std::max(most, x.own + x.shared);

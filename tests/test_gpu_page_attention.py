@@ -277,6 +277,62 @@ def test_pages_that_are_no_longer_shared_in_a_replay(fp8):
         check_attention(p, 0, q, out, lse, seqs)
 
 
+@kinds
+@pytest.mark.parametrize("G", [1, 3, 20])
+@pytest.mark.parametrize("seqs", [[3, 2, 0, 9, 1, 10, 5, 4], [3, 2, 0, 9, 1, 10, 5, 4, 8, 6, 7, 0]], ids=["shares", "stretches"])
+def test_many_heads_and_rows(fp8, D, G, seqs):
+    """Workgroups whose rows begin in one sequence and end in another (few sequences), and workgroups of a sequence each (many), over
+    shared pages too; eager, and replayed while the sequences grow, shrink and part."""
+    Hk, P, lens = 64, 32, [3000, 1, 2500, 40, 0, 1500, 700, 33, 129, 0, 0]
+    n = sum(-(-x // P) for x in lens) + 120
+    shape = (1, n, Hk, P, D)
+    if fp8:
+        k, v = (torch.randint(0, 127, shape, dtype=torch.uint8, device="cuda") for _ in "kv")
+        k += (torch.randint(0, 2, shape, dtype=torch.uint8, device="cuda") << 7)
+        ks, vs = (torch.rand(shape[:4], device="cuda") * 0.01 + 0.001 for _ in "kv")
+    else:
+        k, v = (torch.randn(shape, device="cuda").to(BF16) for _ in "kv")
+        ks = vs = None
+    pages = fsx.Pages(k, v, 11, 120, ks, vs)
+    pages.extend(list(range(11)), lens)
+    pages.fork([2, 2], [9, 10], [2000, 2500])
+    pages.extend([9, 10], [77, 1])
+    q = torch.randn(len(seqs), Hk * G, D, device="cuda").to(BF16)
+    out, lse = torch.empty_like(q), torch.empty(q.shape[:2], device="cuda")
+    ws = torch.empty(pages.attention_workspace(q, seqs), dtype=torch.uint8, device="cuda")
+
+    def call():
+        pages.attention(0, q, out, seqs, lse=lse, workspace=ws)
+
+    def check(what):
+        torch.cuda.synchronize()
+        table, length = pages.tables()
+        heads = [0, 17, 63]
+        host = [t[0][:, heads].cpu() for t in (k, v)]
+        if fp8:
+            host = [t.view(torch.float8_e4m3fn).to(F64) * x[0][:, heads].cpu().to(F64)[..., None] for t, x in zip(host, (ks, vs))]
+        cols = [h * G + j for h in heads for j in range(G)]
+        for i, s in enumerate(seqs):
+            m = -(-int(length[s]) // P)
+            kv = [t[table[s, :m]].to(F64).transpose(1, 2).reshape(m * P, 3, D)[:length[s]] for t in host]
+            o, tol, z, ztol = attend(q[i, cols].cpu(), *kv, D ** -0.5)
+            near(out[i, cols].cpu().to(F64), o, tol + U * (o.abs() + tol), f"{what}: entry {i} sequence {s}")
+            near(lse[i, cols].cpu().to(F64), z, ztol, f"{what}: log sums of entry {i} sequence {s}")
+
+    call()
+    check("eager")
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(graph, stream=side):
+        call()
+    for what, change in (("as captured", lambda: None), ("grown", lambda: pages.extend([0, 4, 1], [700, 300, 1])),
+                         ("shrunk", lambda: pages.keep([0, 10], [[(0, 900)], [(0, 64), (100, 1000)]])), ("freed", lambda: pages.free([2, 5]))):
+        change()
+        out.fill_(9)
+        graph.replay()
+        check(what)
+
+
 def test_two_streams_at_once():
     p = Pool(seqs=2, pages=200, most=100, P=16, L=1, H=2)
     p.extend([0, 1], [1500, 1400])
