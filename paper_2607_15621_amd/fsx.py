@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import sys
 from typing import List, Optional, Sequence
 
 import numpy as np
@@ -380,12 +381,11 @@ def _stream_on(stream, *tensors) -> int:
             device = at
     if device is None:
         return _stream(stream)
-    import torch
-
-    if device != torch.cuda.current_device():
+    C = sys.modules["torch"]._C
+    if device != C._cuda_getDevice():
         raise ValueError("tensors must be on the current device")
-    # (the handle alone: a Stream object costs 2 us, a sixth of a small call)
-    return _stream(stream) if stream is not None else torch._C._cuda_getCurrentRawStream(device)
+    # (the handle alone: a Stream object costs 2 us, a quarter of a small call)
+    return _stream(stream) if stream is not None else C._cuda_getCurrentRawStream(device)
 
 
 def _prompt_desc(q, k, v, out, scale: float, kernel: int) -> PromptDesc:
@@ -502,13 +502,19 @@ def rotary_rows(x, out, positions, plan: RotaryPlan, inverse: bool = False, stre
     tp = positions.stride()
     d = RotaryDesc(_dtype_of(x), sx[1], sx[2], len(plan.axis), plan.layout, positions.shape[0], int(inverse), plan.c_axis, plan.c_freq,
                    tx[0], tx[1], ty[0], ty[1], tp[0], tp[1])
-    _check(lib().fsx_rotary_rows(ctypes.byref(d), _ptr(x), _ptr(out), _ptr(positions), sx[0], _stream_on(stream, x, out, positions)))
+    _check(lib().fsx_rotary_rows(ctypes.byref(d), x.data_ptr(), out.data_ptr(), positions.data_ptr(), sx[0],
+                                 _stream_on(stream, x, out, positions)))
 
 
 def _int32s(values, what: str):
     """A dense int32 array and its address."""
     a = values
-    if not (type(a) is np.ndarray and a.dtype == np.int32 and a.ndim == 1 and a.flags.c_contiguous):
+    if type(a) is list or type(a) is tuple:
+        try:
+            a = np.array(a, np.int32).reshape(-1)
+        except OverflowError:
+            raise ValueError(f"{what} outside 32 bits") from None
+    elif not (type(a) is np.ndarray and a.dtype == np.int32 and a.ndim == 1 and a.flags.c_contiguous):
         a = np.array(values, dtype=np.int64).reshape(-1)
         if a.size and (a.min() < -2 ** 31 or a.max() >= 2 ** 31):
             raise ValueError(f"{what} outside 32 bits")
