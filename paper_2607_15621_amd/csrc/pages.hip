@@ -219,7 +219,7 @@ hipError_t launch_page_move(const PagePool& pool, const int32_t* to_table, int32
 // ---------------------------------------------------------------------------------------------------------------
 // Packed rows into the last rows of their sequences.  A workgroup takes a.block rows of one sequence in one layer, keys or values,
 // and all heads; a thread 16 bytes of a cached row at a time.  The threads of an fp8 row (4 or 8) find its scale by exchange, so each
-// element is read once.  16 prompts of 1,024 rows into fp8 pages, 32 heads, 407 MB: 86 us, 4.7 TB/s (a large copy: 4.9).
+// element is read once.  16 prompts of 1,024 rows into fp8 pages, 32 heads, 407 MB: 87 us, 4.7 TB/s (a large copy: 4.9).
 template <int PDT>
 struct Raw8 {
   uint4 p[PDT == FSX_F32 ? 2 : 1];
