@@ -11,6 +11,7 @@ from __future__ import annotations
 import ctypes
 import os
 import sys
+from array import array
 from typing import List, Optional, Sequence
 
 import numpy as np
@@ -511,10 +512,12 @@ def _int32s(values, what: str):
     a = values
     if type(a) is list or type(a) is tuple:
         try:
-            a = np.array(a, np.int32).reshape(-1)
+            a = np.frombuffer(array("i", a), np.int32)  # (np.array wraps what arrays in a list hold)
         except OverflowError:
             raise ValueError(f"{what} outside 32 bits") from None
-    elif not (type(a) is np.ndarray and a.dtype == np.int32 and a.ndim == 1 and a.flags.c_contiguous):
+        except TypeError:  # lists in lists, floats
+            pass
+    if not (type(a) is np.ndarray and a.dtype == np.int32 and a.ndim == 1 and a.flags.c_contiguous):
         a = np.array(values, dtype=np.int64).reshape(-1)
         if a.size and (a.min() < -2 ** 31 or a.max() >= 2 ** 31):
             raise ValueError(f"{what} outside 32 bits")

@@ -96,3 +96,19 @@ def test_nulls():
     assert L.fsx_pages_attention_workspace(None, None, 1, one, ctypes.byref(need)) == INVALID and need.value == 0
     assert L.fsx_pages_attention_workspace(None, None, 1, one, None) == INVALID
     L.fsx_pages_destroy(None)
+
+
+@pytest.mark.parametrize("values", [
+    [1 << 32], (-(1 << 31) - 1,), [np.int64((1 << 32) + 1)], [np.array((1 << 32) + 1)], [np.array([1 << 31])], np.array([1 << 32]), [3e9],
+    range(1 << 33, (1 << 33) + 2),
+])
+def test_numbers_outside_32_bits(values):
+    for a in ([(values[0], 1)], [(0, values[0])]):
+        with pytest.raises(ValueError, match="outside 32 bits"):
+            fsx.RowRanges([a])
+
+
+@pytest.mark.parametrize("values", [[0, (1 << 31) - 1], (np.int64(5), 7), np.array([3, 4], np.int64), [np.array(9), 2], range(2)])
+def test_numbers_of_32_bits(values):
+    r = fsx.RowRanges([[(x, x) for x in values]])
+    assert r.first.dtype == np.int32 and r.first.tolist() == r.count.tolist() == [int(x) for x in values] and r.counts.tolist() == [len(values)]
