@@ -506,7 +506,9 @@ int fsx_pages_write(fsx_pages* pages, const fsx_pages_rows* desc, const void* k_
  * Scores, softmax statistics and sums are fp32; a weight goes to the matrix instructions as two bf16 values, the second what the
  * first leaves out (2^-15 of it is lost).  Fp8 rows are decoded exactly, a key's scale is applied to its score, a value's to its
  * weight, in fp32.  Queries in FSX_F32 are rounded to bf16.  A weight is at most 2^8 until the end divides by their sum, so values
- * beyond 2^119 / rows may overflow a sum.  Deterministic: the same arguments, lists and lengths give the same bits. */
+ * beyond 2^119 / rows may overflow a sum.  An infinite value makes its channel infinite where its weight is at least 2^-118 of the
+ * largest; a weight far below that is zero in fp32, and the channel NaN.  Deterministic: the same arguments, lists and lengths give the
+ * same bits. */
 int fsx_pages_attention(fsx_pages* pages, const fsx_prompt_desc* desc, int32_t layer, const void* q, void* out, float* lse,
                         int32_t n, const int32_t* seqs, void* workspace, int64_t workspace_bytes, void* stream);
 /* The most workspace the call would use now (0: none). */

@@ -301,12 +301,17 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 || CT == 1 ? 2 : 1) void k_p
           }
           // The weights as two bf16 values: their upper halves, and what those leave out, rounded (2^-15 of a weight is lost; a second
           // product costs nothing next to the loads).  The second one is kept above zero where the weight is, by 2^-24 of it: an
-          // infinite value times zero, or a negative rest, would be NaN.
+          // infinite value times zero, or a negative rest, would be NaN.  Of weights below 2^-109 that is no bf16 value any more: the
+          // rest is then the least there is, 2^-133.  (Fp8 values are finite or NaN.)
           const auto upper = [&](int i) {
             return __builtin_amdgcn_perm(__float_as_uint(pr[i + 1]), __float_as_uint(pr[i]), 0x07060302u);
           };
           const auto rest = [&](int i) {
-            const auto left_out = [](float w) { return fmaf(w, 0x1p-24f, w - __uint_as_float(__float_as_uint(w) & 0xFFFF0000u)); };
+            const auto left_out = [](float w) {
+              const float x = fmaf(w, 0x1p-24f, w - __uint_as_float(__float_as_uint(w) & 0xFFFF0000u));
+              if constexpr (FP8) return x;
+              else return vmax(x, fminf(w, 0x1p-133f));
+            };
             return pack_bf16x2(left_out(pr[i]), left_out(pr[i + 1]));
           };
           pb[ct] = make_uint4(upper(0), upper(2), upper(4), upper(6));
