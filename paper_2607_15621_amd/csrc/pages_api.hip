@@ -8,6 +8,7 @@
 #include <vector>
 
 #include "kernels.h"
+#include "turns.h"
 
 using namespace fsx;
 
@@ -167,8 +168,7 @@ extern "C" int fsx_rotary_rows(const fsx_rotary_desc* d, const void* x, void* y,
     a.f32 = d->dtype == FSX_F32; a.adjacent = d->layout == FSX_ROTARY_ADJACENT; a.inverse = d->inverse;
     a.copy_rest = x != y && 2 * d->n_pairs < d->head_dim;
     for (int j = 0; j < d->n_pairs; ++j) {
-      // turns per step in units of 2^-64, modulo a turn (a long double holds 64 bits; the product is below 2^82)
-      a.turn[j] = (uint64_t)(__int128)(d->freq[j] * (0x1p64L / 6.283185307179586476925286766559L));
+      a.turn[j] = turn_per_step(d->freq[j]);
       a.axis[j] = (uint8_t)d->axis[j];
     }
     const hipError_t e = launch_rotary(a, (hipStream_t)stream);

@@ -7,10 +7,11 @@
 // computes the sines and cosines of its rows once, into LDS, and then walks over the heads (16,384 bf16 rows of 64 heads x 128, 537 MB:
 // 105 us, 5.1 TB/s; a large copy reaches 4.9).
 //
-// Angles: positions are whole numbers and f_j / 2 pi is given as a fraction of a turn in units of 2^-64, so their product modulo
-// 2^64 is the angle's place in its turn, exact but for the fraction's own rounding (2^-65 a step), however far the position: nothing
-// has to be reduced.  The angle is then within an eighth of a turn of a quarter, where Taylor polynomials are off by less than 2e-9
-// (sine to x^9, cosine to x^10); with the roundings on the way a sine or cosine is off by at most 2^-22.
+// Angles: positions are whole numbers and f_j / 2 pi is given as a fraction of a turn in units of 2^-64 (turns.h), so their product
+// modulo 2^64 is the angle's place in its turn, exact but for the fraction's own rounding (2^-65 a step, 2^-34 at position 2^31),
+// however far the position: nothing has to be reduced.  The angle is then within an eighth of a turn of a quarter, where Taylor
+// polynomials are off by less than 2e-9 (sine to x^9, cosine to x^10); with the roundings on the way a sine or cosine is off by at
+// most 2^-22.
 
 #include <algorithm>
 
