@@ -1508,8 +1508,7 @@ hipError_t launch_fill_zero(void* p, size_t bytes, hipStream_t s) {
   const int64_t n16 = (int64_t)(bytes / 16);
   if (n16 == 0) return hipSuccess;
   const int64_t blocks = std::min<int64_t>((n16 + 255) / 256, 2048);
-  hipLaunchKernelGGL(k_fill_zero, dim3((unsigned)blocks), dim3(256), 0, s, (uint4*)p, n16);
-  return hipGetLastError();
+  return enqueue(k_fill_zero, dim3((unsigned)blocks), dim3(256), s, (uint4*)p, n16);
 }
 
 }  // namespace fsx

@@ -16,6 +16,16 @@ namespace fsx {
 // Sets the calling thread's message of fsx_last_error ("" clears it) and returns code.
 int set_error(int code, const std::string& msg);
 
+// Enqueues a kernel and returns the launch's own status: hipGetLastError would take an error that other code of the thread met and
+// left there for one of this launch.
+template <class... P, class... A>
+hipError_t enqueue(void (*kernel)(P...), dim3 grid, dim3 block, hipStream_t s, const A&... a) {
+  return [&](const P&... p) {
+    void* args[] = {const_cast<void*>(static_cast<const void*>(&p))...};
+    return hipLaunchKernel(reinterpret_cast<const void*>(kernel), grid, block, args, 0, s);
+  }(a...);
+}
+
 // Per-forward description of the agents, passed by value in kernel arguments.
 struct TickParams {
   int32_t B, S, T, M;                         // agents, tokens per agent, pooled tokens, rows = B*S

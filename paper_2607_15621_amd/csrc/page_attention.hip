@@ -668,23 +668,23 @@ hipError_t launch_page_attention(PageAttentionArgs a, const int32_t* seqs, const
       if (plan.wide) {
         const auto fn = p.D == 64 ? (p.fp8 ? k_page_attention<64, true, 8, CT> : k_page_attention<64, false, 8, CT>)
                                   : (p.fp8 ? k_page_attention<128, true, 8, CT> : k_page_attention<128, false, 8, CT>);
-        hipLaunchKernelGGL(fn, grid, dim3(512), 0, s, a);
+        return enqueue(fn, grid, dim3(512), s, a);
       } else {
         const auto fn = p.D == 64 ? (p.fp8 ? k_page_attention<64, true, 4, CT> : k_page_attention<64, false, 4, CT>)
                                   : (p.fp8 ? k_page_attention<128, true, 4, CT> : k_page_attention<128, false, 4, CT>);
-        hipLaunchKernelGGL(fn, grid, dim3(256), 0, s, a);
+        return enqueue(fn, grid, dim3(256), s, a);
       }
     };
-    if (W == 32) launch(std::integral_constant<int, 2>{});
-    else launch(std::integral_constant<int, 1>{});
-    if (l.parts) {
+    hipError_t e = W == 32 ? launch(std::integral_constant<int, 2>{}) : launch(std::integral_constant<int, 1>{});
+    if (e == hipSuccess && l.parts) {
       const auto fn = p.D == 64 ? (most > 32 ? k_page_merge<64, 1024> : k_page_merge<64, 256>)
                                 : (most > 32 ? k_page_merge<128, 1024> : k_page_merge<128, 256>);
-      hipLaunchKernelGGL(fn, merge, dim3(most > 32 ? 1024 : 256), 0, s, a);
+      e = enqueue(fn, merge, dim3(most > 32 ? 1024 : 256), s, a);
     }
+    if (e != hipSuccess) return e;
     a.part += (int64_t)l.parts * p.Hk * blocks * part_floats(rows, p.D);
   }
-  return hipGetLastError();
+  return hipSuccess;
 }
 
 }  // namespace fsx

@@ -78,9 +78,10 @@ hipError_t launch_page_update(const PagePool& pool, int32_t* table, int32_t* len
         a.copies[a.n_copies++] = {copies[c].from, copies[c].rows, 1, {copies[c].to}};
       }
     }
-    hipLaunchKernelGGL(k_page_update, dim3(a.n_runs + 2 * a.n_copies * pool.layers * pool.Hk), dim3(256), 0, s, a);
+    const hipError_t e = enqueue(k_page_update, dim3(a.n_runs + 2 * a.n_copies * pool.layers * pool.Hk), dim3(256), s, a);
+    if (e != hipSuccess) return e;
   }
-  return hipGetLastError();
+  return hipSuccess;
 }
 
 // ---------------------------------------------------------------------------------------------------------------
@@ -211,9 +212,10 @@ hipError_t launch_page_move(const PagePool& pool, const int32_t* to_table, int32
       n_ranges += m.n_ranges;
       a.moves[a.n_moves++] = m;
     }
-    hipLaunchKernelGGL(k_page_move, dim3(2 * pool.layers * pool.Hk * a.split, a.n_moves), dim3(256), 0, s, a);
+    const hipError_t e = enqueue(k_page_move, dim3(2 * pool.layers * pool.Hk * a.split, a.n_moves), dim3(256), s, a);
+    if (e != hipSuccess) return e;
   }
-  return hipGetLastError();
+  return hipSuccess;
 }
 
 // ---------------------------------------------------------------------------------------------------------------
@@ -341,9 +343,10 @@ hipError_t launch_page_write(PageWriteArgs a, int n, const int32_t* seqs, const 
     const dim3 grid(a.block_prefix[a.n], a.n_layers, 2);
     const auto fn = a.rows_f32 ? (p.fp8 ? k_page_write<FSX_F32, FSX_FP8_E4M3> : k_page_write<FSX_F32, FSX_BF16>)
                                : (p.fp8 ? k_page_write<FSX_BF16, FSX_FP8_E4M3> : k_page_write<FSX_BF16, FSX_BF16>);
-    hipLaunchKernelGGL(fn, grid, dim3(256), 0, s, a);
+    const hipError_t e = enqueue(fn, grid, dim3(256), s, a);
+    if (e != hipSuccess) return e;
   }
-  return hipGetLastError();
+  return hipSuccess;
 }
 
 }  // namespace fsx

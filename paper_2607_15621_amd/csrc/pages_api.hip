@@ -40,7 +40,11 @@ namespace {
 
 int bad(const std::string& msg) { return set_error(FSX_E_INVALID, msg); }
 int done() { return set_error(FSX_OK, ""); }
-int hip_error(const char* what, hipError_t e) { return set_error(FSX_E_HIP, std::string(what) + ": " + hipGetErrorString(e)); }
+// (reported here, so it does not stay behind as the thread's last error)
+int hip_error(const char* what, hipError_t e) {
+  (void)hipGetLastError();
+  return set_error(FSX_E_HIP, std::string(what) + ": " + hipGetErrorString(e));
+}
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 // No exception crosses the boundary.

@@ -118,8 +118,7 @@ hipError_t launch_rotary(RotaryArgs a, hipStream_t s) {
   const dim3 grid((unsigned)blocks, (unsigned)std::max<int64_t>(1, std::min<int64_t>((a.block * units + 255) / 256, 2048 / blocks)));
   const auto fn = a.f32 ? (v == 4 ? k_rotary<float, 4> : k_rotary<float, 1>)
                         : (v == 8 ? k_rotary<uint16_t, 8> : (v == 4 ? k_rotary<uint16_t, 4> : k_rotary<uint16_t, 1>));
-  hipLaunchKernelGGL(fn, grid, dim3(256), 0, s, a);
-  return hipGetLastError();
+  return enqueue(fn, grid, dim3(256), s, a);
 }
 
 }  // namespace fsx
