@@ -341,14 +341,31 @@ def cache_append_rows_quantize(cache: CacheDesc, k_rows, v_rows, rows_dtype: int
                                                 n_rows, policy, _stream(stream)))
 
 
+def _whole(values, what: str, bits: int = 64):
+    """A dense array of whole numbers, int64, of its own.  Fractions are refused: cut off, they would name another sequence or row."""
+    a = np.asarray(values).reshape(-1)
+    if a.dtype.kind == "O":  # (Python's numbers beyond 64 bits)
+        if not all(hasattr(x, "__index__") for x in a):
+            raise ValueError(f"{what} must be whole numbers")
+        if any(not -2 ** (bits - 1) <= int(x) < 2 ** (bits - 1) for x in a):
+            raise ValueError(f"{what} outside {bits} bits")
+    elif a.dtype.kind == "f":
+        if not (np.isfinite(a) & (np.trunc(a) == a)).all():
+            raise ValueError(f"{what} must be whole numbers")
+    elif a.dtype.kind not in "iub":
+        raise ValueError(f"{what} must be whole numbers")
+    if a.dtype.kind in "iuf" and a.size and not (-2 ** (bits - 1) <= int(a.min()) and int(a.max()) < 2 ** (bits - 1)):
+        raise ValueError(f"{what} outside {bits} bits")
+    return np.array(a, dtype=np.int64)
+
+
 class PackedRows:
     """Rows of several sequences (or agents) in one tensor: sequence i in rows start[i] .. start[i] + len[i] - 1; without
     starts, one after the other."""
 
     def __init__(self, lengths, starts=None):
-        self.len = np.array(lengths, dtype=np.int64).reshape(-1)
-        self.start = (np.cumsum(self.len) - self.len if starts is None else
-                      np.array(starts, dtype=np.int64).reshape(-1))
+        self.len = _whole(lengths, "lengths")
+        self.start = np.cumsum(self.len) - self.len if starts is None else _whole(starts, "starts")
         if len(self.start) != len(self.len):
             raise ValueError("as many starts as lengths")
         P = ctypes.POINTER(ctypes.c_int64)
@@ -460,7 +477,7 @@ def cache_read_rows(cache: CacheDesc, layer: int, n_layers: int, k_rows, v_rows,
     [n_layers][total][H][Dh], decoded; k_rows or v_rows may be None."""
     dtype, total = _row_tensors(cache, n_layers, k_rows, v_rows, rows)
     if first is not None:
-        first = np.array(first, dtype=np.int64).reshape(-1)
+        first = _whole(first, "first rows")
         if len(first) != rows.n:
             raise ValueError("a first row of every agent of the cache")
     _check(lib().fsx_cache_read_rows(ctypes.byref(cache.c), layer, n_layers,
@@ -474,7 +491,7 @@ class RotaryPlan:
     ROTARY_ADJACENT (pairs (2j, 2j+1))."""
 
     def __init__(self, axis, freq, layout: int = ROTARY_HALVES):
-        self.axis = np.array(axis, dtype=np.int32).reshape(-1)
+        self.axis = _whole(axis, "axes", 32).astype(np.int32)
         self.freq = np.array(freq, dtype=np.float64).reshape(-1)
         if len(self.axis) != len(self.freq):
             raise ValueError("as many axes as frequencies: one of each for every pair")
@@ -486,7 +503,7 @@ class RotaryPlan:
     def sections(cls, pairs: Sequence[int], base: float = 10000.0, joint: bool = True, layout: int = ROTARY_HALVES) -> "RotaryPlan":
         """Axis i gets the next pairs[i] pairs.  joint: one ladder base^(-j / pairs of all axes) over all pairs; else each axis has
         its own, base^(-j / pairs[i])."""
-        pairs = [int(n) for n in pairs]
+        pairs = _whole(pairs, "pairs").tolist()
         steps = np.arange(sum(pairs)) / max(1, sum(pairs)) if joint else np.concatenate([np.arange(n) / max(1, n) for n in pairs])
         return cls(np.repeat(np.arange(len(pairs)), pairs), float(base) ** -steps, layout)
 
@@ -518,10 +535,7 @@ def _int32s(values, what: str):
         except TypeError:  # lists in lists, floats
             pass
     if not (type(a) is np.ndarray and a.dtype == np.int32 and a.ndim == 1 and a.flags.c_contiguous):
-        a = np.array(values, dtype=np.int64).reshape(-1)
-        if a.size and (a.min() < -2 ** 31 or a.max() >= 2 ** 31):
-            raise ValueError(f"{what} outside 32 bits")
-        a = a.astype(np.int32)
+        a = _whole(values, what, 32).astype(np.int32)
     return a, a.ctypes.data
 
 
