@@ -495,7 +495,8 @@ int fsx_pages_write(fsx_pages* pages, const fsx_pages_rows* desc, const void* k_
  * key head h / (n_heads / n_kv_heads)) belongs to seqs[i].  A sequence without rows gives 0, and a lse of -infinity.
  *   desc      as in fsx_prompt_attention: n_heads, n_kv_heads and head_dim (equal to the pool's), q_dtype, out_dtype, scale, q_rows
  *             (at least n), q_row, q_head, out_row, out_head; the other fields are not read
- *   out       DEVICE, rows and heads as q's, n rows; must not overlap q
+ *   out       DEVICE, rows and heads as q's, n rows; out, lse and workspace must not overlap each other, q or the pool (FSX_E_INVALID;
+ *             heads of one between those of the other are no overlap)
  *   lse       DEVICE [n][n_heads] fp32, to merge with another part by, or NULL
  *   workspace DEVICE, 16-byte aligned, for the parts of long sequences, at most workspace_bytes of it are used; with less than
  *             fsx_pages_attention_workspace says, the sequences are cut into fewer parts, with none (NULL, 0) into one.  Calls that

@@ -7,6 +7,7 @@
 #include <string>
 #include <vector>
 
+#include "extents.h"
 #include "kernels.h"
 #include "turns.h"
 
@@ -27,6 +28,13 @@ struct fsx_pages {
     const bool swapped = hipThreadExchangeStreamCaptureMode(&mode) == hipSuccess;
     (void)hipFree(table);
     if (swapped) (void)hipThreadExchangeStreamCaptureMode(&mode);
+  }
+  // The caller's memory: keys, values and, fp8, their scales (otherwise empty, at 0).
+  std::array<Extent, 4> memory() const {
+    const int64_t rows = (int64_t)cfg.n_layers * cfg.n_pages * cfg.n_kv_heads * cfg.page_rows;
+    const bool fp8 = cfg.dtype == FSX_FP8_E4M3;
+    const int64_t bytes = rows * cfg.head_dim * (fp8 ? 1 : 2), scales = fp8 ? 4 * rows : 0;
+    return {block(cfg.k, bytes), block(cfg.v, bytes), block(fp8 ? cfg.k_scale : nullptr, scales), block(fp8 ? cfg.v_scale : nullptr, scales)};
   }
   PagePool pool() const {
     int shift = 0;
@@ -114,13 +122,6 @@ int64_t extent(int64_t rows, int64_t row, int64_t heads, int64_t head, int64_t d
   return (rows - 1) * row + (heads - 1) * head + dim;
 }
 
-// Rows and heads that do not overlap each other, whichever of the two strides is the larger.
-bool apart(int64_t rows, int64_t row, int64_t heads, int64_t head, int64_t dim) {
-  const bool head_major = head > row;
-  const int64_t lo = head_major ? row : head, hi = head_major ? head : row, n_lo = head_major ? rows : heads, n_hi = head_major ? heads : rows;
-  return !((n_lo > 1 && lo < dim) || (n_hi > 1 && hi < (n_lo - 1) * lo + dim));
-}
-
 // What the attention reads of its descriptor.
 int check_attention(const fsx_pages* h, const fsx_prompt_desc* d, int32_t n, const int32_t* seqs) {
   if (!d) return bad("desc is NULL");
@@ -150,7 +151,7 @@ extern "C" int fsx_rotary_rows(const fsx_rotary_desc* d, const void* x, void* y,
     const uintptr_t es = d->dtype == FSX_F32 ? 4 : 2;
     if ((uintptr_t)x % es || (uintptr_t)y % es || (uintptr_t)positions % 4) return bad("x, y and positions must be aligned to their elements");
     const int64_t H = d->n_heads, D = d->head_dim;
-    if (!apart(n_rows, d->y_row, H, d->y_head, D)) return bad("rows and heads of y overlap");
+    if (!apart({0, n_rows, d->y_row, H, d->y_head, D})) return bad("rows and heads of y overlap");
     if (x == y ? (d->x_row != d->y_row && n_rows > 1) || (d->x_head != d->y_head && H > 1) : false)
       return bad("x and y in the same place must have the same strides");
     if (x != y) {
@@ -365,10 +366,25 @@ extern "C" int fsx_pages_attention(fsx_pages* h, const fsx_prompt_desc* d, int32
     if (d->q_rows < n || d->q_rows > (int64_t)1 << 40) return bad("q_rows must be in n..2^40");
     for (const int64_t s : {d->q_row, d->q_head, d->out_row, d->out_head})
       if (s < 0 || s % 8 || s > (int64_t)1 << 40) return bad("strides must be non-negative multiples of 8 elements, at most 2^40");
-    if (!apart(n, d->out_row, d->n_heads, d->out_head, d->head_dim)) return bad("rows and heads of out overlap");
+    if (!apart({0, n, d->out_row, d->n_heads, d->out_head, d->head_dim})) return bad("rows and heads of out overlap");
     if (!q || !out || !aligned16(q) || !aligned16(out)) return bad("q and out must be non-NULL and 16-byte aligned");
     if (workspace_bytes < 0 || (workspace_bytes > 0 && !workspace) || !aligned16(workspace))
       return bad("workspace must be 16-byte aligned, of workspace_bytes >= 0 bytes");
+    // Workgroups end one after the other: what some write must not be what others have still to read, or written by two.
+    const auto rows = [&](const void* p, int32_t dtype, int64_t row, int64_t head) {
+      const int64_t es = dtype == FSX_F32 ? 4 : 2;
+      return Extent{(int64_t)(uintptr_t)p, n, row * es, d->n_heads, head * es, d->head_dim * es};
+    };
+    const Extent writes[] = {rows(out, d->out_dtype, d->out_row, d->out_head), block(lse, (int64_t)4 * n * d->n_heads), block(workspace, workspace_bytes)};
+    const char* names[] = {"out", "lse", "workspace"};
+    for (int i = 0; i < 3; ++i) {
+      if (!(i == 0 || (i == 1 ? lse != nullptr : workspace_bytes > 0))) continue;
+      if (meet(rows(q, d->q_dtype, d->q_row, d->q_head), writes[i])) return bad(std::string(names[i]) + " must not overlap q");
+      for (const Extent& x : h->memory())
+        if (meet(x, writes[i])) return bad(std::string(names[i]) + " must not lie in the pool");
+      for (int j = 0; j < i; ++j)
+        if ((j == 0 || lse) && meet(writes[i], writes[j])) return bad(std::string(names[i]) + " must not overlap " + names[j]);
+    }
     PageAttentionArgs a{};
     a.pool = h->pool();
     a.q = q; a.out = out; a.lse = lse; a.part = (float*)workspace;
