@@ -416,7 +416,7 @@ typedef struct {
   int64_t pos_axis, pos_row;             /* strides of positions in elements: axis a of row r is positions[a * pos_axis + r * pos_row] */
 } fsx_rotary_desc;
 /* Rows 0..n_rows-1 (at most 2^26) of x into y, DEVICE.  y may be x, with the same strides; otherwise they must not overlap (heads of
- * the same rows may: a row's queries and keys beside what was not turned), and no element of y lie twice.
+ * the same rows may: a row's queries and keys beside what was not turned), and no element of y lie twice or be a position.
  *   positions DEVICE int32, of any sign and size.  The angle's place in its turn is exact whatever the position (off by less than
  *             2^-32 turns and the rounding of freq); sine and cosine are fp32, off by at most 2^-22, products and sums fp32,
  *             rounded once to dtype */

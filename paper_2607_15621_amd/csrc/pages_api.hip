@@ -165,6 +165,12 @@ extern "C" int fsx_rotary_rows(const fsx_rotary_desc* d, const void* x, void* y,
         if (!whole || row != d->y_row || row < wx || row < wy || at < wx || at + wy > row) return bad("x and y overlap");
       }
     }
+    // positions that a pair's axis reads (an axis of its own for every pair, at most)
+    const int64_t es8 = (int64_t)es, at = (int64_t)(uintptr_t)positions;
+    const Extent rotated{(int64_t)(uintptr_t)y, n_rows, d->y_row * es8, H, d->y_head * es8, D * es8};
+    for (int j = 0; j < d->n_pairs; ++j)
+      if (j == 0 || d->axis[j] != d->axis[j - 1])
+        if (meet({at + 4 * d->axis[j] * d->pos_axis, n_rows, 4 * d->pos_row, 1, 0, 4}, rotated)) return bad("positions and y overlap");
     RotaryArgs a{};
     a.x = x; a.y = y; a.pos = positions;
     a.x_row = d->x_row; a.x_head = d->x_head; a.y_row = d->y_row; a.y_head = d->y_head;
