@@ -476,7 +476,7 @@ int fsx_pages_free(fsx_pages* pages, int32_t n, const int32_t* seqs, void* strea
 int fsx_pages_tables(const fsx_pages* pages, int32_t* len, int32_t* table, int64_t* free_pages);
 /* Packed rows of sequences as in fsx_prompt_attention (row_start, row_len HOST [n]): the row_len[i] rows become the last rows of
  * seqs[i] (none twice), in layers layer .. layer + n_layers - 1.  Element (layer l, row r, head h, channel c) of k_rows is
- * k_rows[l * k_layer + r * k_row + h * k_head + c], 16-byte aligned, strides multiples of 8, not in the pool itself.
+ * k_rows[l * k_layer + r * k_row + h * k_head + c], 16-byte aligned, strides multiples of 8, not in the pool itself (nor its scales).
  * BF16 pages: a copy, or one rounding (rows_dtype FSX_F32).  FP8 pages: per row and head scale = max(amax / 448, 2^-126) in fp32,
  * amax the row's largest finite magnitude (1 where that is 0), and the codes of fsx_cache_append_rows_quantize with it.
  * FSX_E_INVALID: a sequence has fewer rows, or some of the rows lie in a page that another sequence has too (extend first).  Lengths

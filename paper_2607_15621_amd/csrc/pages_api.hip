@@ -326,14 +326,13 @@ extern "C" int fsx_pages_write(fsx_pages* h, const fsx_pages_rows* d, const void
     if (total == 0) return done();
     if (total > (int64_t)1 << 31) return set_error(FSX_E_UNSUPPORTED, "more than 2^31 rows");
     if (!k_rows || !v_rows || !aligned16(k_rows) || !aligned16(v_rows)) return bad("k_rows and v_rows must be non-NULL and 16-byte aligned");
-    // rows that lie in the pool themselves would be read and written at once
+    // rows that lie in the pool themselves, its scales among it, would be read and written at once
     const int64_t es = d->rows_dtype == FSX_F32 ? 4 : 2;
-    const int64_t pool = (int64_t)c.n_layers * c.n_pages * c.n_kv_heads * c.page_rows * c.head_dim * (c.dtype == FSX_BF16 ? 2 : 1);
     const auto meets = [&](const void* rows, int64_t layer, int64_t row, int64_t head) {
       const __int128 n = (__int128)(d->n_layers - 1) * layer + (__int128)(d->total_rows - 1) * row + (__int128)(c.n_kv_heads - 1) * head + c.head_dim;
       const __int128 from = (__int128)(uintptr_t)rows, to = from + n * es;
-      for (const void* x : {c.k, c.v})
-        if (from < (__int128)(uintptr_t)x + pool && (__int128)(uintptr_t)x < to) return true;
+      for (const Extent& x : h->memory())
+        if (from < x.end() && x.at < to) return true;
       return false;
     };
     if (meets(k_rows, d->k_layer, d->k_row, d->k_head) || meets(v_rows, d->v_layer, d->v_row, d->v_head))
