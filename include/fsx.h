@@ -447,7 +447,7 @@ typedef struct {
   int32_t max_seq_pages;  /* pages of one sequence, max_seq_pages * page_rows at most 2^28; max_seqs * max_seq_pages at most 2^28 */
   void* k;                /* DEVICE [n_layers][n_pages][n_kv_heads][page_rows][head_dim], 16-byte aligned, the caller's; must */
   void* v;                /* outlive the handle.  Rows that no sequence has may hold anything, infinities and NaN included */
-  float* k_scale;         /* FP8 only: DEVICE [n_layers][n_pages][n_kv_heads][page_rows], 16-byte aligned */
+  float* k_scale;         /* FP8 only: DEVICE [n_layers][n_pages][n_kv_heads][page_rows], 16-byte aligned.  None may overlap another */
   float* v_scale;
 } fsx_pages_cfg;
 /* All pages free, all sequences empty.  The lists' device memory is the handle's; `stream` is synchronised. */

@@ -13,6 +13,14 @@
 
 using namespace fsx;
 
+// The caller's memory: keys, values and, fp8, their scales (otherwise empty, at 0).
+static std::array<Extent, 4> pool_memory(const fsx_pages_cfg& cfg) {
+  const int64_t rows = (int64_t)cfg.n_layers * cfg.n_pages * cfg.n_kv_heads * cfg.page_rows;
+  const bool fp8 = cfg.dtype == FSX_FP8_E4M3;
+  const int64_t bytes = rows * cfg.head_dim * (fp8 ? 1 : 2), scales = fp8 ? 4 * rows : 0;
+  return {block(cfg.k, bytes), block(cfg.v, bytes), block(fp8 ? cfg.k_scale : nullptr, scales), block(fp8 ? cfg.v_scale : nullptr, scales)};
+}
+
 struct fsx_pages {
   fsx_pages_cfg cfg{};
   int device = 0;
@@ -29,13 +37,7 @@ struct fsx_pages {
     (void)hipFree(table);
     if (swapped) (void)hipThreadExchangeStreamCaptureMode(&mode);
   }
-  // The caller's memory: keys, values and, fp8, their scales (otherwise empty, at 0).
-  std::array<Extent, 4> memory() const {
-    const int64_t rows = (int64_t)cfg.n_layers * cfg.n_pages * cfg.n_kv_heads * cfg.page_rows;
-    const bool fp8 = cfg.dtype == FSX_FP8_E4M3;
-    const int64_t bytes = rows * cfg.head_dim * (fp8 ? 1 : 2), scales = fp8 ? 4 * rows : 0;
-    return {block(cfg.k, bytes), block(cfg.v, bytes), block(fp8 ? cfg.k_scale : nullptr, scales), block(fp8 ? cfg.v_scale : nullptr, scales)};
-  }
+  std::array<Extent, 4> memory() const { return pool_memory(cfg); }
   PagePool pool() const {
     int shift = 0;
     while (1 << shift < cfg.page_rows) ++shift;
@@ -207,6 +209,11 @@ extern "C" int fsx_pages_create(const fsx_pages_cfg* c, void* stream, fsx_pages*
     if (!c->k || !c->v || !aligned16(c->k) || !aligned16(c->v)) return bad("k and v must be non-NULL and 16-byte aligned");
     if (c->dtype == FSX_FP8_E4M3 && (!c->k_scale || !c->v_scale || !aligned16(c->k_scale) || !aligned16(c->v_scale)))
       return bad("fp8 pages need k_scale and v_scale, 16-byte aligned");
+    // Keys and values are moved by workgroups of their own: in one place, one would read what the other has moved already.
+    const auto memory = pool_memory(*c);
+    for (int i = 0; i < 4; ++i)
+      for (int j = 0; j < i; ++j)
+        if (meet(memory[i], memory[j])) return bad("k, v, k_scale and v_scale must not overlap");
     hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
     hipError_t e = hipStreamIsCapturing((hipStream_t)stream, &status);
     if (e != hipSuccess) return hip_error("hipStreamIsCapturing", e);
