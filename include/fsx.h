@@ -512,7 +512,10 @@ int fsx_pages_write(fsx_pages* pages, const fsx_pages_rows* desc, const void* k_
  * same bits. */
 int fsx_pages_attention(fsx_pages* pages, const fsx_prompt_desc* desc, int32_t layer, const void* q, void* out, float* lse,
                         int32_t n, const int32_t* seqs, void* workspace, int64_t workspace_bytes, void* stream);
-/* The most workspace the call would use now (0: none). */
+/* The most workspace the call would use now (0: none).  It changes with the lengths; for any lengths and sharing of n sequences it is at
+ * most s (2 t w ceil(n / 113) + 3 n) bytes, with G = n_heads / n_kv_heads, c = 16 columns (32 where G > 16), b = n_kv_heads ceil(G / c),
+ * s = 4 b (min(G, c) (head_dim + 2) rounded up to a multiple of 4), w = max(1, 256 / b), t = 16 / G where G <= 8, else 1 (divisions
+ * rounded down). */
 int fsx_pages_attention_workspace(const fsx_pages* pages, const fsx_prompt_desc* desc, int32_t n, const int32_t* seqs,
                                   int64_t* bytes);
 

@@ -366,7 +366,7 @@ struct PageAttentionArgs {
   int32_t per, each, tiled, total, tiled_parts;
   int32_t seq[PAGE_QUERIES], base[PAGE_QUERIES];
   uint16_t row[PAGE_QUERIES];
-  int32_t all[PAGE_QUERIES + 1];                                      // parts of the entries before, shared rows' too
+  int32_t all[PAGE_QUERIES + 1];                                      // parts of the split entries before, shared rows' too
   int32_t steps[PAGE_QUERIES + 1], parts[PAGE_QUERIES + 1];           // steps, and stretches, before the entries' own
   uint8_t tile[PAGE_QUERIES / 2], members[PAGE_QUERIES / 2];          // first entries of the tiles, and how many
   int32_t tile_steps[PAGE_QUERIES / 2 + 1], tile_parts[PAGE_QUERIES / 2 + 1];  // before the tiles
@@ -377,6 +377,7 @@ struct PagePlan {
   struct Entry {
     int32_t index, base;        // row of q; rows that a tile reads
     int32_t steps, own, shared; // steps of the others; parts of them, and of the tile's
+    int states() const { return own + shared > 1 ? own + shared : 0; }  // that are put together
   };
   struct Tile {
     int32_t first, members;

@@ -593,7 +593,7 @@ void plan_page_attention(const PagePool& p, const PageLists& lists, int H, int n
       const auto parts = [&](int64_t at, int64_t count) {
         return (int)(l.each ? (count + l.per - 1) / l.per : (at + count - 1) / l.per - at / l.per + 1);
       };
-      int64_t at = 0, split = 0;
+      int64_t at = 0;
       stretches = l.parts = 0;
       for (int t = 0; t < l.n_tiles; ++t) {
         const auto& x = plan.tiles[l.first_tile + t];
@@ -606,25 +606,37 @@ void plan_page_attention(const PagePool& p, const PageLists& lists, int H, int n
         auto& x = plan.entries[l.first + j];
         x.own = parts(at, x.steps + l.extra);
         stretches += x.own;
-        l.parts += x.own + x.shared;
-        split += x.own + x.shared > 1;
+        l.parts += x.states();
         at += x.steps + l.extra;
       }
       if (l.each) l.workgroups = (int)stretches;
-      if (!split) l.parts = 0;
       most += l.parts;
     }
     plan.bytes = most * state;
   };
-  int64_t w = std::max<int64_t>(1, CUS / units);
-  // With less workspace, longer parts, but none of several sequences: at the least a workgroup for each.
-  for (cut(w, false); plan.bytes > workspace_bytes && w > 1;) cut(w /= 2, true);
-  if (plan.bytes > workspace_bytes) {
+  const int64_t full = std::max<int64_t>(1, CUS / units);
+  // With less workspace than that, even shares of up to a quarter fewer workgroups, then longer parts, but none of several sequences: at
+  // the least a workgroup for each.  us (32 heads over 8 of 128 channels, bf16) with nine tenths of the workspace, and where parts come
+  // apart at once, in half the workgroups: 64 of 501 to 14,928 rows 337 and 374, 16 of 301 to 7,936 56 and 63, one of 100,003 76 and 87.
+  const auto fits = [&](int64_t workgroups, bool apart) {
+    cut(workgroups, apart);
+    return plan.bytes <= workspace_bytes;
+  };
+  bool done = fits(full, false);
+  if (!done && workspace_bytes >= 2 * state) {  // (what is split has two parts at least)
+    for (int64_t w = full - 1; !done && 4 * w >= 3 * full; w -= std::max<int64_t>(1, full / 16)) done = fits(w, false);
+    // fewer by as many as there are parts too many, were all of them the workgroups': never too few, so again until it fits
+    for (int64_t w = std::max<int64_t>(1, 3 * full / 4); !done && w >= 1;) {
+      done = fits(w, true);
+      if (!done) w = std::min(w - 1, (int64_t)((double)w * workspace_bytes / plan.bytes));
+    }
+  }
+  if (!done) {
     plan.tiles.clear();
     for (auto& x : plan.entries) x.base = 0;
     for (auto& l : plan.launches) l.first_tile = l.n_tiles = 0;
     for (auto& x : plan.entries) x.steps = std::max(1, steps(lists.len[seqs[x.index]]));
-    return whole();
+    whole();
   }
   for (const auto& l : plan.launches)
     if (l.each && !l.n_tiles)
@@ -658,7 +670,7 @@ hipError_t launch_page_attention(PageAttentionArgs a, const int32_t* seqs, const
       a.base[j] = x.base;
       a.steps[j + 1] = a.steps[j] + x.steps + l.extra;
       a.parts[j + 1] = a.parts[j] + x.own;
-      a.all[j + 1] = a.all[j] + x.own + x.shared;
+      a.all[j + 1] = a.all[j] + x.states();
       most = std::max(most, x.own + x.shared);
     }
     a.total = a.steps[l.n];
