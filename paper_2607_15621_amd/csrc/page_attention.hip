@@ -5,8 +5,9 @@
 // rows of all sequences, one after the other, are cut into even shares for the workgroups, one for each CU; a workgroup takes one key
 // head (and at most 16 of its query heads), and k_page_merge puts the states of a sequence's parts together.  Pages that several
 // sequences share (forks of one history) are read once for as many of them as the 16 columns of a product hold.
-// 64 histories of 7,700 rows (32 heads over 8, 2.03 GB): 335 us, 6.0 TB/s, which is what a plain read reaches; one of 100,003 rows 76
-// us, 5.4 TB/s, 16 of 4,100 55 us, 4.9 TB/s, of which 5 us are the merge and 3 the way to the first keys (arguments, length, list).
+// 64 histories of 501 to 14,928 rows (2.03 GB; 32 query heads over 8 key heads of 128 channels, bf16, as everywhere below where nothing
+// else is said): 336 us, 6.0 TB/s, which is what a plain read reaches; one of 100,003 rows 76 us, 5.4 TB/s, 16 of 301 to 7,936 55 us, 4.9
+// TB/s, of which 5 us are the merge and 3 the way to the first keys (arguments, length, list).
 //
 // The waves of a workgroup take tiles of 32 rows in turn, each on its own until the end.  Nothing goes through LDS on the way:
 //   S = K Q^T   16x16x32 MFMA, A = 16 rows x 32 channels of keys as loaded (16 bytes of a row per lane), B = the queries; lane l
@@ -28,12 +29,14 @@ namespace fsx {
 
 constexpr int PA_KEYS = 32;     // rows that a wave takes at a time
 // Steps that a stretch's start and end are worth, where a workgroup takes one after the other: as part of its length, in even shares (64
-// sequences of 1 to 7,300 rows, 24 heads over 8, 66.6 us without and 52 with it; 2 and 4: 63 and 58, 10: 52).
+// sequences of 1 to 7,300 rows, as many of one length as of twice that, 24 heads over 8: 58.8 us without and 50.6 with it; 2 and 4: 55.0
+// and 52.9, 10: 50.0).
 constexpr int PA_START = 8;
 constexpr int PA_SHARED = 128;  // shared rows that are worth a tile
 
 // Columns of a workgroup: 16, or 32 for groups of more query heads, which would read the keys twice (16 histories of 900 rows, 8
-// key heads, 160 query heads: 17.5 us instead of 21.8).
+// key heads, 160 query heads: 17.7 us instead of 22.2; a single key head and 20 query heads, little enough to be read twice: 12.4 and
+// 11.5).
 __host__ __device__ constexpr int columns(int G) { return G > 16 ? 32 : 16; }
 
 // A state of a part: G x D sums of weighted values, then G maxima (log2 units) and G sums of weights; whole 16-byte pieces.
@@ -69,8 +72,8 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 || CT == 1 ? 2 : 1) void k_p
   const PagePool& p = a.pool;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, c16 = lane & 15;
   const int blocks = (a.G + W - 1) / W;
-  // Stretch by stretch, the longest first, where each is a workgroup; otherwise head by head (us, the other way round: 64 of 740 fp8
-  // rows behind shared ones 103 instead of 90, 64 histories of 7,700 rows 345 instead of 335).
+  // Stretch by stretch, the longest first, where each is a workgroup; otherwise head by head (us, the other way round: 64 of 17 to 1,466
+  // fp8 rows behind 2,051 shared ones, 32 heads over 32, 100 instead of 82; 64 of 501 to 14,928 and 16 of 301 to 7,936 rows no different).
   const int hq = a.each ? blockIdx.x : blockIdx.y, index = a.each ? blockIdx.y : blockIdx.x;
   const int hk = hq / blocks, qb = hq - hk * blocks, h0 = hk * a.G + W * qb, rows = min(a.G, W);
   const list_t lens = (list_t)p.len;
@@ -162,7 +165,8 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 || CT == 1 ? 2 : 1) void k_p
     const int ch = NC * (threadIdx.x & 15), en = e + min((int)(threadIdx.x >> 4) / width, members - 1);
     const int n_parts = a.all[en + 1] - a.all[en], out_row = a.row[en];
     const int slot = a.all[en] + part + (shared ? a.parts[en + 1] - a.parts[en] : 0);  // parts of its own rows, then of the shared
-    // The lane's columns: queries of the channels that its keys have in step s.
+    // The lane's columns: queries of the channels that its keys have in step s.  Fp32 queries are rounded to bf16 (2^-9 of each), as the
+    // attention over whole prompts rounds them: its scores and these are the same, and bf16 is what the keys were rounded to.
     uint4 q[CT][KS];
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) {
@@ -428,7 +432,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 || CT == 1 ? 2 : 1) void k_p
 
 // The parts of one (entry, query head) put together: groups of D / 4 threads take every GROUPS-th part each, then the first the groups'
 // states.  What counts is the round trips to other XCDs' memory, so where a sequence has many parts there are four times the groups
-// (one of 36,830 rows in 288 parts: 15.9 us in all instead of 20.2).
+// (five sequences, the longest of 36,830 rows in 288 parts, 4 heads over 1: 15.9 us in all instead of 19.1).
 template <int D, int THREADS>
 __global__ __launch_bounds__(THREADS) void k_page_merge(PageAttentionArgs a) {
   constexpr int T = D / 4, GROUPS = THREADS / T, AT_ONCE = 4;
@@ -548,8 +552,8 @@ void plan_page_attention(const PagePool& p, const PageLists& lists, int H, int n
   }
   if (shared && G <= 8 && n > 1) share_pages(lists, seqs, 16 / G, plan);
   // Short sequences that do not fill the chip: no parts, in workgroups of eight waves, and one launch.  us with and without, 32 heads
-  // over 8: one sequence of 300 rows 8.6 and 11.1, of 1,000 14.2 and 10.7, 16 of 500 10.7 and 13.2, of 1,000 15.5 and 17.9; 64 of
-  // 1,000 51 and 50, 200 of 600 108 and 103.
+  // over 8: one sequence of 300 rows 8.5 and 10.6, of 1,000 14.3 and 10.4, 16 of 500 10.9 and 13.5, of 1,000 16.2 and 17.9; 64 of
+  // 1,000 53 and 49, 200 of 600 107 and 95.
   const int64_t all = (int64_t)n * units;
   plan.wide = plan.tiles.empty() && all < 2 * CUS && longest <= (4 * all >= CUS ? 1024 : 512);
   const auto steps = [](int64_t rows) { return (int)((rows + PA_KEYS - 1) / PA_KEYS); };
@@ -572,11 +576,12 @@ void plan_page_attention(const PagePool& p, const PageLists& lists, int H, int n
   if (plan.wide) return whole();
   // As many steps for every workgroup, at least four (one for each wave), so that all of them run at once and end together; a
   // workgroup's steps may begin in one sequence and end in another.  Where those stretches are many and short, their starts and ends
-  // weigh more than an even share: then each is a workgroup of its own.  us, the one and the other: 64 uneven histories of 7,700
-  // rows (32 heads over 8) 336 and 445, 16 of 4,100 55 and 65; 64 of 740 fp8 rows (32 over 32) behind shared ones 144 and 107, one
-  // of 60,000 and 63 of 10 (32 over 32) 350 and 238.  So too where a share is short, with two workgroups for each CU if there are
-  // several sequences: 16 of 301 to 1,051 15.3 instead of 17.4, 16 of 1,500 fp8 rows 16.8 instead of 19.3, five of 300 to 5,000 15.2
-  // instead of 17.4.  Otherwise more workgroups than CUs cost: 16 of 4,100 56 instead of 55, one of 100,003 77 instead of 75.
+  // weigh more than an even share: then each is a workgroup of its own.  us, the one and the other: 64 histories of 501 to 14,928 rows
+  // (32 heads over 8) 338 and 374, 16 of 301 to 7,936 55 and 71; 64 of 17 to 1,466 fp8 rows behind 2,051 shared ones (32 over 32) 109
+  // and 82, one of 60,000 and 63 of 10 (32 over 32) 187 and 171.  So too where a share is short, with two workgroups for each CU if there
+  // are several sequences: 16 of 301 to 1,051 (32 over 8) 15.3 instead of 17.3, 16 of 1,500 fp8 rows 16.3 instead of 19.1, five of 300
+  // to 5,000 15.2 instead of 17.2.  Otherwise more workgroups than CUs cost: 16 of 301 to 7,936 58 instead of 55, one of 100,003 79
+  // instead of 76.
   const auto cut = [&](int64_t workgroups, bool apart) {
     int64_t most = 0;
     for (auto& l : plan.launches) {

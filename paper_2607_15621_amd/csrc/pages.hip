@@ -17,8 +17,8 @@ __device__ __forceinline__ int64_t page_row(const PagePool& p, int layer, int pa
 
 // ---------------------------------------------------------------------------------------------------------------
 // A workgroup for each run of entries, and one for each copied page, layer, head, and keys or values; it reads the page's rows once
-// for up to four copies (16 copies of 43 rows, 32 layers of 8 heads, 96 MB: 18 us, 5.4 TB/s, mostly written; 23 with a read for every
-// copy).
+// for up to four copies (16 copies of 43 bf16 rows, 32 layers of 8 heads of 128 channels, 96 MB: 18 us, 5.4 TB/s, mostly written; 23
+// with a read for every copy).
 __global__ __launch_bounds__(256) void k_page_update(PageUpdateArgs a) {
   const PagePool& p = a.pool;
   if ((int)blockIdx.x < a.n_runs) {
@@ -88,8 +88,8 @@ hipError_t launch_page_update(const PagePool& pool, int32_t* table, int32_t* len
 // Rows that close up, in place where the sequence has its pages alone.  A workgroup takes one head of one layer, keys or values (or
 // some of their channels), of a sequence from its first row that is written to its last: no row moves up, so the rows that a stretch
 // of the outcome overwrites come from that stretch or have been read before.  A stretch is read whole before it is written, and the
-// next one is on its way by then (16 sequences of 1,024 rows, 560 of them moved, 4 layers of 8 heads, 294 MB: 48 us, 6.1 TB/s, some of it from
-// the memory-side cache; 80 with the pages looked up when they are needed, 84 with one stretch at a time).
+// next one is on its way by then (16 sequences of 1,024 bf16 rows, 560 of them moved, 4 layers of 8 heads of 128 channels, 294 MB: 48
+// us, 6.1 TB/s, some of it from the memory-side cache; 80 with the pages looked up when they are needed, 84 with one stretch at a time).
 __global__ __launch_bounds__(256) void k_page_move(PageMoveArgs a) {
   __shared__ PageRange ranges[PAGE_RANGES];
   const PagePool& p = a.pool;
@@ -221,7 +221,8 @@ hipError_t launch_page_move(const PagePool& pool, const int32_t* to_table, int32
 // ---------------------------------------------------------------------------------------------------------------
 // Packed rows into the last rows of their sequences.  A workgroup takes a.block rows of one sequence in one layer, keys or values,
 // and all heads; a thread 16 bytes of a cached row at a time.  The threads of an fp8 row (4 or 8) find its scale by exchange, so each
-// element is read once.  16 prompts of 1,024 rows into fp8 pages, 32 heads, 407 MB: 87 us, 4.7 TB/s (a large copy: 4.9).
+// element is read once.  16 prompts of 1,024 bf16 rows into fp8 pages, 32 heads of 128 channels, 407 MB: 87 us, 4.7 TB/s (a large
+// copy: 4.9).
 template <int PDT>
 struct Raw8 {
   uint4 p[PDT == FSX_F32 ? 2 : 1];
@@ -324,8 +325,8 @@ hipError_t launch_page_write(PageWriteArgs a, int n, const int32_t* seqs, const 
   const PagePool& p = a.pool;
   int64_t total = 0;
   for (int i = 0; i < n; ++i) total += rows[i];
-  // rows of a workgroup: four pieces for every thread, once there are two workgroups for each CU (15,000 uneven rows of 4 heads x 64
-  // into fp8 pages: 10 us, with eight for each 15)
+  // rows of a workgroup: four pieces for every thread, once there are two workgroups for each CU (15,000 rows of 4 heads of 64 channels,
+  // uneven sequences, into fp8 pages: 10 us, with eight for each 15)
   const int64_t full = std::max<int64_t>(1, 4 * 256 / (p.Hk * (p.D / (p.fp8 ? 16 : 8))));
   a.block = (int)std::max<int64_t>({1, std::min<int64_t>(full, total * a.n_layers * 2 / 512), (total >> 23) + 1});
   for (int i = 0; i < n;) {

@@ -97,7 +97,8 @@ __global__ __launch_bounds__(256) void k_rotary(RotaryArgs a) {
 }
 
 hipError_t launch_rotary(RotaryArgs a, hipStream_t s) {
-  // the widest piece that the widths, strides and addresses allow
+  // the widest piece that the widths, strides and addresses allow.  Pairs that are not a multiple of four go element by element, in 2 or
+  // 4 bytes an access: the two halves of a head then begin at different places of their 16 bytes.
   const int es = a.f32 ? 4 : 2;
   const auto fits = [&](int v) {
     const int64_t b = v * es;
