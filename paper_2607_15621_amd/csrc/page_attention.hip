@@ -165,8 +165,8 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 || CT == 1 ? 2 : 1) void k_p
     const int ch = NC * (threadIdx.x & 15), en = e + min((int)(threadIdx.x >> 4) / width, members - 1);
     const int n_parts = a.all[en + 1] - a.all[en], out_row = a.row[en];
     const int slot = a.all[en] + part + (shared ? a.parts[en + 1] - a.parts[en] : 0);  // parts of its own rows, then of the shared
-    // The lane's columns: queries of the channels that its keys have in step s.  Fp32 queries are rounded to bf16 (2^-9 of each), as the
-    // attention over whole prompts rounds them: its scores and these are the same, and bf16 is what the keys were rounded to.
+    // The lane's columns: queries of the channels that its keys have in step s.  Fp32 queries are rounded to bf16 (by 2^-8 of
+    // each at most), as the attention over whole prompts rounds them: a token's scores are the same in both, and no key has more bits.
     uint4 q[CT][KS];
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) {
